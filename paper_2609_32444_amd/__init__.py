@@ -44,6 +44,21 @@ from ._binding import (  # noqa: F401
     workspace_bytes,
     workspace_bytes_ex,
 )
+from ._tokens import (  # noqa: F401
+    KL_FORWARD,
+    KL_REVERSE,
+    TOP_MAX_K,
+    DistillCall,
+    SampleCall,
+    TopLogitsCall,
+    distill_bwd,
+    distill_fwd,
+    distill_workspace_bytes,
+    sample,
+    sample_workspace_bytes,
+    top_logits,
+    top_logits_workspace_bytes,
+)
 
 __all__ = [
     "CisError", "CIS_BF16", "CIS_F32", "LMHEAD_CHUNK", "LossCall", "NOALLOC_MAX_T", "OP_CIS", "OP_EXACT", "OP_ICEPOP", "OP_KPOP",
@@ -52,4 +67,7 @@ __all__ = [
     "lmhead_workspace_bytes", "load_library", "loss_bwd", "loss_bwd_ex", "loss_bwd_noalloc",
     "loss_fwd", "loss_fwd_ex", "params", "read_stats", "status_string", "weights", "weights_ex",
     "workspace_bytes", "workspace_bytes_ex",
+    "KL_FORWARD", "KL_REVERSE", "TOP_MAX_K", "DistillCall", "SampleCall", "TopLogitsCall",
+    "distill_bwd", "distill_fwd", "distill_workspace_bytes", "sample", "sample_workspace_bytes",
+    "top_logits", "top_logits_workspace_bytes",
 ]

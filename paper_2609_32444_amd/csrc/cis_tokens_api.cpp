@@ -1,0 +1,248 @@
+// C-ABI entry points of the token operators (cis_tokens.h): argument checks, launch configuration and
+// launches on the caller's stream. No device memory is allocated and nothing synchronises.
+#include <hip/hip_runtime.h>
+#include <math.h>
+#include <stdint.h>
+#include <string.h>
+
+#include <mutex>
+
+#include "cis_tok.h"
+
+namespace {
+
+constexpr int64_t kMaxV = int64_t(1) << 28;
+constexpr int kMaxDevices = 64;
+
+// Compute units of the current device, or CIS_ERR_DEVICE.
+int device_cus() {
+  static std::mutex mu;
+  static int cus[kMaxDevices] = {};   // 0: not looked at yet
+  int dev = -1;
+  if (hipGetDevice(&dev) != hipSuccess || dev < 0 || dev >= kMaxDevices) return CIS_ERR_DEVICE;
+  std::lock_guard<std::mutex> lk(mu);
+  if (cus[dev] == 0) {
+    hipDeviceProp_t prop;
+    if (hipGetDeviceProperties(&prop, dev) != hipSuccess) return CIS_ERR_DEVICE;
+    cus[dev] = strncmp(prop.gcnArchName, "gfx950", 6) == 0 ? prop.multiProcessorCount
+                                                           : CIS_ERR_DEVICE;
+  }
+  return cus[dev];
+}
+
+bool aligned(const void* p, size_t a) { return ((uintptr_t)p % a) == 0; }
+bool known(int dtype) { return dtype == CIS_BF16 || dtype == CIS_F32; }
+int elem_bytes(int dtype) { return dtype == CIS_BF16 ? 2 : 4; }
+
+int launch(const void* fn, int64_t grid, int block, void* arg, hipStream_t stream) {
+  void* args[] = {arg};
+  return hipLaunchKernel(fn, dim3((unsigned)grid), dim3(block), args, 0, stream) == hipSuccess
+             ? CIS_OK
+             : CIS_ERR_LAUNCH;
+}
+
+// The rows' shape; pointers and alignment follow once every size has been found right.
+int check_shape(int dtype, int64_t T, int64_t V, int64_t ld) {
+  if (!known(dtype)) return CIS_ERR_DTYPE;
+  if (T < 0 || V < 1 || V > kMaxV || ld < V || ld > INT64_MAX / elem_bytes(dtype))
+    return CIS_ERR_SHAPE;
+  return CIS_OK;
+}
+bool aligned_rows(const void* p, int dtype, int64_t ld) {
+  return aligned(p, 16) && (ld * elem_bytes(dtype)) % 16 == 0;
+}
+int check_workspace(const void* workspace, size_t have, size_t need) {
+  if (!aligned(workspace, 256)) return CIS_ERR_ALIGN;
+  return have < need ? CIS_ERR_WORKSPACE : CIS_OK;
+}
+
+cis::TokRows tok_rows(const void* logits, int dtype, int64_t T, int64_t V, int64_t ld,
+                      const uint8_t* mask) {
+  const int epv = 16 / elem_bytes(dtype);
+  return cis::TokRows{logits, ld * elem_bytes(dtype), mask, T, (int32_t)V,
+                      (int32_t)((V + epv - 1) / epv)};
+}
+
+// Workgroups for T rows of one each; the kernels loop beyond that many.
+int64_t row_grid(int64_t T) { return T < (int64_t(1) << 20) ? T : int64_t(1) << 20; }
+
+// Temperatures of a softmax: log2(e) / temperature and a logit's exponent stay within float32.
+bool softmax_temperature(float t) { return t >= 0x1p-64f && t <= 0x1p64f; }
+
+// The call's statistics and loss, as in the loss entry points: few rows by one workgroup, more
+// by one per part and another over the parts (at wpre, which nothing else uses here).
+int launch_finalize(char* base, const cis::WsLayout& L, int64_t T, float* loss_out,
+                    hipStream_t stream) {
+  auto f = [&](size_t off) { return reinterpret_cast<float*>(base + off); };
+  cis::FinalizeArgs fa{f(L.terms), reinterpret_cast<uint8_t*>(base + L.flags), f(L.logk),
+                       f(L.excess), T, reinterpret_cast<cis_stats_t*>(base), loss_out, nullptr,
+                       reinterpret_cast<cis::RowStats*>(base + L.wpre), 0, 0};
+  if (T <= cis::kFinalizeOne) {
+    const int block = T <= cis::kFinalizeSmall ? 256 : cis::kFinalizeBlock;
+    return launch(cis::finalize_kernel(block, false), 1, block, &fa, stream);
+  }
+  const int64_t even = (T + cis::kFinalizeParts - 1) / cis::kFinalizeParts;
+  fa.rows = even <= cis::kFinalizeRows ? cis::kFinalizeRows : (even + 3) / 4 * 4;
+  fa.nparts = (int32_t)((T + fa.rows - 1) / fa.rows);
+  if (int rc = launch(cis::finalize_kernel(256, true), fa.nparts, 256, &fa, stream)) return rc;
+  return launch(cis::finalize_parts_kernel(), 1, cis::kFinalizeParts, &fa, stream);
+}
+
+struct DistillCall {
+  const void* logits;
+  int dtype;
+  int64_t T, V, ld;
+  const int32_t* ids;
+  const float* values;
+  int64_t K, ld_top;
+  const float *tail, *weight;
+  const uint8_t* mask;
+  const cis_distill_params_t* prm;
+  bool bwd;
+  void* dlogits;
+  int64_t ld_g;
+  float *terms, *loss;
+  void* workspace;
+  size_t workspace_bytes;
+};
+
+int run_distill(const DistillCall& c, hipStream_t stream) {
+  if (!c.prm) return CIS_ERR_NULL;
+  if (int rc = check_shape(c.dtype, c.T, c.V, c.ld)) return rc;
+  const int es = elem_bytes(c.dtype);
+  if (c.K < 1 || c.K > CIS_TOP_MAX_K || c.ld_top < c.K || c.ld_top > INT64_MAX / 4)
+    return CIS_ERR_SHAPE;
+  if (c.bwd && (c.ld_g < c.V || c.ld_g > INT64_MAX / es)) return CIS_ERR_SHAPE;
+  const cis_distill_params_t& p = *c.prm;
+  if (p.kind != CIS_KL_FORWARD && p.kind != CIS_KL_REVERSE) return CIS_ERR_PARAM;
+  if (!softmax_temperature(p.temperature) || !isfinite(p.scale)) return CIS_ERR_PARAM;
+  if (p.kind == CIS_KL_REVERSE && c.T > 0 && !c.tail) return CIS_ERR_PARAM;
+  if (!c.workspace) return CIS_ERR_NULL;
+  if (c.T > 0 && (!c.logits || !c.ids || !c.values || (c.bwd && !c.dlogits))) return CIS_ERR_NULL;
+  if (int rc = check_workspace(c.workspace, c.workspace_bytes,
+                               cis_distill_workspace_bytes(c.T, c.V, c.K, c.dtype)))
+    return rc;
+  if (c.T > 0) {
+    if (!aligned_rows(c.logits, c.dtype, c.ld)) return CIS_ERR_ALIGN;
+    if (c.bwd) {
+      if (!aligned_rows(c.dlogits, c.dtype, c.ld_g)) return CIS_ERR_ALIGN;
+      const uintptr_t a0 = (uintptr_t)c.logits, a1 = a0 + (uintptr_t)(c.T * c.ld * es);
+      const uintptr_t b0 = (uintptr_t)c.dlogits, b1 = b0 + (uintptr_t)(c.T * c.ld_g * es);
+      if (a0 == b0 ? c.ld_g != c.ld : a0 < b1 && b0 < a1) return CIS_ERR_ALIAS;
+    }
+  }
+  if (const int cus = device_cus(); cus < 0) return cus;
+
+  char* base = static_cast<char*>(c.workspace);
+  const cis::WsLayout L = cis::ws_layout(c.T, 0);
+  if (c.T > 0) {
+    cis::DistillArgs a{};
+    a.r = tok_rows(c.logits, c.dtype, c.T, c.V, c.ld, c.mask);
+    a.dlogits = c.dlogits;
+    a.grow_bytes = c.bwd ? c.ld_g * es : 0;
+    a.ids = c.ids;
+    a.values = c.values;
+    a.ld_top = c.ld_top;
+    a.K = (int32_t)c.K;
+    a.tail = c.tail;
+    a.weight = c.weight;
+    a.reverse = p.kind == CIS_KL_REVERSE;
+    a.temperature = p.temperature;
+    a.scale = p.scale;
+    a.terms_user = c.terms;
+    a.terms_ws = reinterpret_cast<float*>(base + L.terms);
+    a.flags_ws = reinterpret_cast<uint8_t*>(base + L.flags);
+    a.logk_ws = reinterpret_cast<float*>(base + L.logk);
+    a.excess_ws = reinterpret_cast<float*>(base + L.excess);
+    if (int rc = launch(cis::distill_kernel(c.dtype, c.bwd), row_grid(c.T), cis::kTokBlock, &a,
+                        stream))
+      return rc;
+  }
+  return launch_finalize(base, L, c.T, c.loss, stream);
+}
+
+}  // namespace
+
+extern "C" {
+
+size_t cis_sample_workspace_bytes(int64_t T, int64_t V, int dtype) {
+  return T < 0 || V < 1 || V > kMaxV || !known(dtype) ? 0 : 256;
+}
+
+size_t cis_top_logits_workspace_bytes(int64_t T, int64_t V, int64_t K, int dtype) {
+  return T < 0 || V < 1 || V > kMaxV || K < 1 || K > CIS_TOP_MAX_K || !known(dtype) ? 0 : 256;
+}
+
+size_t cis_distill_workspace_bytes(int64_t T, int64_t V, int64_t K, int dtype) {
+  if (T < 0 || V < 1 || V > kMaxV || K < 1 || K > CIS_TOP_MAX_K || !known(dtype)) return 0;
+  return cis::ws_layout(T, 0).total;
+}
+
+int cis_sample(const void* logits, int dtype, int64_t T, int64_t V, int64_t ld, const float* u,
+               const uint8_t* mask, const cis_sample_params_t* params, const float* temperature,
+               const int32_t* top_k, const float* top_p, const float* min_p, int64_t* ids_out,
+               float* logp_out, float* logp_kept_out, void* workspace, size_t workspace_bytes,
+               hipStream_t stream) {
+  if (!params) return CIS_ERR_NULL;
+  if (int rc = check_shape(dtype, T, V, ld)) return rc;
+  const cis_sample_params_t& p = *params;
+  if (!temperature && !(p.temperature >= 0.f && isfinite(p.temperature))) return CIS_ERR_PARAM;
+  if (!top_k && p.top_k < 0) return CIS_ERR_PARAM;
+  if (!top_p && !(p.top_p > 0.f && p.top_p <= 1.f)) return CIS_ERR_PARAM;
+  if (!min_p && !(p.min_p >= 0.f && p.min_p <= 1.f)) return CIS_ERR_PARAM;
+  if (!workspace) return CIS_ERR_NULL;
+  if (T > 0 && (!logits || !u || !ids_out)) return CIS_ERR_NULL;
+  if (int rc = check_workspace(workspace, workspace_bytes, cis_sample_workspace_bytes(T, V, dtype)))
+    return rc;
+  if (T > 0 && !aligned_rows(logits, dtype, ld)) return CIS_ERR_ALIGN;
+  if (const int cus = device_cus(); cus < 0) return cus;
+  if (T == 0) return CIS_OK;
+  cis::SampleArgs a{tok_rows(logits, dtype, T, V, ld, mask), u, p, temperature, top_k, top_p, min_p,
+                    ids_out, logp_out, logp_kept_out};
+  return launch(cis::sample_kernel(dtype), row_grid(T), cis::kTokBlock, &a, stream);
+}
+
+int cis_top_logits(const void* logits, int dtype, int64_t T, int64_t V, int64_t ld,
+                   const uint8_t* mask, int64_t K, float temperature, int32_t* ids_out,
+                   float* values_out, float* tail_out, void* workspace, size_t workspace_bytes,
+                   hipStream_t stream) {
+  if (int rc = check_shape(dtype, T, V, ld)) return rc;
+  if (K < 1 || K > CIS_TOP_MAX_K) return CIS_ERR_SHAPE;
+  if (!softmax_temperature(temperature)) return CIS_ERR_PARAM;
+  if (!workspace) return CIS_ERR_NULL;
+  if (T > 0 && (!logits || !ids_out || !values_out)) return CIS_ERR_NULL;
+  if (int rc = check_workspace(workspace, workspace_bytes,
+                               cis_top_logits_workspace_bytes(T, V, K, dtype)))
+    return rc;
+  if (T > 0 && !aligned_rows(logits, dtype, ld)) return CIS_ERR_ALIGN;
+  if (const int cus = device_cus(); cus < 0) return cus;
+  if (T == 0) return CIS_OK;
+  cis::TopArgs a{tok_rows(logits, dtype, T, V, ld, mask), (int32_t)K, temperature, ids_out,
+                 values_out, tail_out};
+  return launch(cis::top_kernel(dtype), row_grid(T), cis::kTokBlock, &a, stream);
+}
+
+int cis_distill_fwd(const void* logits, int dtype, int64_t T, int64_t V, int64_t ld,
+                    const int32_t* top_ids, const float* top_values, int64_t K, int64_t ld_top,
+                    const float* top_tail, const float* row_weight, const uint8_t* mask,
+                    const cis_distill_params_t* params, float* terms_out, float* loss_out,
+                    void* workspace, size_t workspace_bytes, hipStream_t stream) {
+  return run_distill(DistillCall{logits, dtype, T, V, ld, top_ids, top_values, K, ld_top, top_tail,
+                                 row_weight, mask, params, false, nullptr, 0, terms_out, loss_out,
+                                 workspace, workspace_bytes},
+                     stream);
+}
+
+int cis_distill_bwd(const void* logits, int dtype, int64_t T, int64_t V, int64_t ld,
+                    const int32_t* top_ids, const float* top_values, int64_t K, int64_t ld_top,
+                    const float* top_tail, const float* row_weight, const uint8_t* mask,
+                    const cis_distill_params_t* params, void* dlogits, int64_t ld_g,
+                    float* terms_out, float* loss_out, void* workspace, size_t workspace_bytes,
+                    hipStream_t stream) {
+  return run_distill(DistillCall{logits, dtype, T, V, ld, top_ids, top_values, K, ld_top, top_tail,
+                                 row_weight, mask, params, true, dlogits, ld_g, terms_out, loss_out,
+                                 workspace, workspace_bytes},
+                     stream);
+}
+
+}  // extern "C"
