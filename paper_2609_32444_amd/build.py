@@ -15,7 +15,7 @@ ROOT = os.path.dirname(HERE)
 LIB_PATH = os.path.join(HERE, "libcis.so")
 SOURCES = [os.path.join(HERE, "csrc", f) for f in
            ("cis_kernels.hip", "cis_kernels_ext.hip", "cis_gemm.hip", "cis_api.cpp",
-            "cis_sample.hip", "cis_distill.hip", "cis_tokens_api.cpp")]
+            "cis_top.hip", "cis_sample.hip", "cis_distill.hip", "cis_tokens_api.cpp")]
 # bandwidth probes for the roofline (a separate library; not part of the loss)
 PROBE_PATH = os.path.join(HERE, "libcis_probe.so")
 PROBE_SOURCES = [os.path.join(HERE, "csrc", "bw_probe.hip")]

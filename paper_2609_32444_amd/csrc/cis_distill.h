@@ -11,9 +11,6 @@
 namespace cis {
 
 constexpr float kLn2 = 0.693147180559945309417f;
-// Lowest reference: keeps R finite where a row or a lane holds nothing but -inf.
-constexpr float kMinExp = -0x1p126f;
-
 // expm1(d) - d >= 0, to a few units in the last place (near 0 by its series, which does not
 // cancel: nine terms, the first left out below 2^-24 of the sum up to |d| = 0.6).
 __device__ __forceinline__ float expm1_less(float d) {

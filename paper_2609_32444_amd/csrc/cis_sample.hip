@@ -1,5 +1,4 @@
-// Sampling and top-logits kernels (gfx950): one workgroup per row, which it reads as often as its
-// cuts take.
+// Sampling kernels (gfx950): one workgroup per row, which it reads as often as its cuts take.
 #include "cis_tok_row.h"
 
 namespace cis {
@@ -191,128 +190,9 @@ __global__ __launch_bounds__(kTokBlock) void cis_sample_kernel(const SampleArgs 
   }
 }
 
-// ------------------------------------------------------------------------------------------
-// The K largest logits of a row, sorted by one workgroup, and the log-sum-exp of the others.
-// ------------------------------------------------------------------------------------------
-struct TopShared {
-  CutShared cut;
-  float f[16];
-  u64 u[16];
-  double d[16];
-  uint32_t ties[kChunks];
-  uint32_t count;
-  u64 list[CIS_TOP_MAX_K];   // key << 32 | ~id: falls in the order of the tokens
-};
-
-template <class E>
-__global__ __launch_bounds__(kTokBlock) void cis_top_kernel(const TopArgs a) {
-  constexpr int BLOCK = kTokBlock, NW = BLOCK / 64, EPV = E::kPerVec;
-  __shared__ TopShared sh;
-  const int tid = threadIdx.x, lane = tid & 63, wid = tid >> 6;
-  const int V = a.r.V, nvec = a.r.nvec;
-  const float c = kLog2e / a.temperature;
-  for (int64_t row = blockIdx.x; row < a.r.T; row += gridDim.x) {
-    const __amdgpu_buffer_rsrc_t rs = tok_rsrc(a.r, row);
-    const bool on = tok_on(a.r, row);
-    RowFacts facts{0.f, true, 0};
-    if (on) facts = row_facts<E, BLOCK>(rs, nvec, V, sh.f, sh.u);
-    const int n = !facts.finite ? 0 : facts.tokens < (u64)a.K ? (int)facts.tokens : a.K;
-    if (n > 0) {
-      const Cut cut = radix_cut<E, BLOCK>(rs, nvec, V, (u64)n, 0u, [](float) { return 1u; }, sh.cut);
-      const int cv = chunk_vecs(nvec);
-      if (tid == 0) sh.count = 0;
-      for (int ch = wid; ch < kChunks; ch += NW) {
-        uint32_t t = 0;
-        for (int v = ch * cv + lane; v < min((ch + 1) * cv, nvec); v += 64) {
-          float f[EPV];
-          tok_vec<E>(rs, v, V, f);
-#pragma unroll
-          for (int e = 0; e < EPV; ++e) t += order_key(f[e]) == cut.key ? 1 : 0;
-        }
-        t = wave_sum(t);
-        if (lane == 0) sh.ties[ch] = t;
-      }
-      __syncthreads();
-      float top = -INFINITY;   // of the tokens that are not listed, and their sum relative to it
-      double rest = 0.0;
-      uint32_t before = 0;
-      for (int ch = 0; ch < kChunks; ++ch) {   // (each wave adds up the pieces before its own)
-        if (ch % NW == wid) {
-          uint32_t tb = before;
-          for (int v0 = ch * cv; v0 < min((ch + 1) * cv, nvec); v0 += 64) {
-            const int v = v0 + lane;
-            float f[EPV];
-            if (v < nvec) {
-              tok_vec<E>(rs, v, V, f);
-            } else {
-              for (int e = 0; e < EPV; ++e) f[e] = -INFINITY;
-            }
-            uint32_t nt = 0;
-            for (int e = 0; e < EPV; ++e) nt += order_key(f[e]) == cut.key ? 1 : 0;
-            const uint32_t upto = tb + wave_scan(nt, lane);
-            uint32_t t = upto - nt;
-            float m = top, s = 0.f;
-            for (int e = 0; e < EPV; ++e) {
-              const uint32_t key = order_key(f[e]);
-              const bool tie = key == cut.key;
-              if (key > cut.key || (tie && t < cut.ties)) {
-                sh.list[atomicAdd(&sh.count, 1u)] =
-                    ((u64)key << 32) | (uint32_t)~(uint32_t)(v * EPV + e);
-                f[e] = -INFINITY;
-              }
-              m = fmaxf(m, f[e]);
-              t += tie ? 1 : 0;
-            }
-            if (m > -INFINITY) {
-              for (int e = 0; e < EPV; ++e) s += fast_exp2((f[e] - m) * c);
-              rest = rest * fast_exp2((top - m) * c) + s;
-              top = m;
-            }
-            tb = __shfl(upto, 63, 64);
-          }
-        }
-        before += sh.ties[ch];
-      }
-      const float most = block_max<NW>(top, sh.f);
-      if (top > -INFINITY) rest *= fast_exp2((top - most) * c);
-      rest = block_sum<NW>(rest, sh.d);
-      // bitonic sort, falling, of the next power of two (0 sorts last)
-      int P = 1;
-      while (P < n) P <<= 1;
-      if (tid >= n && tid < P) sh.list[tid] = 0;
-      for (int size = 2; size <= P; size <<= 1)
-        for (int step = size >> 1; step > 0; step >>= 1) {
-          __syncthreads();
-          const int i = 2 * tid - (tid & (step - 1)), j = i + step;
-          if (j < P) {
-            const u64 x = sh.list[i], y = sh.list[j];
-            if (((i & size) == 0) == (x < y)) {
-              sh.list[i] = y;
-              sh.list[j] = x;
-            }
-          }
-        }
-      __syncthreads();
-      if (tid == 0 && a.tail)
-        a.tail[row] = most > -INFINITY ? most / a.temperature + logf((float)rest) : -INFINITY;
-    } else if (tid == 0 && a.tail) {
-      a.tail[row] = facts.finite ? -INFINITY : NAN;
-    }
-    for (int k = tid; k < a.K; k += BLOCK) {
-      const u64 x = k < n ? sh.list[k] : 0;
-      a.ids[row * a.K + k] = k < n ? (int32_t)~(uint32_t)x : -1;
-      a.values[row * a.K + k] = k < n ? key_value((uint32_t)(x >> 32)) : -INFINITY;
-    }
-    __syncthreads();
-  }
-}
-
 const void* sample_kernel(int dtype) {
   return dtype == CIS_BF16 ? (const void*)&cis_sample_kernel<Bf16>
                            : (const void*)&cis_sample_kernel<F32>;
-}
-const void* top_kernel(int dtype) {
-  return dtype == CIS_BF16 ? (const void*)&cis_top_kernel<Bf16> : (const void*)&cis_top_kernel<F32>;
 }
 
 }  // namespace cis

@@ -20,6 +20,50 @@ struct TokRows {
 // add up within 32 bits, and the 2^28 of the longest row within 64.
 constexpr uint32_t kDrawOne = 1u << 28;
 
+// What a scan of the rows leaves in the workspace: the row in chunks of kScanVecs vectors (one wave's),
+// each with its largest logit m and the sum of exp2(z c - R) over its tokens, R = m c rounded (at
+// least kMinExp), added up in double from the float32 sums of its vectors; and the largest logit
+// of every group of `gv` vectors, in the logits' format. A chunk with a NaN or a +inf has a NaN sum;
+// one without tokens the largest logit -inf.
+constexpr int kScanVecs = 512;
+constexpr int kScanBlock = 256;
+struct TokScan {
+  void* gmax;      // [T, ngrp]
+  float* cmax;     // [T, nch]
+  double* csum;    // [T, nch]
+  int32_t nch, ngrp, gv;
+};
+// Vectors per group, for the K largest logits of a row of nvec vectors: 8 (a 128-byte line),
+// where that leaves four times as many groups as logits are asked for, or each by itself. (The
+// groups whose largest logit is among the K largest of those hold the row's K largest logits; the
+// fewer groups, the more else they hold.)
+inline int32_t scan_group(int32_t nvec, int64_t K) { return nvec / 8 >= 4 * K ? 8 : 1; }
+
+struct ScanLayout {
+  size_t gmax, cmax, csum, total;
+  int32_t nch, ngrp, gv;
+};
+inline ScanLayout scan_layout(int64_t T, int32_t nvec, int elem_bytes, int32_t gv) {
+  ScanLayout L{};
+  L.nch = (nvec + kScanVecs - 1) / kScanVecs;
+  L.gv = gv;
+  L.ngrp = (nvec + gv - 1) / gv;
+  L.csum = 0;
+  L.cmax = L.csum + align_up((size_t)T * L.nch * 8, 256);
+  L.gmax = L.cmax + align_up((size_t)T * L.nch * 4, 256);
+  L.total = L.gmax + align_up((size_t)T * L.ngrp * elem_bytes, 256);
+  return L;
+}
+
+// The factor of a logit's exponent in base 2.
+inline float scan_c(float temperature) { return 1.44269504088896340736f / temperature; }
+
+struct ScanArgs {
+  TokRows r;
+  TokScan s;
+  float c;         // log2(e) / temperature
+};
+
 struct SampleArgs {
   TokRows r;
   const float* u;
@@ -35,8 +79,9 @@ struct SampleArgs {
 
 struct TopArgs {
   TokRows r;
+  TokScan s;
   int32_t K;
-  float temperature;
+  float temperature, c;       // c = scan_c(temperature)
   int32_t* ids;
   float* values;
   float* tail;                // nullable
@@ -62,6 +107,8 @@ struct DistillArgs {
 };
 
 constexpr int kTokBlock = 1024;
+constexpr int kTopBlock = 256;
+const void* scan_kernel(int dtype, int32_t gv);
 const void* sample_kernel(int dtype);
 const void* top_kernel(int dtype);
 const void* distill_kernel(int dtype, bool bwd);

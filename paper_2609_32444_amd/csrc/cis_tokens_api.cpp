@@ -56,11 +56,29 @@ int check_workspace(const void* workspace, size_t have, size_t need) {
   return have < need ? CIS_ERR_WORKSPACE : CIS_OK;
 }
 
+int32_t row_vecs(int64_t V, int dtype) {
+  const int epv = 16 / elem_bytes(dtype);
+  return (int32_t)((V + epv - 1) / epv);
+}
 cis::TokRows tok_rows(const void* logits, int dtype, int64_t T, int64_t V, int64_t ld,
                       const uint8_t* mask) {
-  const int epv = 16 / elem_bytes(dtype);
-  return cis::TokRows{logits, ld * elem_bytes(dtype), mask, T, (int32_t)V,
-                      (int32_t)((V + epv - 1) / epv)};
+  return cis::TokRows{logits, ld * elem_bytes(dtype), mask, T, (int32_t)V, row_vecs(V, dtype)};
+}
+
+cis::ScanLayout top_layout(int64_t T, int64_t V, int64_t K, int dtype) {
+  const int32_t nvec = row_vecs(V, dtype);
+  return cis::scan_layout(T, nvec, elem_bytes(dtype), cis::scan_group(nvec, K));
+}
+cis::TokScan scan_at(char* base, const cis::ScanLayout& L) {
+  return cis::TokScan{base + L.gmax, reinterpret_cast<float*>(base + L.cmax),
+                      reinterpret_cast<double*>(base + L.csum), L.nch, L.ngrp, L.gv};
+}
+int launch_scan(const cis::TokRows& r, const cis::TokScan& s, int dtype, float c,
+                hipStream_t stream) {
+  cis::ScanArgs a{r, s, c};
+  const int64_t per = cis::kScanBlock / 64, need = (r.T * s.nch + per - 1) / per;
+  const int64_t cap = int64_t(1) << 23;   // (the kernel loops beyond: HIP refuses 2^32 work items)
+  return launch(cis::scan_kernel(dtype, s.gv), need < cap ? need : cap, cis::kScanBlock, &a, stream);
 }
 
 // Workgroups for T rows of one each; the kernels loop beyond that many.
@@ -170,7 +188,9 @@ size_t cis_sample_workspace_bytes(int64_t T, int64_t V, int dtype) {
 }
 
 size_t cis_top_logits_workspace_bytes(int64_t T, int64_t V, int64_t K, int dtype) {
-  return T < 0 || V < 1 || V > kMaxV || K < 1 || K > CIS_TOP_MAX_K || !known(dtype) ? 0 : 256;
+  if (T < 0 || V < 1 || V > kMaxV || K < 1 || K > CIS_TOP_MAX_K || !known(dtype)) return 0;
+  const size_t n = top_layout(T, V, K, dtype).total;
+  return n < 256 ? 256 : n;
 }
 
 size_t cis_distill_workspace_bytes(int64_t T, int64_t V, int64_t K, int dtype) {
@@ -217,9 +237,13 @@ int cis_top_logits(const void* logits, int dtype, int64_t T, int64_t V, int64_t 
   if (T > 0 && !aligned_rows(logits, dtype, ld)) return CIS_ERR_ALIGN;
   if (const int cus = device_cus(); cus < 0) return cus;
   if (T == 0) return CIS_OK;
-  cis::TopArgs a{tok_rows(logits, dtype, T, V, ld, mask), (int32_t)K, temperature, ids_out,
-                 values_out, tail_out};
-  return launch(cis::top_kernel(dtype), row_grid(T), cis::kTokBlock, &a, stream);
+  const cis::TokRows r = tok_rows(logits, dtype, T, V, ld, mask);
+  const cis::ScanLayout L = top_layout(T, V, K, dtype);
+  const cis::TokScan s = scan_at(static_cast<char*>(workspace), L);
+  if (int rc = launch_scan(r, s, dtype, cis::scan_c(temperature), stream)) return rc;
+  cis::TopArgs a{r, s, (int32_t)K, temperature, cis::scan_c(temperature),
+                 ids_out, values_out, tail_out};
+  return launch(cis::top_kernel(dtype), row_grid(T), cis::kTopBlock, &a, stream);
 }
 
 int cis_distill_fwd(const void* logits, int dtype, int64_t T, int64_t V, int64_t ld,
