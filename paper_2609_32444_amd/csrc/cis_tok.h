@@ -82,6 +82,7 @@ struct TopArgs {
   TokScan s;
   int32_t K;
   float temperature, c;       // c = scan_c(temperature)
+  int64_t row0;               // the launch's first row
   int32_t* ids;
   float* values;
   float* tail;                // nullable
@@ -110,7 +111,8 @@ constexpr int kTokBlock = 1024;
 constexpr int kTopBlock = 256;
 const void* scan_kernel(int dtype, int32_t gv);
 const void* sample_kernel(int dtype);
-const void* top_kernel(int dtype);
+const void* top_kernel(int dtype, int64_t K);
+int top_block(int64_t K);
 const void* distill_kernel(int dtype, bool bwd);
 
 }  // namespace cis

@@ -81,6 +81,8 @@ int launch_scan(const cis::TokRows& r, const cis::TokScan& s, int dtype, float c
   return launch(cis::scan_kernel(dtype, s.gv), need < cap ? need : cap, cis::kScanBlock, &a, stream);
 }
 
+// Rows per launch of kernels of one workgroup per row (HIP refuses 2^32 work items).
+constexpr int64_t kMaxRows = int64_t(1) << 20;
 // Workgroups for T rows of one each; the kernels loop beyond that many.
 int64_t row_grid(int64_t T) { return T < (int64_t(1) << 20) ? T : int64_t(1) << 20; }
 
@@ -241,9 +243,13 @@ int cis_top_logits(const void* logits, int dtype, int64_t T, int64_t V, int64_t 
   const cis::ScanLayout L = top_layout(T, V, K, dtype);
   const cis::TokScan s = scan_at(static_cast<char*>(workspace), L);
   if (int rc = launch_scan(r, s, dtype, cis::scan_c(temperature), stream)) return rc;
-  cis::TopArgs a{r, s, (int32_t)K, temperature, cis::scan_c(temperature),
-                 ids_out, values_out, tail_out};
-  return launch(cis::top_kernel(dtype), row_grid(T), cis::kTopBlock, &a, stream);
+  cis::TopArgs a{r, s, (int32_t)K, temperature, cis::scan_c(temperature), 0, ids_out, values_out,
+                 tail_out};
+  for (; a.row0 < T; a.row0 += kMaxRows)
+    if (int rc = launch(cis::top_kernel(dtype, K), T - a.row0 < kMaxRows ? T - a.row0 : kMaxRows,
+                        cis::top_block(K), &a, stream))
+      return rc;
+  return CIS_OK;
 }
 
 int cis_distill_fwd(const void* logits, int dtype, int64_t T, int64_t V, int64_t ld,
