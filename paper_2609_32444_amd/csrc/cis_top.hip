@@ -167,7 +167,7 @@ __device__ __forceinline__ void sort_list(u64* list, int count) {
 }
 
 template <class E, int BLOCK, int LIST>
-__global__ __launch_bounds__(BLOCK) __attribute__((amdgpu_waves_per_eu(6))) void cis_top_kernel(
+__global__ __launch_bounds__(BLOCK) __attribute__((amdgpu_waves_per_eu(4))) void cis_top_kernel(
     const TopArgs a) {
   constexpr int NW = BLOCK / 64, EPV = E::kPerVec;
   typedef std::conditional_t<EPV == 8, uint16_t, uint32_t> elem;
@@ -255,9 +255,18 @@ __global__ __launch_bounds__(BLOCK) __attribute__((amdgpu_waves_per_eu(6))) void
       if (!finer && !coarser) break;
       scale *= finer ? 16.f : 0.0625f;
     }
-    auto in = [&](float f) {
-      return f > -INFINITY && (uint32_t)below(f, M, scale, 255.f) <= bin;
-    };
+    // what is taken reaches the smallest of the groups' largest logits within the steps
+    float least = INFINITY;
+    if (bin == 256)
+      least = -FLT_MAX;
+    else
+      each_group([&](int, float x) {
+        if (x > -INFINITY && (uint32_t)below(x, M, scale, 255.f) <= bin) least = fminf(least, x);
+      });
+    least = -wave_max(-least);
+    if (lane == 0) sh.f[wid] = least;
+    __syncthreads();
+    for (int w = 0; w < NW; ++w) least = fminf(least, sh.f[w]);
     // a place in a list for every lane that takes one
     auto place = [&](bool take, uint32_t* counter) {
       const u64 who = __ballot(take);
@@ -270,7 +279,7 @@ __global__ __launch_bounds__(BLOCK) __attribute__((amdgpu_waves_per_eu(6))) void
     };
     // 2. the list
     each_group([&](int g, float x) {
-      const bool take = in(x);
+      const bool take = x >= least;
       const uint32_t at = place(take, &sh.groups);
       if (take && at < LIST / 2) sh.group[at] = (uint32_t)g;
     });
@@ -289,32 +298,35 @@ __global__ __launch_bounds__(BLOCK) __attribute__((amdgpu_waves_per_eu(6))) void
           if (i < nv) v[J] = gv == 1 ? (int)sh.group[i] : (int)sh.group[i >> 3] * 8 + (i & 7);
           x[J] = bload_aux<0>(rs, v[J] < nvec ? (uint32_t)v[J] * 16u : kOutOfRange);
         });
-        // a lane's logits that are taken, as bits, and places for all of them at once
-        uint32_t bits = 0;
+        // places for all that a wave takes at once
+        uint32_t mine = 0;
         static_for<U>([&](auto J) {
           float f[EPV];
           E::unpack(x[J], f);
-          if ((v[J] + 1) * EPV > V) mask_past_end<E>(f, v[J], V);
+          if ((v[J] + 1) * EPV > V) {
+            mask_past_end<E>(f, v[J], V);
+            x[J] = E::pack(f);
+          }
 #pragma unroll
-          for (int e = 0; e < EPV; ++e) bits |= in(f[e]) ? 1u << (J * EPV + e) : 0u;
+          for (int e = 0; e < EPV; ++e) mine += f[e] >= least ? 1 : 0;
           slot_fence();
         });
-        const uint32_t mine = __popc(bits), upto = wave_scan(mine, lane);
+        const uint32_t upto = wave_scan(mine, lane);
         uint32_t at = 0;
         if (lane == 63 && upto) at = atomicAdd(&sh.count, upto);
         at = __builtin_amdgcn_readlane(at, 63) + upto - mine;
-        static_for<U>([&](auto J) {
-          if (!__ballot(bits >> (J * EPV) & ((1u << EPV) - 1))) return;
-          float f[EPV];
-          E::unpack(x[J], f);
+        if (mine)
+          static_for<U>([&](auto J) {
+            float f[EPV];
+            E::unpack(x[J], f);
 #pragma unroll
-          for (int e = 0; e < EPV; ++e)
-            if (bits >> (J * EPV + e) & 1) {
-              if (at < LIST) sh.list[at] = token_of(f[e], v[J] * EPV + e);
-              ++at;
-            }
-          slot_fence();
-        });
+            for (int e = 0; e < EPV; ++e)
+              if (f[e] >= least) {
+                if (at < LIST) sh.list[at] = token_of(f[e], v[J] * EPV + e);
+                ++at;
+              }
+            slot_fence();
+          });
       }
       __syncthreads();
       fits = sh.count <= LIST;
