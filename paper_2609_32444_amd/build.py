@@ -24,7 +24,8 @@ HEADERS = [os.path.join(ROOT, "include", "cis.h"), os.path.join(HERE, "csrc", "c
            os.path.join(HERE, "csrc", "cis_plan.h"),
            os.path.join(HERE, "csrc", "cis_seg.h"), os.path.join(HERE, "csrc", "cis_stats.h"),
            os.path.join(ROOT, "include", "cis_tokens.h"), os.path.join(HERE, "csrc", "cis_tok.h"),
-           os.path.join(HERE, "csrc", "cis_tok_row.h"), os.path.join(HERE, "csrc", "cis_distill.h")]
+           os.path.join(HERE, "csrc", "cis_tok_row.h"),
+           os.path.join(HERE, "csrc", "cis_select.h"), os.path.join(HERE, "csrc", "cis_distill.h")]
 
 # -packed-fp32-ops: no v_pk_{add,mul,fma}_f32 in device code (the compiler's host pass warns
 # that it does not know the feature; that warning is expected).

@@ -10,6 +10,8 @@
 
 namespace cis {
 
+// Lowest reference of a row's sum: finite where there is nothing but -inf.
+constexpr float kMinExp = -0x1p126f;
 constexpr float kLn2 = 0.693147180559945309417f;
 // expm1(d) - d >= 0, to a few units in the last place (near 0 by its series, which does not
 // cancel: nine terms, the first left out below 2^-24 of the sum up to |d| = 0.6).

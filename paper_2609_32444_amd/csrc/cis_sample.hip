@@ -1,198 +1,691 @@
-// Sampling kernels (gfx950): one workgroup per row, which it reads as often as its cuts take.
-#include "cis_tok_row.h"
+// Sampling kernels (gfx950).
+//
+// A row is drawn from the scan (TokScan) in one of four ways, by what its cuts keep at most:
+//   * top_k up to kDrawK (and greedy rows): the candidates that RowSelect collects, put in order; the
+//     cuts and the draw run on that list.
+//   * nothing but min_p cuts: the weights' sums by chunks (cis_weigh_kernel), the chunk that the
+//     random number falls into, and the token within it.
+//   * top_p: the same sums give the target; if the collected candidates reach it, the list decides.
+//   * otherwise a histogram of the weights' exponents over the row narrows the cut down to one step of
+//     1/64 octave, whose tokens are sorted; then the sums by chunks of what is kept. Where a
+//     step overflows the list (many equal logits), the cut is found byte by byte (radix_cut).
+#include "cis_select.h"
 
 namespace cis {
 
+constexpr int kDrawK = 1024;
+
+struct RowParams {
+  float u, temp, top_p, min_p;
+  int64_t top_k;   // V: no limit
+  float c;
+  bool ok;
+  bool counted;    // top_k (V: all of a short row) leaves few enough for a list
+  uint32_t least_w;
+};
+__device__ __forceinline__ RowParams row_params(const SampleArgs& a, int64_t row) {
+  RowParams p;
+  p.u = a.u[row];
+  p.temp = a.temperature ? a.temperature[row] : a.prm.temperature;
+  const int k = a.top_k ? a.top_k[row] : a.prm.top_k;
+  p.top_p = a.top_p ? a.top_p[row] : a.prm.top_p;
+  p.min_p = a.min_p ? a.min_p[row] : a.prm.min_p;
+  p.ok = tok_on(a.r, row) && p.u >= 0.f && p.u < 1.f && p.temp >= 0.f && p.temp < INFINITY &&
+         k >= 0 && p.top_p > 0.f && p.top_p <= 1.f && p.min_p >= 0.f && p.min_p <= 1.f;
+  p.c = kLog2e / p.temp;
+  const bool greedy = !(p.c < INFINITY);
+  p.top_k = greedy ? 1 : k == 0 || k >= a.r.V ? a.r.V : k;
+  if (greedy) p.c = kLog2e;
+  p.counted = greedy || (p.top_k <= kDrawK && (p.top_k < a.r.V || p.top_p < 1.f));
+  p.least_w = (uint32_t)ceil((double)p.min_p * kDrawOne);
+  return p;
+}
+// Rows that cis_weigh_kernel sums up: those that no count cuts.
+__device__ __forceinline__ bool row_weighed(const RowParams& p, int V) {
+  return p.ok && !p.counted && p.top_k == V;
+}
+
+// Weights of a vector, at least `least_w` or 0; their sum stays below 2^32.
+template <class E>
+__device__ __forceinline__ uint32_t vec_weight(const float (&f)[E::kPerVec], float M, float c,
+                                               uint32_t least_w) {
+  uint32_t s = 0;
+#pragma unroll
+  for (int e = 0; e < E::kPerVec; ++e) {
+    const uint32_t w = draw_weight(f[e], M, c);
+    s += w >= least_w ? w : 0u;
+  }
+  return s;
+}
+
+__device__ __forceinline__ u64 wave_total(u64 x) {
+#pragma unroll
+  for (int off = 32; off >= 1; off >>= 1) x += __shfl_xor(x, off, 64);
+  return x;
+}
+
 // ------------------------------------------------------------------------------------------
-// One token per row. The cuts give one pair (key, ties); the draw sums the kept weights in pieces
-// of the row in order of the ids, finds the piece that the random number falls into and then the
-// token, all in whole numbers.
+// One wave per chunk: the sum of its weights. A chunk whose largest logit has no weight is not read.
 // ------------------------------------------------------------------------------------------
-struct SampleShared {
-  CutShared cut;
-  float f[16];
-  u64 u[16];
-  double d[16];
-  u64 mass[kChunks];
-  uint32_t ties[kChunks];
+template <class E>
+__global__ __launch_bounds__(kWeighBlock) void cis_weigh_kernel(const SampleArgs a) {
+  constexpr int NW = kWeighBlock / 64, EPV = E::kPerVec;
+  const int lane = threadIdx.x & 63, wid = __builtin_amdgcn_readfirstlane(threadIdx.x) >> 6;
+  const int nch = a.s.nch;
+  const int64_t total = a.r.T * (int64_t)nch;
+  for (int64_t w = (int64_t)blockIdx.x * NW + wid; w < total; w += (int64_t)gridDim.x * NW) {
+    const int64_t row = w / nch;
+    const int ch = (int)(w - row * nch);
+    const RowParams p = row_params(a, row);
+    if (!row_weighed(p, a.r.V)) continue;
+    u32x4 x[kScanSlots];
+    load_chunk<E, 0>(tok_rsrc(a.r, row), a.r, ch, lane, x);
+    const float* cmax = a.s.cmax + row * nch;
+    float M = -INFINITY;
+    for (int i = lane; i < nch; i += 64) M = fmaxf(M, cmax[i]);
+    M = wave_max(M);
+    u64 s = 0;
+    if ((cmax[ch] - M) * p.c >= -28.f) {
+      const uint32_t least = p.top_p < 1.f ? 0u : p.least_w;   // (top_p counts every weight)
+      static_for<kScanSlots>([&](auto I) {
+        float f[EPV];
+        E::unpack(x[I], f);
+        s += vec_weight<E>(f, M, p.c, least);
+        slot_fence();
+      });
+      s = wave_total(s);
+    }
+    if (lane == 0) a.draw[w] = s;
+  }
+}
+
+// ------------------------------------------------------------------------------------------
+// The draw.
+// ------------------------------------------------------------------------------------------
+constexpr int kFine = 64;                  // histogram steps per octave
+constexpr int kFineSteps = 29 * kFine;     // (a weight's exponent is at least -28, or it is 0)
+struct WideShared {
+  u64 mass[kFineSteps];
+  uint32_t count[kFineSteps];
+  uint32_t step;
+  u64 left, before;
 };
 
-template <class E>
-__global__ __launch_bounds__(kTokBlock) void cis_sample_kernel(const SampleArgs a) {
-  constexpr int BLOCK = kTokBlock, NW = BLOCK / 64, EPV = E::kPerVec;
-  __shared__ SampleShared sh;
-  const int tid = threadIdx.x, lane = tid & 63, wid = tid >> 6;
-  const int V = a.r.V, nvec = a.r.nvec;
-  for (int64_t row = blockIdx.x; row < a.r.T; row += gridDim.x) {
-    const float u = a.u[row];
-    const float temp = a.temperature ? a.temperature[row] : a.prm.temperature;
-    const int top_k = a.top_k ? a.top_k[row] : a.prm.top_k;
-    const float top_p = a.top_p ? a.top_p[row] : a.prm.top_p;
-    const float min_p = a.min_p ? a.min_p[row] : a.prm.min_p;
-    bool draw = tok_on(a.r, row) && u >= 0.f && u < 1.f && temp >= 0.f && temp < INFINITY &&
-                top_k >= 0 && top_p > 0.f && top_p <= 1.f && min_p >= 0.f && min_p <= 1.f;
-    const __amdgpu_buffer_rsrc_t rs = tok_rsrc(a.r, row);
-    RowFacts facts{};
-    if (draw) {
-      facts = row_facts<E, BLOCK>(rs, nvec, V, sh.f, sh.u);
-      draw = facts.finite && facts.tokens > 0;
-    }
-    if (!draw) {
-      if (tid == 0) {
-        a.ids[row] = -1;
-        if (a.logp) a.logp[row] = 0.f;
-        if (a.logp_kept) a.logp_kept[row] = 0.f;
-      }
-      continue;
-    }
-    const float M = facts.M;
-    float c = kLog2e / temp;
-    u64 k = top_k > 0 ? (u64)top_k : facts.tokens;
-    if (!(c < INFINITY)) {   // greedy
-      c = kLog2e;
-      k = 1;
-    }
-    Cut cut{kNoToken, 0};    // keeps every token
-    auto weight = [&](float f) { return draw_weight(f, M, c); };
-    if (k < facts.tokens)
-      cut = radix_cut<E, BLOCK>(rs, nvec, V, k, 0u, [](float) { return 1u; }, sh.cut);
-    if (top_p < 1.f && k > 1) {
-      u64 s = 0;
-      for (int v = tid; v < nvec; v += BLOCK) {
-        float f[EPV];
-        tok_vec<E>(rs, v, V, f);
+template <class E, int BLOCK, int LIST, bool WIDE>
+struct RowDraw {
+  static constexpr int NW = BLOCK / 64, EPV = E::kPerVec;
+  const SampleArgs& a;
+  const RowParams& p;
+  RowSelect<E, BLOCK, LIST>& sel;
+  SelectShared<LIST>& sh;
+  int64_t row;
+  float rest;   // sum of exp(z - M) over the row but one of its largest logits
+
+  __device__ __forceinline__ uint32_t weight(float f) const { return draw_weight(f, sel.M, p.c); }
+
+  __device__ __forceinline__ void put_row(int id, float f, u64 w, u64 N) const {
+    a.ids[row] = id;
+    if (a.logp) a.logp[row] = (f - sel.M) - log1pf(rest);
+    if (a.logp_kept) a.logp_kept[row] = (float)log((double)w / (double)N);
+  }
+
+  // Sum over the row but one largest logit, relative to it: the chunks' sums, except for the
+  // first chunk that holds it, which is summed again without it.
+  __device__ __forceinline__ void sum_rest() {
+    const int tid = threadIdx.x, lane = tid & 63;
+    int first = sel.nch;
+    double s = 0.0;
+    for (int i = tid; i < sel.nch; i += BLOCK)
+      if (sel.cmax[i] == sel.M) first = first < i ? first : i;
 #pragma unroll
-        for (int e = 0; e < EPV; ++e)
-          if (order_key(f[e]) > cut.key) s += weight(f[e]);
-      }
-      s = block_sum<NW>(s, sh.u);
-      if (cut.ties > 0) s += cut.ties * weight(key_value(cut.key));
-      const double want = ceil((double)top_p * (double)s);
-      const Cut p = radix_cut<E, BLOCK>(rs, nvec, V, (u64)want, cut.key, weight, sh.cut);
-      // the sum that the key's tokens have to bring, as a count of them
-      const u64 w = weight(key_value(p.key));
-      if (w > 0) cut = Cut{p.key, (p.ties + w - 1) / w};
+    for (int off = 32; off >= 1; off >>= 1) {
+      const int o = __shfl_xor(first, off, 64);
+      first = first < o ? first : o;
     }
-    const uint32_t least_w = (uint32_t)ceil((double)min_p * kDrawOne);
-    // the kept weights by pieces
-    const int cv = chunk_vecs(nvec);
-    for (int ch = wid; ch < kChunks; ch += NW) {
-      u64 s = 0;
-      uint32_t t = 0;
-      for (int v = ch * cv + lane; v < min((ch + 1) * cv, nvec); v += 64) {
-        float f[EPV];
-        tok_vec<E>(rs, v, V, f);
+    if (lane == 0) sh.u[tid >> 6] = (u64)first;
+    __syncthreads();
+    for (int w = 0; w < NW; ++w) first = first < (int)sh.u[w] ? first : (int)sh.u[w];
+    for (int i = tid; i < sel.nch; i += BLOCK)
+      if (i != first)
+        s += sel.csum[i] * (double)fast_exp2((sel.cmax[i] - sel.M) * kLog2e);
+    if (tid < 64) {
+      u32x4 x[kScanSlots];
+      load_chunk<E, 0>(sel.rs, a.r, first, lane, x);
+      uint32_t n = 0;
+      static_for<kScanSlots>([&](auto I) {
+        float f[EPV], t = 0.f;
+        E::unpack(x[I], f);
 #pragma unroll
         for (int e = 0; e < EPV; ++e) {
-          const uint32_t key = order_key(f[e]);
-          if (key > cut.key) {
-            const uint32_t w = weight(f[e]);
-            s += w >= least_w ? w : 0;
-          }
-          t += key == cut.key ? 1 : 0;
+          t += f[e] == sel.M ? 0.f : fast_exp2((f[e] - sel.M) * kLog2e);
+          n += f[e] == sel.M ? 1 : 0;
         }
+        s += (double)t;
+        slot_fence();
+      });
+      n = wave_sum(n);
+      if (tid == 0) s += (double)(n - 1);
+    }
+    rest = (float)block_sum<NW>(s, sh.d);
+  }
+
+  // Draws from the list's first logits in order: at most `n` of them; of those the fewest that
+  // reach `want` (0: all), at least least_w each.
+  __device__ __forceinline__ void from_list(int n, u64 want) {
+    const int tid = threadIdx.x, lane = tid & 63, wid = tid >> 6;
+    constexpr int PT = LIST / BLOCK;
+    u64 t[PT];
+    uint32_t q[PT];
+    u64 s = 0;
+    static_for<PT>([&](auto J) {
+      const int i = tid * PT + J;
+      q[J] = 0;
+      if (i < n) {
+        t[J] = sh.list[i];
+        q[J] = weight(token_value(t[J]));
       }
-      s = wave_sum(s);
-      t = wave_sum(t);
-      if (lane == 0) {
-        sh.mass[ch] = s;
-        sh.ties[ch] = t;
+      s += q[J];
+    });
+    u64 before = wave_scan(s, lane);
+    if (lane == 63) sh.u[wid] = before;
+    __syncthreads();
+    before -= s;
+    u64 total = 0;
+    for (int w = 0; w < NW; ++w) {
+      if (w < wid) before += sh.u[w];
+      total += sh.u[w];
+    }
+    if (p.top_p < 1.f && want == 0) want = (u64)ceil((double)p.top_p * (double)total);
+    // the cuts: each keeps a first part
+    u64 keep = 0;   // by top_p, and above by min_p
+    u64 b = before;
+    static_for<PT>([&](auto J) {
+      if (tid * PT + J < n) {
+        keep += want == 0 || b < want ? 1 : 0;
+        keep += q[J] >= p.least_w ? u64(1) << 32 : 0;
+      }
+      b += q[J];
+    });
+    __syncthreads();
+    keep = block_sum<NW>(keep, sh.u);
+    const int np = (int)(uint32_t)keep, nm = (int)(keep >> 32);
+    n = n < np ? n : np;
+    n = n < nm ? n : nm;
+    s = 0;
+    static_for<PT>([&](auto J) {
+      if (tid * PT + J >= n) q[J] = 0;
+      s += q[J];
+    });
+    __syncthreads();
+    const u64 N = block_sum<NW>(s, sh.u);
+    u64 at = (u64)((double)p.u * (double)N);
+    if (at >= N) at = N - 1;
+    // in order of the ids: (id, weight) pairs
+    static_for<PT>([&](auto J) {
+      const int i = tid * PT + J;
+      if (i < n) sh.list[i] = ((u64)(uint32_t)token_id(t[J]) << 32) | q[J];
+    });
+    __syncthreads();
+    if (n > 256) {
+      // narrowed to the tokens that share the first bits of the drawn one's id
+      int shift = 0;
+      while ((sel.V - 1) >> shift >= kSteps) ++shift;
+      for (int i = tid; i < kSteps; i += BLOCK) sh.mass[i] = 0;
+      if (tid == 0) sh.count = 0;
+      __syncthreads();
+      static_for<PT>([&](auto J) {
+        if (tid * PT + J < n) atomicAdd(&sh.mass[token_id(t[J]) >> shift], (u64)q[J]);
+      });
+      __syncthreads();
+      constexpr int S = kSteps / BLOCK;
+      u64 m[S], ms = 0;
+      static_for<S>([&](auto J) { ms += m[J] = sh.mass[tid * S + J]; });
+      u64 mb = wave_scan(ms, lane);
+      if (lane == 63) sh.u[wid] = mb;
+      __syncthreads();
+      mb -= ms;
+      for (int w = 0; w < wid; ++w) mb += sh.u[w];
+      static_for<S>([&](auto J) {
+        if (mb <= at && at < mb + m[J]) {
+          sh.bin = tid * S + J;
+          sh.mass[0] = mb;   // (every thread has read its own)
+        }
+        mb += m[J];
+      });
+      __syncthreads();
+      const uint32_t bin = sh.bin;
+      at -= sh.mass[0];
+      static_for<PT>([&](auto J) {
+        if (tid * PT + J < n && (uint32_t)(token_id(t[J]) >> shift) == bin)
+          sh.list[atomicAdd(&sh.count, 1u)] = ((u64)(uint32_t)token_id(t[J]) << 32) | q[J];
+      });
+      __syncthreads();
+      n = (int)sh.count;
+    }
+    for (int i = tid; i < n; i += BLOCK) {
+      const u64 me = sh.list[i];
+      u64 upto = 0;
+      for (int j = 0; j < n; ++j) {
+        const u64 x = sh.list[j];
+        upto += x <= me ? (uint32_t)x : 0;   // ids differ: lower ids first
+      }
+      const uint32_t w = (uint32_t)me;
+      if (upto > at && upto - w <= at) {
+        // its logit: from the row (the list holds it no more)
+        const int id = (int)(me >> 32);
+        float f[EPV], fy = 0.f;
+        tok_vec<E>(sel.rs, id / EPV, sel.V, f);
+#pragma unroll
+        for (int e = 0; e < EPV; ++e) fy = id % EPV == e ? f[e] : fy;
+        put_row(id, fy, w, N);
       }
     }
-    // the row's own log-sum-exp, relative to the largest logit and without its term (one of them,
-    // where there are several): the sums keep what is left of a confident row to full accuracy
-    double rest = 0.0;
-    u64 largest = 0;
-    for (int v = tid; v < nvec; v += BLOCK) {
-      float f[EPV], s = 0.f;
-      tok_vec<E>(rs, v, V, f);
+  }
+
+  // Draws by the chunks' sums at a.draw, with `ties` (null: none) tokens of the cut's key per
+  // chunk of which the row's first cut.ties count.
+  __device__ __forceinline__ void from_chunks(const Cut& cut, const uint32_t* ties, uint32_t least) {
+    const int tid = threadIdx.x, lane = tid & 63;
+    if (tid >= 64) return;
+    const u64* mass = a.draw + row * sel.nch;
+    uint32_t wt = ties && cut.ties > 0 ? weight(key_value(cut.key)) : 0;
+    if (wt < least) wt = 0;
+    // (chunk i0 + lane's kept mass, and the ties up to it)
+    auto chunk_mass = [&](int i0, u64& tb, u64& nt) {
+      const int i = i0 + lane;
+      nt = ties && i < sel.nch ? ties[i] : 0;
+      const u64 upto = tb + (ties ? wave_scan(nt, lane) : 0), b = upto - nt;
+      const u64 left = cut.ties > b ? cut.ties - b : 0;
+      if (ties) tb = __shfl(upto, 63, 64);
+      return (i < sel.nch ? mass[i] : 0) + (nt < left ? nt : left) * wt;
+    };
+    u64 N = 0, tb = 0, nt;
+    for (int i0 = 0; i0 < sel.nch; i0 += 64) N += wave_total(chunk_mass(i0, tb, nt));
+    u64 at = (u64)((double)p.u * (double)N);
+    if (at >= N) at = N - 1;
+    u64 before = 0;
+    tb = 0;
+    int ch = 0;
+    for (int i0 = 0; i0 < sel.nch; i0 += 64) {
+      const u64 tb0 = tb, m = chunk_mass(i0, tb, nt), upto = before + wave_scan(m, lane);
+      const u64 hit = __ballot(upto > at);
+      if (hit) {
+        const int who = __ffsll(hit) - 1;
+        ch = i0 + who;
+        before = __shfl(upto - m, who, 64);
+        tb = ties ? tb0 + __shfl(wave_scan(nt, lane) - nt, who, 64) : 0;
+        break;
+      }
+      before = __shfl(upto, 63, 64);
+    }
+    u32x4 x[kScanSlots];
+    load_chunk<E, 0>(sel.rs, a.r, ch, lane, x);
+    bool done = false;
+    static_for<kScanSlots>([&](auto I) {
+      if (done) return;
+      float f[EPV];
+      E::unpack(x[I], f);
+      const int v = ch * kScanVecs + I * 64 + lane;
+      uint32_t n = 0;
+      if (ties) {
+#pragma unroll
+        for (int e = 0; e < EPV; ++e) n += order_key(f[e]) == cut.key ? 1 : 0;
+      }
+      const u64 tupto = ties ? tb + wave_scan(n, lane) : 0;
+      u64 t = tupto - n;
+      uint32_t w[EPV];
+      u64 sum = 0;
 #pragma unroll
       for (int e = 0; e < EPV; ++e) {
-        s += f[e] == M ? 0.f : fast_exp2((f[e] - M) * kLog2e);
-        largest += f[e] == M ? 1 : 0;
+        const uint32_t key = order_key(f[e]), q = weight(f[e]);
+        w[e] = key > cut.key && q >= least ? q : 0;
+        if (ties && key == cut.key) w[e] = t++ < cut.ties ? wt : 0;
+        sum += w[e];
       }
-      rest += s;
-    }
-    rest = block_sum<NW>(rest, sh.d) + (double)(block_sum<NW>(largest, sh.u) - 1);
-    if (wid == 0) {
-      uint32_t wt = cut.ties > 0 ? weight(key_value(cut.key)) : 0;
-      if (wt < least_w) wt = 0;
-      // piece 4 l + i of lane l
-      u64 ties[4], mass[4], nt = 0;
+      const u64 upto = before + wave_scan(sum, lane);
+      const u64 hit = __ballot(upto > at);
+      if (hit) {
+        if (lane == __ffsll(hit) - 1) {
+          u64 b = upto - sum;
+          bool found = false;
 #pragma unroll
-      for (int i = 0; i < 4; ++i) nt += ties[i] = sh.ties[4 * lane + i];
-      u64 tb = wave_scan(nt, lane) - nt, s = 0;
-#pragma unroll
-      for (int i = 0; i < 4; ++i) {
-        const u64 left = cut.ties > tb ? cut.ties - tb : 0;
-        mass[i] = sh.mass[4 * lane + i] + (ties[i] < left ? ties[i] : left) * wt;
-        tb += ties[i];
-        s += mass[i];
-      }
-      const u64 upto = wave_scan(s, lane), N = __shfl(upto, 63, 64);
-      u64 at = (u64)((double)u * (double)N);
-      if (at >= N) at = N - 1;
-      const int who = __ffsll(__ballot(upto > at)) - 1;
-      // the piece, what is before it, and the ties before it
-      u64 before = upto - s, tbefore = wave_scan(nt, lane) - nt;
-      int ch = 4 * lane;
-      for (int i = 0; i < 3 && before + mass[i] <= at; ++i) {
-        before += mass[i];
-        tbefore += ties[i];
-        ++ch;
-      }
-      ch = __shfl(ch, who, 64);
-      before = __shfl(before, who, 64);
-      tbefore = __shfl(tbefore, who, 64);
-      for (int v0 = ch * cv; v0 < nvec; v0 += 64) {
-        const int v = v0 + lane;
-        float f[EPV];
-        if (v < nvec) {
-          tok_vec<E>(rs, v, V, f);
-        } else {
-          for (int e = 0; e < EPV; ++e) f[e] = -INFINITY;
-        }
-        uint32_t nt = 0;
-        for (int e = 0; e < EPV; ++e) nt += order_key(f[e]) == cut.key ? 1 : 0;
-        const u64 tupto = tbefore + wave_scan(nt, lane);
-        u64 w[EPV], sum = 0, t = tupto - nt;
-        for (int e = 0; e < EPV; ++e) {
-          const uint32_t key = order_key(f[e]), q = weight(f[e]);
-          w[e] = key > cut.key && q >= least_w ? q : 0;
-          if (key == cut.key) w[e] = t++ < cut.ties ? wt : 0;
-          sum += w[e];
-        }
-        const u64 supto = before + wave_scan(sum, lane);
-        const u64 hit = __ballot(supto > at);
-        if (hit) {
-          if (lane == __ffsll(hit) - 1) {
-            u64 b = supto - sum;
-            int e = 0;
-            while (b + w[e] <= at) b += w[e++];
-            float fy = f[0];
-            u64 wy = w[0];
-#pragma unroll
-            for (int i = 1; i < EPV; ++i) {
-              fy = i == e ? f[i] : fy;
-              wy = i == e ? w[i] : wy;
+          for (int e = 0; e < EPV; ++e) {
+            if (!found && b + w[e] > at) {
+              found = true;
+              put_row(v * EPV + e, f[e], w[e], N);
             }
-            a.ids[row] = (int64_t)v * EPV + e;
-            if (a.logp) a.logp[row] = (fy - M) - log1pf((float)rest);
-            if (a.logp_kept) a.logp_kept[row] = (float)log((double)wy / (double)N);
+            b += w[e];
           }
-          break;
         }
-        before = __shfl(supto, 63, 64);
-        tbefore = __shfl(tupto, 63, 64);
+        done = true;
+      }
+      before = __shfl(upto, 63, 64);
+      tb = ties ? __shfl(tupto, 63, 64) : 0;
+      slot_fence();
+    });
+  }
+
+  // The step of the histogram of weights that a logit falls into; kFineSteps: it has no weight.
+  __device__ __forceinline__ int fine_step(float f) const {
+    const float t = (sel.M - f) * p.c * (float)kFine;
+    return t < (float)kFineSteps ? (int)t : kFineSteps;
+  }
+
+  // f(logits, vector) for the row's chunks that hold a weight, whole waves together.
+  template <class F>
+  __device__ __forceinline__ void each_chunk(F&& f) const {
+    const int lane = threadIdx.x & 63, wid = __builtin_amdgcn_readfirstlane(threadIdx.x) >> 6;
+    for (int ch = wid; ch < sel.nch; ch += NW) {
+      const bool any = (sel.cmax[ch] - sel.M) * p.c >= -28.f;
+      u32x4 x[kScanSlots];
+      if (any) load_chunk<E, 0>(sel.rs, a.r, ch, lane, x);
+      f(ch, any, x);
+    }
+  }
+
+  // The first step at which the sum of `part(step)` reaches `want`: the step, what it has to
+  // bring, and the sum before it.
+  template <class G>
+  __device__ __forceinline__ void find_step(WideShared& ws, u64 want, G&& part) const {
+    const int tid = threadIdx.x, lane = tid & 63;
+    __syncthreads();
+    if (tid < 64) {
+      constexpr int S = kFineSteps / 64;
+      u64 s = 0;
+      for (int i = 0; i < S; ++i) s += part(lane * S + i);
+      const u64 upto = wave_scan(s, lane);
+      u64 before = upto - s;
+      if (before < want && want <= upto) {
+        int i = 0;
+        while (before + part(lane * S + i) < want) before += part(lane * S + i++);
+        ws.step = lane * S + i;
+        ws.left = want - before;
+        ws.before = before;
       }
     }
     __syncthreads();
   }
+
+  // The tokens of a step, in order; false where the list does not hold them.
+  __device__ __forceinline__ bool collect_step(int step) {
+    const int lane = threadIdx.x & 63;
+    __syncthreads();
+    if (threadIdx.x == 0) sh.count = 0;
+    __syncthreads();
+    each_chunk([&](int ch, bool any, u32x4 (&x)[kScanSlots]) {
+      if (!any) return;
+      static_for<kScanSlots>([&](auto I) {
+        float f[EPV];
+        E::unpack(x[I], f);
+#pragma unroll
+        for (int e = 0; e < EPV; ++e) {
+          const bool take = fine_step(f[e]) == step;
+          const uint32_t at = take_place(take, &sh.count, lane);
+          if (take && at < LIST)
+            sh.list[at] = token_of(f[e], (ch * kScanVecs + I * 64 + lane) * EPV + e);
+        }
+        slot_fence();
+      });
+    });
+    __syncthreads();
+    sel.count = (int)sh.count;
+    if (sel.count > LIST) return false;
+    sort_list<BLOCK>(sh.list, sel.count);
+    return true;
+  }
+
+  // The cut from a histogram over the row.
+  __device__ __forceinline__ Cut wide_cut(WideShared& ws) {
+    const int tid = threadIdx.x;
+    const bool by_count = p.top_k < sel.V;
+    for (int i = tid; i < kFineSteps; i += BLOCK) {
+      ws.mass[i] = 0;
+      ws.count[i] = 0;
+    }
+    __syncthreads();
+    each_chunk([&](int, bool any, u32x4 (&x)[kScanSlots]) {
+      if (!any) return;
+      static_for<kScanSlots>([&](auto I) {
+        float f[EPV];
+        E::unpack(x[I], f);
+#pragma unroll
+        for (int e = 0; e < EPV; ++e) {
+          const int st = fine_step(f[e]);
+          if (st < kFineSteps) {
+            atomicAdd(&ws.mass[st], (u64)weight(f[e]));
+            if (by_count) atomicAdd(&ws.count[st], 1u);
+          }
+        }
+        slot_fence();
+      });
+    });
+    __syncthreads();
+    // the list's first n logits as a cut
+    auto cut_at = [&](int n) {
+      const uint32_t key = (uint32_t)(sh.list[n - 1] >> 32);
+      u64 ties = 0;
+      for (int i = tid; i < n; i += BLOCK) ties += (uint32_t)(sh.list[i] >> 32) == key ? 1 : 0;
+      __syncthreads();
+      return Cut{key, block_sum<NW>(ties, sh.u)};
+    };
+    // how many of the list's logits it takes to reach `want`
+    auto reach = [&](u64 want) {
+      constexpr int PT = LIST / BLOCK;
+      const int lane = tid & 63, wid = tid >> 6;
+      u64 s = 0, n = 0;
+      for (int j = 0; j < PT && tid * PT + j < sel.count; ++j)
+        s += weight(token_value(sh.list[tid * PT + j]));
+      u64 b = wave_scan(s, lane);
+      __syncthreads();
+      if (lane == 63) sh.u[wid] = b;
+      __syncthreads();
+      b -= s;
+      for (int w = 0; w < wid; ++w) b += sh.u[w];
+      for (int j = 0; j < PT && tid * PT + j < sel.count; ++j) {
+        n += b < want ? 1 : 0;
+        b += weight(token_value(sh.list[tid * PT + j]));
+      }
+      __syncthreads();
+      n = block_sum<NW>(n, sh.u);
+      return (int)n;
+    };
+    auto radix = [&](u64 want, uint32_t least, auto&& weigh) {
+      return radix_cut<E, BLOCK>(sel.rs, sel.nvec, sel.V, want, least, weigh, sh.cut);
+    };
+    auto mass = [&](int i) { return ws.mass[i]; };
+    auto count = [&](int i) { return (u64)ws.count[i]; };
+    Cut cut{kNoToken, 0};
+    u64 sum = 0;       // the mass that the count leaves
+    int kstep = -1;    // the step that the list holds
+    u64 n = 0;
+    for (int i = tid; i < kFineSteps; i += BLOCK) {
+      sum += ws.mass[i];
+      n += ws.count[i];
+    }
+    sum = block_sum<NW>(sum, sh.u);
+    __syncthreads();
+    n = block_sum<NW>(n, sh.u);
+    if (by_count && (u64)p.top_k < n) {   // (else every token with a weight is kept)
+      find_step(ws, (u64)p.top_k, count);
+      const int step = ws.step;
+      const int left = (int)ws.left;
+      if (collect_step(step)) {
+        kstep = step;
+        cut = cut_at(left);
+      } else {
+        cut = radix((u64)p.top_k, 0u, [](float) { return 1u; });
+      }
+      u64 s = 0;
+      if (kstep >= 0) {
+        for (int i = tid; i < step; i += BLOCK) s += ws.mass[i];
+        for (int i = tid; i < left; i += BLOCK) s += weight(token_value(sh.list[i]));
+      } else {   // (the step's tokens above the key are not known: the row again)
+        for (int v = tid; v < sel.nvec; v += BLOCK) {
+          float f[EPV];
+          tok_vec<E>(sel.rs, v, sel.V, f);
+          for (int e = 0; e < EPV; ++e)
+            if (order_key(f[e]) > cut.key) s += weight(f[e]);
+        }
+        if (tid == 0) s += cut.ties * weight(key_value(cut.key));
+      }
+      __syncthreads();
+      sum = block_sum<NW>(s, sh.u);
+    }
+    if (p.top_p < 1.f) {
+      const u64 want = (u64)ceil((double)p.top_p * (double)sum);
+      find_step(ws, want, mass);
+      const int step = ws.step;
+      const u64 left = ws.left;
+      if (step == kstep || collect_step(step)) {
+        cut = cut_at(reach(left));
+      } else {
+        const Cut c = radix(want, cut.key, [&](float f) { return weight(f); });
+        const u64 w = weight(key_value(c.key));
+        if (w > 0) cut = Cut{c.key, (c.ties + w - 1) / w};
+      }
+    }
+    return cut;
+  }
+
+  // The kept weights' sums and ties by chunks, and the draw from them.
+  __device__ __forceinline__ void from_cut(const Cut& cut) {
+    const int lane = threadIdx.x & 63;
+    u64* mass = a.draw + row * sel.nch;
+    uint32_t* ties = a.ties + row * sel.nch;
+    const float least_f = key_value(cut.key);
+    each_chunk([&](int ch, bool any, u32x4 (&x)[kScanSlots]) {
+      u64 s = 0;
+      uint32_t t = 0;
+      if (any && sel.cmax[ch] + 0.f >= least_f) {
+        static_for<kScanSlots>([&](auto I) {
+          float f[EPV];
+          E::unpack(x[I], f);
+#pragma unroll
+          for (int e = 0; e < EPV; ++e) {
+            const uint32_t key = order_key(f[e]);
+            if (key > cut.key) {
+              const uint32_t w = weight(f[e]);
+              s += w >= p.least_w ? w : 0;
+            }
+            t += key == cut.key ? 1 : 0;
+          }
+          slot_fence();
+        });
+        s = wave_total(s);
+        t = wave_sum(t);
+      }
+      if (lane == 0) {
+        mass[ch] = s;
+        ties[ch] = t;
+      }
+    });
+    __syncthreads();
+    from_chunks(cut, ties, p.least_w);
+  }
+
+  __device__ __forceinline__ void run(WideShared* ws) {
+    const int tid = threadIdx.x;
+    sum_rest();
+    const int64_t V = sel.V;
+    const int k = (int)p.top_k;
+    if (p.counted) {
+      if (sel.collect(k)) {
+        sel.order(k);
+        from_list(sel.count < k ? sel.count : k, 0);
+        return;
+      }
+    } else if (p.top_k == V) {
+      if (p.top_p == 1.f) {
+        __syncthreads();
+        from_chunks(Cut{kNoToken, 0}, nullptr, p.least_w);
+        return;
+      }
+      if constexpr (WIDE) {
+        u64 sum = 0;
+        for (int i = tid; i < sel.nch; i += BLOCK) sum += a.draw[row * sel.nch + i];
+        __syncthreads();
+        sum = block_sum<NW>(sum, sh.u);
+        const u64 want = (u64)ceil((double)p.top_p * (double)sum);
+        for (int n = 64; n <= kDrawK; n *= 16) {
+          __syncthreads();
+          if (!sel.collect(n)) break;
+          u64 s = 0;
+          for (int i = tid; i < sel.count; i += BLOCK) s += weight(token_value(sh.list[i]));
+          s = block_sum<NW>(s, sh.u);
+          __syncthreads();
+          if (s >= want) {
+            sel.order(LIST);
+            from_list(sel.count, want);
+            return;
+          }
+          if (sel.bin == 256) break;
+        }
+      }
+    }
+    if constexpr (WIDE) {
+      __syncthreads();
+      from_cut(wide_cut(*ws));
+    } else {
+      // a row of many equal logits
+      __syncthreads();
+      Cut cut = radix_cut<E, BLOCK>(sel.rs, sel.nvec, sel.V, (u64)k, 0u,
+                                    [](float) { return 1u; }, sh.cut);
+      if (p.top_p < 1.f) {
+        u64 s = 0;
+        for (int v = tid; v < sel.nvec; v += BLOCK) {
+          float f[EPV];
+          tok_vec<E>(sel.rs, v, sel.V, f);
+          for (int e = 0; e < EPV; ++e)
+            if (order_key(f[e]) > cut.key) s += weight(f[e]);
+        }
+        if (tid == 0) s += cut.ties * weight(key_value(cut.key));
+        s = block_sum<NW>(s, sh.u);
+        __syncthreads();
+        const Cut c = radix_cut<E, BLOCK>(
+            sel.rs, sel.nvec, sel.V, (u64)ceil((double)p.top_p * (double)s), cut.key,
+            [&](float f) { return weight(f); }, sh.cut);
+        const u64 w = weight(key_value(c.key));
+        if (w > 0) cut = Cut{c.key, (c.ties + w - 1) / w};
+      }
+      from_cut(cut);
+    }
+  }
+};
+
+// WIDE: any parameters; else top_k in [1, LIST / 8] for every row, or nothing to cut but min_p.
+template <class E, int BLOCK, int LIST, bool WIDE>
+__global__ __launch_bounds__(BLOCK) __attribute__((amdgpu_waves_per_eu(4))) void cis_sample_kernel(
+    const SampleArgs a) {
+  __shared__ SelectShared<LIST> sh;
+  __shared__ std::conditional_t<WIDE, WideShared, uint32_t> ws;
+  const int64_t row = a.row0 + blockIdx.x;
+  const RowParams p = row_params(a, row);
+  RowSelect<E, BLOCK, LIST> sel(sh, a.r, a.s, row, p.ok);
+  if (!p.ok || !sel.tokens()) {
+    if (threadIdx.x == 0) {
+      a.ids[row] = -1;
+      if (a.logp) a.logp[row] = 0.f;
+      if (a.logp_kept) a.logp_kept[row] = 0.f;
+    }
+    return;
+  }
+  RowDraw<E, BLOCK, LIST, WIDE> draw{a, p, sel, sh, row, 0.f};
+  if constexpr (WIDE)
+    draw.run(&ws);
+  else
+    draw.run(nullptr);
 }
 
-const void* sample_kernel(int dtype) {
-  return dtype == CIS_BF16 ? (const void*)&cis_sample_kernel<Bf16>
-                           : (const void*)&cis_sample_kernel<F32>;
+const void* weigh_kernel(int dtype) {
+  return dtype == CIS_BF16 ? (const void*)&cis_weigh_kernel<Bf16>
+                           : (const void*)&cis_weigh_kernel<F32>;
+}
+const void* sample_kernel(int dtype, bool wide) {
+  if (dtype == CIS_BF16)
+    return wide ? (const void*)&cis_sample_kernel<Bf16, kTokBlock, 8192, true>
+                : (const void*)&cis_sample_kernel<Bf16, kTopBlock, 1024, false>;
+  return wide ? (const void*)&cis_sample_kernel<F32, kTokBlock, 8192, true>
+              : (const void*)&cis_sample_kernel<F32, kTopBlock, 1024, false>;
 }
 
 }  // namespace cis

@@ -21,9 +21,8 @@ struct TokRows {
 constexpr uint32_t kDrawOne = 1u << 28;
 
 // What a scan of the rows leaves in the workspace: the row in chunks of kScanVecs vectors (one wave's),
-// each with its largest logit m and the sum of exp2(z c - R) over its tokens, R = m c rounded (at
-// least kMinExp), added up in double from the float32 sums of its vectors; and the largest logit
-// of every group of `gv` vectors, in the logits' format. A chunk with a NaN or a +inf has a NaN sum;
+// each with its largest logit m and the sum of exp2((z - m) c) over its tokens, added up in double
+// from the float32 sums of its vectors; and the largest logit of every group of `gv` vectors, in the logits' format. A chunk with a NaN or a +inf has a NaN sum;
 // one without tokens the largest logit -inf.
 constexpr int kScanVecs = 512;
 constexpr int kScanBlock = 256;
@@ -66,6 +65,10 @@ struct ScanArgs {
 
 struct SampleArgs {
   TokRows r;
+  TokScan s;                  // of the rows at temperature 1
+  unsigned long long* draw;                // [T, nch] the chunks' weights
+  uint32_t* ties;             // [T, nch] their tokens of a cut's key
+  int64_t row0;               // the launch's first row
   const float* u;
   cis_sample_params_t prm;
   const float* temperature;   // nullable, as the next three
@@ -109,8 +112,12 @@ struct DistillArgs {
 
 constexpr int kTokBlock = 1024;
 constexpr int kTopBlock = 256;
+constexpr int kWeighBlock = 256;
+constexpr int kDrawListK = 128;   // top_k that the kernel for short lists takes
 const void* scan_kernel(int dtype, int32_t gv);
-const void* sample_kernel(int dtype);
+// wide: any parameters; else top_k in [1, 128] for every row or nothing to cut but min_p
+const void* sample_kernel(int dtype, bool wide);
+const void* weigh_kernel(int dtype);
 const void* top_kernel(int dtype, int64_t K);
 int top_block(int64_t K);
 const void* distill_kernel(int dtype, bool bwd);

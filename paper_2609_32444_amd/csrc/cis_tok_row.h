@@ -43,22 +43,20 @@ __device__ __forceinline__ void tok_vec(__amdgpu_buffer_rsrc_t rs, int v, int V,
   if ((v + 1) * E::kPerVec > V) mask_past_end<E>(f, v, V);
 }
 
-// Lowest reference of a sum of exponentials (in units of log2): finite where a row or a chunk
-// holds nothing but -inf.
-constexpr float kMinExp = -0x1p126f;
-
-// Sum of exp2(f c - R) over a vector. Its order is fixed and nothing in it can be contracted: a vector
-// gives the same bits wherever it is summed, so that a sum taken out of a larger one (in double)
-// leaves exactly the others.
+// Sum of exp2((f - m) c) over a vector. Its order is fixed and nothing in it can be contracted: a
+// vector gives the same bits wherever it is summed, so that a sum taken out of a larger one (in
+// double) leaves exactly the others.
 template <class E>
-__device__ __forceinline__ float vec_sum(const float (&f)[E::kPerVec], float c, float R) {
+__device__ __forceinline__ float vec_sum(const float (&f)[E::kPerVec], float c, float m) {
   float x[E::kPerVec];
 #pragma unroll
-  for (int e = 0; e < E::kPerVec; ++e) x[e] = fast_exp2(__builtin_fmaf(f[e], c, -R));
+  for (int e = 0; e < E::kPerVec; ++e) x[e] = fast_exp2((f[e] - m) * c);
   float s = (x[0] + x[1]) + (x[2] + x[3]);
   if constexpr (E::kPerVec == 8) s += (x[4] + x[5]) + (x[6] + x[7]);
   return s;
 }
+// The reference of a sum whose largest logit is m: finite where there is nothing but -inf.
+__device__ __forceinline__ float sum_ref(float m) { return fmaxf(m, -FLT_MAX); }
 
 template <class T>
 __device__ __forceinline__ T wave_sum(T x) {

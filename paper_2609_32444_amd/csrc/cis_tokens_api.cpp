@@ -69,6 +69,23 @@ cis::ScanLayout top_layout(int64_t T, int64_t V, int64_t K, int dtype) {
   const int32_t nvec = row_vecs(V, dtype);
   return cis::scan_layout(T, nvec, elem_bytes(dtype), cis::scan_group(nvec, K));
 }
+// Workgroups of 256 threads per launch of kernels that loop beyond (HIP refuses 2^32 work items).
+constexpr int64_t kMaxBlocks = int64_t(1) << 23;
+// Logits that a draw may have to look at where its parameters do not say.
+constexpr int64_t kManyLogits = 256;
+
+struct SampleLayout {
+  cis::ScanLayout scan;
+  size_t draw, ties, total;
+};
+SampleLayout sample_layout(int64_t T, int32_t nvec, int es, int32_t gv) {
+  SampleLayout L{};
+  L.scan = cis::scan_layout(T, nvec, es, gv);
+  L.draw = L.scan.total;
+  L.ties = L.draw + cis::align_up((size_t)T * L.scan.nch * 8, 256);
+  L.total = L.ties + cis::align_up((size_t)T * L.scan.nch * 4, 256);
+  return L;
+}
 cis::TokScan scan_at(char* base, const cis::ScanLayout& L) {
   return cis::TokScan{base + L.gmax, reinterpret_cast<float*>(base + L.cmax),
                       reinterpret_cast<double*>(base + L.csum), L.nch, L.ngrp, L.gv};
@@ -77,8 +94,8 @@ int launch_scan(const cis::TokRows& r, const cis::TokScan& s, int dtype, float c
                 hipStream_t stream) {
   cis::ScanArgs a{r, s, c};
   const int64_t per = cis::kScanBlock / 64, need = (r.T * s.nch + per - 1) / per;
-  const int64_t cap = int64_t(1) << 23;   // (the kernel loops beyond: HIP refuses 2^32 work items)
-  return launch(cis::scan_kernel(dtype, s.gv), need < cap ? need : cap, cis::kScanBlock, &a, stream);
+  return launch(cis::scan_kernel(dtype, s.gv), need < kMaxBlocks ? need : kMaxBlocks,
+                cis::kScanBlock, &a, stream);
 }
 
 // Rows per launch of kernels of one workgroup per row (HIP refuses 2^32 work items).
@@ -186,7 +203,13 @@ int run_distill(const DistillCall& c, hipStream_t stream) {
 extern "C" {
 
 size_t cis_sample_workspace_bytes(int64_t T, int64_t V, int dtype) {
-  return T < 0 || V < 1 || V > kMaxV || !known(dtype) ? 0 : 256;
+  if (T < 0 || V < 1 || V > kMaxV || !known(dtype)) return 0;
+  // (the shape of the scan goes by the call's parameters: the larger of its two)
+  const int32_t nvec = row_vecs(V, dtype);
+  const SampleLayout a = sample_layout(T, nvec, elem_bytes(dtype), 1),
+                     b = sample_layout(T, nvec, elem_bytes(dtype), 8);
+  const size_t n = a.total > b.total ? a.total : b.total;
+  return n < 256 ? 256 : n;
 }
 
 size_t cis_top_logits_workspace_bytes(int64_t T, int64_t V, int64_t K, int dtype) {
@@ -219,9 +242,35 @@ int cis_sample(const void* logits, int dtype, int64_t T, int64_t V, int64_t ld, 
   if (T > 0 && !aligned_rows(logits, dtype, ld)) return CIS_ERR_ALIGN;
   if (const int cus = device_cus(); cus < 0) return cus;
   if (T == 0) return CIS_OK;
-  cis::SampleArgs a{tok_rows(logits, dtype, T, V, ld, mask), u, p, temperature, top_k, top_p, min_p,
-                    ids_out, logp_out, logp_kept_out};
-  return launch(cis::sample_kernel(dtype), row_grid(T), cis::kTokBlock, &a, stream);
+  // What the call's rows can ask for. A row whose list is short takes a small workgroup; rows that no
+  // count cuts need their weights summed up.
+  const bool greedy = !temperature && !(cis::scan_c(p.temperature) < INFINITY);
+  const int64_t k = greedy ? 1 : p.top_k == 0 || p.top_k >= V ? V : p.top_k;
+  const bool counted = greedy || (!top_k && k <= cis::kDrawListK && k < V);   // every row
+  const bool uncut = !counted && !top_k && k == V && !top_p && p.top_p == 1.f;
+  const bool wide = !counted && !uncut;
+  const bool weighed = !counted && (top_k || k == V);
+  const cis::TokRows r = tok_rows(logits, dtype, T, V, ld, mask);
+  char* base = static_cast<char*>(workspace);
+  const SampleLayout L = sample_layout(T, r.nvec, elem_bytes(dtype),
+                                       cis::scan_group(r.nvec, counted ? k : kManyLogits));
+  const cis::TokScan s = scan_at(base, L.scan);
+  if (int rc = launch_scan(r, s, dtype, cis::scan_c(1.f), stream)) return rc;
+  cis::SampleArgs a{r, s, reinterpret_cast<unsigned long long*>(base + L.draw),
+                    reinterpret_cast<uint32_t*>(base + L.ties), 0, u, p, temperature, top_k, top_p,
+                    min_p, ids_out, logp_out, logp_kept_out};
+  if (weighed) {
+    const int64_t per = cis::kWeighBlock / 64, need = (T * s.nch + per - 1) / per;
+    if (int rc = launch(cis::weigh_kernel(dtype), need < kMaxBlocks ? need : kMaxBlocks,
+                        cis::kWeighBlock, &a, stream))
+      return rc;
+  }
+  const int block = wide ? cis::kTokBlock : cis::kTopBlock;
+  for (; a.row0 < T; a.row0 += kMaxRows)
+    if (int rc = launch(cis::sample_kernel(dtype, wide),
+                        T - a.row0 < kMaxRows ? T - a.row0 : kMaxRows, block, &a, stream))
+      return rc;
+  return CIS_OK;
 }
 
 int cis_top_logits(const void* logits, int dtype, int64_t T, int64_t V, int64_t ld,
