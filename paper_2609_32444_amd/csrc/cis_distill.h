@@ -41,11 +41,6 @@ __device__ __forceinline__ float kl_part(float a, float d, float b) {
   return a > 0.f ? a * expm1_less(-d) : b;
 }
 
-// What sweep 2 needs of a row: a gradient of sgn exp2(fma(z, c, -b2)) where the token is not listed.
-struct RestGrad {
-  float b2;
-  uint32_t neg;
-};
 __device__ __forceinline__ RestGrad rest_grad(float coef, float R, float total) {
   const float b2 = coef != 0.f ? (R + log2f(total)) - log2f(fabsf(coef)) : INFINITY;
   return RestGrad{b2, coef < 0.f ? 1u : 0u};
@@ -62,6 +57,126 @@ __device__ __forceinline__ float others_grad(bool reverse, float p_rest, float q
   if (!(p_rest > 0.f)) return 0.f;
   if (reverse) return d - kl;
   return q_rest > 0.f ? -expm1f(-d) : 1.f;
+}
+
+// ------------------------------------------------------------------------------------------
+// A row's list in LDS, and the loss on it by one wave (KMAX entries at most; lane l has entries l,
+// l + 64, ...).
+// ------------------------------------------------------------------------------------------
+constexpr uint32_t kNone = 0xFFFFFFFFu;
+
+template <int KMAX>
+struct ListShared {
+  int32_t id[KMAX];       // -1: no entry
+  float z[KMAX];          // the student's logits
+  float lq[KMAX];         // log q
+  uint32_t grad[KMAX];    // gradient, in the logits' format
+};
+
+// Both lists' sums, in every lane.
+struct Teacher {
+  float q_rest, log_rest;   // the tail's share, and its log
+  bool finite;
+};
+struct Student {
+  float term;
+  RestGrad rest;
+  bool finite;
+};
+
+// A lane's share of a sum over the entries.
+template <class F>
+__device__ __forceinline__ void each_entry(const int32_t* id, int K, int lane, F&& f) {
+  for (int k = lane; k < K; k += 64)
+    if (id[k] >= 0) f(k);
+}
+
+// log q of the listed tokens, and of the tail.
+template <int KMAX>
+__device__ __forceinline__ Teacher teacher_list(const DistillArgs& a, int64_t row,
+                                                ListShared<KMAX>& sh, int lane) {
+  const float* values = a.values + row * a.ld_top;
+  const float c = a.c, tail = a.tail ? a.tail[row] * kLog2e : -INFINITY;
+  float m = -INFINITY;
+  each_entry(sh.id, a.K, lane, [&](int k) { m = fmaxf(m, values[k]); });
+  const float R = fmaxf(fmaxf(wave_max(m) * c, tail), kMinExp);
+  float s = 0.f;
+  each_entry(sh.id, a.K, lane, [&](int k) {
+    const float x = __builtin_fmaf(values[k], c, -R);
+    s += fast_exp2(x);
+    sh.lq[k] = x;
+  });
+  s = wave_sum(s);
+  const float rest = fast_exp2(tail - R), total = s + rest, L = log2f(total);
+  each_entry(sh.id, a.K, lane, [&](int k) { sh.lq[k] = (sh.lq[k] - L) * kLn2; });
+  return Teacher{rest / total, log_rest(s, rest), total > 0.f && total < INFINITY};
+}
+
+// The loss of a row whose listed logits are at sh.z and whose other tokens sum up to rest 2^R, and with
+// BWD its gradient: of the listed tokens at sh.grad.
+template <class E, bool BWD, int KMAX>
+__device__ __forceinline__ Student student_list(const DistillArgs& a, int64_t row,
+                                                ListShared<KMAX>& sh, int lane, const Teacher& t,
+                                                float R, float rest) {
+  const float c = a.c;
+  const bool reverse = a.reverse != 0;
+  float m = -INFINITY;
+  each_entry(sh.id, a.K, lane, [&](int k) { m = fmaxf(m, sh.z[k]); });
+  const float Rs = fmaxf(R, wave_max(m) * c);
+  rest *= fast_exp2(R - Rs);
+  float s = 0.f;
+  each_entry(sh.id, a.K, lane, [&](int k) { s += fast_exp2(__builtin_fmaf(sh.z[k], c, -Rs)); });
+  s = wave_sum(s);
+  const float total = s + rest, L = log2f(total);
+  const float p_rest = rest / total, d_rest = log_rest(s, rest) - t.log_rest;
+  auto lp_of = [&](int k) { return (__builtin_fmaf(sh.z[k], c, -Rs) - L) * kLn2; };
+  float kl = 0.f;
+  each_entry(sh.id, a.K, lane, [&](int k) {
+    const float lp = lp_of(k), lq = sh.lq[k], p = expf(lp), q = expf(lq);
+    kl += reverse ? kl_part(p, lp - lq, q) : kl_part(q, lq - lp, p);
+  });
+  kl = wave_sum(kl);
+  kl += reverse ? kl_part(p_rest, d_rest, t.q_rest) : kl_part(t.q_rest, -d_rest, p_rest);
+  // (kl_part takes a NaN share for 0)
+  if (!(total > 0.f && total < INFINITY) || !t.finite) kl = NAN;
+  const float w = a.scale * (a.weight ? a.weight[row] : 1.f);
+  Student out;
+  out.term = w == 0.f ? 0.f : w * kl;
+  out.finite = isfinite(kl) && isfinite(out.term);
+  out.rest = RestGrad{INFINITY, 0u};
+  if (BWD) {
+    const float cf = w / a.temperature;
+    each_entry(sh.id, a.K, lane, [&](int k) {
+      const float lp = lp_of(k), lq = sh.lq[k];
+      sh.grad[k] = E::bits_of(
+          cf == 0.f ? 0.f : cf * listed_grad(reverse, expf(lp), expf(lq), lp - lq, kl));
+    });
+    out.rest = rest_grad(cf == 0.f ? 0.f : cf * others_grad(reverse, p_rest, t.q_rest, d_rest, kl),
+                         Rs, total);
+  }
+  return out;
+}
+
+// The row's results, by one thread.
+__device__ __forceinline__ void put_row(const DistillArgs& a, int64_t row, float term, bool valid,
+                                        bool bad, bool finite) {
+  if (a.terms_user) a.terms_user[row] = term;
+  a.terms_ws[row] = term;
+  a.flags_ws[row] = (valid ? kFlagValid : 0) | (bad ? kFlagBadId : 0) |
+                    (valid && !finite ? kFlagNonFinite : 0);
+  a.logk_ws[row] = 0.f;
+  a.excess_ws[row] = 0.f;
+}
+
+// The gradient of a vector of logits none of which is listed.
+template <class E>
+__device__ __forceinline__ u32x4 rest_vec(u32x4 z, float c, const RestGrad& g) {
+  float f[E::kPerVec];
+  E::unpack(z, f);
+#pragma unroll
+  for (int e = 0; e < E::kPerVec; ++e) f[e] = fast_exp2(__builtin_fmaf(f[e], c, -g.b2));
+  const uint32_t sgn = g.neg ? E::kSignMask : 0u;
+  return E::pack(f) ^ u32x4{sgn, sgn, sgn, sgn};
 }
 
 }  // namespace cis

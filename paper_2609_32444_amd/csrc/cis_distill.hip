@@ -1,196 +1,354 @@
-// Distillation kernels (gfx950).
+// Distillation kernels (gfx950): a fused pass that holds a row on the compute unit, and a pass in
+// parts (scan, one wave per row, gradient by segments) for the forward direction and for few rows.
 #include "cis_distill.h"
+#include "cis_select.h"
 
 namespace cis {
 
 // ------------------------------------------------------------------------------------------
-// One workgroup per row. The list goes into a table in LDS, hashed by the 16-byte vector that a
-// token lies in, with chains; a sweep looks every vector up (one LDS read), leaves the listed
-// tokens out of its sum and notes their logits, and the gradient sweep puts theirs in.
+// Fused forward and backward: one workgroup per row, which it reads once and holds in registers (the
+// first NV vectors of every thread; longer rows read the rest a second time). The list goes into a
+// table in LDS, hashed by the vector that a token lies in, with chains; both sweeps look every
+// vector up (one LDS read), the first to leave the listed tokens out of its sum and to note their
+// logits, the second to put their gradients in.
 // ------------------------------------------------------------------------------------------
-constexpr int kDistillTable = 8192;
-constexpr uint32_t kNone = 0xFFFFFFFFu;
-struct DistillShared {
-  uint32_t head[kDistillTable];
-  uint32_t next[CIS_TOP_MAX_K];
-  int32_t id[CIS_TOP_MAX_K];
-  float z[CIS_TOP_MAX_K];        // the student's logits
-  float lq[CIS_TOP_MAX_K];       // log q
-  uint32_t grad[CIS_TOP_MAX_K];  // gradient, in the logits' format
-  float f[16];
+template <int BLOCK, int KMAX>
+struct FusedShared {
+  static constexpr int kTable = BLOCK == 1024 ? 8192 : BLOCK == 512 ? 4096 : BLOCK == 256 ? 2048 : 1024;
+  uint32_t head[kTable];
+  uint32_t next[KMAX];
+  ListShared<KMAX> list;
+  float f[16], g[16];
   u64 u[16];
+  RestGrad rest;
 };
 
-template <class E, bool BWD>
-__global__ __launch_bounds__(kTokBlock) void cis_distill_kernel(const DistillArgs a) {
-  constexpr int BLOCK = kTokBlock, NW = BLOCK / 64, EPV = E::kPerVec;
-  __shared__ DistillShared sh;
-  const int tid = threadIdx.x;
+template <class E, int BLOCK, int NV, int KMAX>
+__global__ __launch_bounds__(BLOCK) void cis_distill_kernel(const DistillArgs a) {
+  constexpr int NW = BLOCK / 64, EPV = E::kPerVec;
+  typedef FusedShared<BLOCK, KMAX> Shared;
+  __shared__ Shared sh;
+  const int tid = threadIdx.x, lane = tid & 63, wid = __builtin_amdgcn_readfirstlane(tid) >> 6;
   const int V = a.r.V, nvec = a.r.nvec, K = a.K;
-  const float c = kLog2e / a.temperature;
-  const bool reverse = a.reverse != 0, ragged = V % EPV != 0;
-  for (int i = tid; i < kDistillTable; i += BLOCK) sh.head[i] = kNone;
+  const float c = a.c;
+  const int64_t row = a.row0 + blockIdx.x;
+  const bool on = tok_on(a.r, row);
+  const __amdgpu_buffer_rsrc_t rs =
+      make_rsrc((const char*)a.r.logits + row * a.r.row_bytes, on ? (uint32_t)nvec * 16u : 0u);
+  // the list's ids are asked for before the row, so that the table is built while the row comes in
+  int32_t id0 = -1;
+  if (on && tid < K) id0 = a.ids[row * a.ld_top + tid];
+  u32x4 r[NV];
+  static_for<NV>([&](auto I) {
+    r[I] = bload(rs, (uint32_t)(I * BLOCK + tid) * 16u, 0u);
+    slot_fence();
+  });
+  for (int i = tid; i < Shared::kTable; i += BLOCK) sh.head[i] = kNone;
   __syncthreads();
-  auto sum = [&](float x) {
-    const float s = block_sum<NW>(x, sh.f);
-    __syncthreads();
-    return s;
+  u64 seen = 0;   // entries, and above them ids out of range or repeated
+  if (on)
+    for (int k = tid; k < K; k += BLOCK) {
+      const int32_t id = k < BLOCK ? id0 : a.ids[row * a.ld_top + k];
+      const bool in = id >= 0 && id < V;
+      sh.list.id[k] = in ? id : -1;
+      sh.next[k] = kNone;
+      if (in) sh.next[k] = atomicExch(&sh.head[(id / EPV) & (Shared::kTable - 1)], (uint32_t)k);
+      seen += in ? 1 : id == -1 ? 0 : u64(1) << 32;
+    }
+  __syncthreads();
+  if (on)
+    for (int k = tid; k < K; k += BLOCK)
+      if (sh.list.id[k] >= 0)
+        for (uint32_t o = sh.next[k]; o != kNone; o = sh.next[o])
+          if (sh.list.id[o] == sh.list.id[k]) seen += u64(1) << 32;
+  seen = block_sum<NW>(seen, sh.u);
+  const bool bad = (seen >> 32) != 0, valid = on && !bad && seen != 0;
+  Teacher teacher{};
+  if (valid && wid == 0) teacher = teacher_list(a, row, sh.list, lane);
+  auto head_of = [&](int v) { return sh.head[v & (Shared::kTable - 1)]; };
+  // sweep 1: the tokens that are not listed
+  float R = kMinExp, s = 0.f;
+  auto fold = [&](int v, u32x4 x) {
+    float f[EPV];
+    E::unpack(x, f);
+    if ((v + 1) * EPV > V) mask_past_end<E>(f, v, V);
+    for (uint32_t k = head_of(v); k != kNone; k = sh.next[k]) {
+      const int id = sh.list.id[k];
+      if (id / EPV != v) continue;
+#pragma unroll
+      for (int e = 0; e < EPV; ++e)
+        if (id % EPV == e) {
+          sh.list.z[k] = f[e];
+          f[e] = -INFINITY;
+        }
+    }
+    float m = f[0];
+#pragma unroll
+    for (int e = 1; e < EPV; ++e) m = fmaxf(m, f[e]);
+    const float Rn = fmaxf(R, m * c);
+    float part = 0.f;
+#pragma unroll
+    for (int e = 0; e < EPV; ++e) part += fast_exp2(__builtin_fmaf(f[e], c, -Rn));
+    s = s * fast_exp2(R - Rn) + part;
+    R = Rn;
   };
-  auto max = [&](float x) {
-    const float m = block_max<NW>(x, sh.f);
-    __syncthreads();
-    return m;
-  };
-  for (int64_t row = blockIdx.x; row < a.r.T; row += gridDim.x) {
-    const bool on = tok_on(a.r, row);
-    const int32_t* ids = a.ids + row * a.ld_top;
-    const float* values = a.values + row * a.ld_top;
-    // the table
-    u64 seen = 0;   // entries, and above them ids out of range or repeated
-    if (on)
-      for (int k = tid; k < K; k += BLOCK) {
-        const int32_t id = ids[k];
-        const bool in = id >= 0 && id < V;
-        sh.id[k] = in ? id : -1;
-        sh.next[k] = kNone;
-        if (in) sh.next[k] = atomicExch(&sh.head[(id / EPV) & (kDistillTable - 1)], (uint32_t)k);
-        seen += in ? 1 : id == -1 ? 0 : u64(1) << 32;
-      }
-    __syncthreads();
-    if (on)
-      for (int k = tid; k < K; k += BLOCK)
-        if (sh.id[k] >= 0)
-          for (uint32_t o = sh.next[k]; o != kNone; o = sh.next[o])
-            if (sh.id[o] == sh.id[k]) seen += u64(1) << 32;
-    seen = block_sum<NW>(seen, sh.u);
-    const bool bad = (seen >> 32) != 0, valid = on && !bad && seen != 0;
-    const __amdgpu_buffer_rsrc_t rs = tok_rsrc(a.r, row);
-    RestGrad g{INFINITY, 0u};
-    float term = 0.f;
-    bool nonfinite = false;
+  if (valid) {
+    static_for<NV>([&](auto I) {
+      if (I * BLOCK < nvec) fold(I * BLOCK + tid, r[I]);
+      slot_fence();
+    });
+    for (int v = NV * BLOCK + tid; v < nvec; v += BLOCK)
+      fold(v, bload_aux<kAuxStream1>(rs, (uint32_t)v * 16u));
+    wave_lse(R, s);
+    if (lane == 0) {
+      sh.f[wid] = R;
+      sh.g[wid] = s;
+    }
+  }
+  __syncthreads();
+  if (wid == 0) {
+    Student st{0.f, RestGrad{INFINITY, 0u}, true};
     if (valid) {
-      // sweep 1: the tokens that are not listed
-      float R = kMinExp, s = 0.f;
-      for (int v = tid; v < nvec; v += BLOCK) {
+      R = lane < NW ? sh.f[lane] : kMinExp;
+      s = lane < NW ? sh.g[lane] : 0.f;
+      wave_lse(R, s);
+      st = student_list<E, true>(a, row, sh.list, lane, teacher, R, s);
+    }
+    if (lane == 0) {
+      put_row(a, row, st.term, valid, on && bad, st.finite);
+      sh.rest = st.rest;
+    }
+  }
+  __syncthreads();
+  // sweep 2
+  const RestGrad g = sh.rest;
+  opaque(r);
+  void* grow = (char*)a.dlogits + row * a.grow_bytes;
+  const bool ragged = V % EPV != 0;
+  const __amdgpu_buffer_rsrc_t ws = make_rsrc(grow, (uint32_t)(nvec - (ragged ? 1 : 0)) * 16u);
+  auto put = [&](int v, u32x4 x) {
+    u32x4 out{0u, 0u, 0u, 0u};
+    if (valid) {
+      out = rest_vec<E>(x, c, g);
+      for (uint32_t k = head_of(v); k != kNone; k = sh.next[k])
+        if (sh.list.id[k] / EPV == v) out = E::set(out, sh.list.id[k] % EPV, sh.list.grad[k]);
+    }
+    bstore(out, ws, (uint32_t)v * 16u, 0u);
+    if (ragged && v == nvec - 1)
+      for (int e = 0; e < V - v * EPV; ++e) E::store_elem(grow, v * EPV + e, E::elem_bits(out, e));
+  };
+  static_for<NV>([&](auto I) {
+    if (I * BLOCK < nvec) put(I * BLOCK + tid, r[I]);
+    slot_fence();
+  });
+  for (int v = NV * BLOCK + tid; v < nvec; v += BLOCK)
+    put(v, bload_aux<kAuxStream2>(rs, (uint32_t)v * 16u));
+}
+
+// ------------------------------------------------------------------------------------------
+// In parts, 2: one wave per row. The scan has left the chunks' sums over all tokens; the vectors that
+// hold listed ones are read again, and taken out of the sums but for what else they hold (the sums
+// are in double, and a vector's sum is the same bits wherever it is formed). Where less than 2^-28
+// of the row remains, the row is summed again without the listed tokens. The vectors are found
+// in a table in LDS: open addressing, a key and the listed tokens of the vector as bits.
+// ------------------------------------------------------------------------------------------
+template <int KMAX>
+struct RowShared {
+  static constexpr int kTable = 4 * KMAX;
+  uint32_t key[kTable];
+  uint32_t bits[kTable];
+  uint16_t slot[KMAX];
+  ListShared<KMAX> list;
+};
+
+template <class E, bool BWD, int KMAX>
+__global__ __launch_bounds__(64) void cis_distill_row_kernel(const DistillArgs a) {
+  constexpr int EPV = E::kPerVec;
+  typedef RowShared<KMAX> Shared;
+  __shared__ Shared sh;
+  const int lane = threadIdx.x;
+  const int V = a.r.V, nvec = a.r.nvec, K = a.K, nch = a.s.nch;
+  const float c = a.c;
+  const int64_t row = a.row0 + blockIdx.x;
+  const bool on = tok_on(a.r, row);
+  const float* cmax = a.s.cmax + row * nch;
+  const double* csum = a.s.csum + row * nch;
+  uint32_t seen = 0, wrong = 0;
+  for (int i = lane; i < Shared::kTable; i += 64) sh.key[i] = kNone;
+  for (int i = lane; i < Shared::kTable; i += 64) sh.bits[i] = 0;
+  __syncthreads();   // (one wave)
+  if (on)
+    for (int k = lane; k < K; k += 64) {
+      const int32_t id = a.ids[row * a.ld_top + k];
+      const bool in = id >= 0 && id < V;
+      sh.list.id[k] = in ? id : -1;
+      if (in) {
+        const uint32_t v = (uint32_t)(id / EPV);
+        uint32_t at = (v * 0x9E3779B1u >> 16) & (Shared::kTable - 1);
+        for (;; at = (at + 1) & (Shared::kTable - 1)) {   // (a quarter full at most)
+          const uint32_t was = atomicCAS(&sh.key[at], kNone, v);
+          if (was == kNone || was == v) break;
+        }
+        const uint32_t bit = 1u << (id % EPV);
+        wrong += atomicOr(&sh.bits[at], bit) & bit ? 1 : 0;
+        sh.slot[k] = (uint16_t)at;
+        ++seen;
+      } else {
+        wrong += id != -1 ? 1 : 0;
+      }
+    }
+  seen = wave_sum(seen);
+  const bool bad = wave_sum(wrong) != 0, valid = on && !bad && seen != 0;
+  Student st{0.f, RestGrad{INFINITY, 0u}, true};
+  __syncthreads();
+  if (valid) {
+    const __amdgpu_buffer_rsrc_t rs = tok_rsrc(a.r, row);
+    float M = -INFINITY;
+    for (int i = lane; i < nch; i += 64) M = fmaxf(M, cmax[i]);
+    M = sum_ref(wave_max(M));
+    double whole = 0.0, less = 0.0;
+    for (int i = lane; i < nch; i += 64)
+      if (!(cmax[i] == -INFINITY && csum[i] == 0.0))
+        whole += csum[i] * (double)fast_exp2((cmax[i] - M) * c);
+    for (int k = lane; k < K; k += 64) {
+      const int id = sh.list.id[k];
+      if (id < 0) continue;
+      const int v = id / EPV;
+      const uint32_t bits = sh.bits[sh.slot[k]];
+      float f[EPV];
+      tok_vec<E>(rs, v, V, f);
+      const float m = sum_ref(cmax[v / kScanVecs]);
+      const float all = vec_sum<E>(f, c, m);
+#pragma unroll
+      for (int e = 0; e < EPV; ++e) {
+        if (id % EPV == e) sh.list.z[k] = f[e];
+        if (bits >> e & 1) f[e] = -INFINITY;
+      }
+      if (id % EPV == __ffs(bits) - 1)   // once for every vector
+        less += ((double)all - (double)vec_sum<E>(f, c, m)) * (double)fast_exp2((m - M) * c);
+    }
+    whole = wave_sum(whole);
+    double rest = whole - wave_sum(less);
+    float R = fmaxf(M * c, kMinExp), s;
+    // rest is relative to M; the loss takes it relative to 2^R
+    const float shift = fast_exp2(__builtin_fmaf(M, c, -R));
+    s = (float)rest * shift;
+    if (!(rest > whole * 0x1p-28)) {
+      R = kMinExp;
+      s = 0.f;
+      for (int v = lane; v < nvec; v += 64) {
         float f[EPV];
         tok_vec<E>(rs, v, V, f);
-        for (uint32_t k = sh.head[v & (kDistillTable - 1)]; k != kNone; k = sh.next[k]) {
-          const int id = sh.id[k];
-          if (id / EPV != v) continue;
+        uint32_t at = ((uint32_t)v * 0x9E3779B1u >> 16) & (Shared::kTable - 1), bits = 0;
+        for (; sh.key[at] != kNone; at = (at + 1) & (Shared::kTable - 1))
+          if (sh.key[at] == (uint32_t)v) {
+            bits = sh.bits[at];
+            break;
+          }
+        float m = -INFINITY, part = 0.f;
 #pragma unroll
-          for (int e = 0; e < EPV; ++e)
-            if (id % EPV == e) {
-              sh.z[k] = f[e];
-              f[e] = -INFINITY;
-            }
+        for (int e = 0; e < EPV; ++e) {
+          if (bits >> e & 1) f[e] = -INFINITY;
+          m = fmaxf(m, f[e]);
         }
-        float m = f[0];
-#pragma unroll
-        for (int e = 1; e < EPV; ++e) m = fmaxf(m, f[e]);
         const float Rn = fmaxf(R, m * c);
-        float part = 0.f;
 #pragma unroll
         for (int e = 0; e < EPV; ++e) part += fast_exp2(__builtin_fmaf(f[e], c, -Rn));
         s = s * fast_exp2(R - Rn) + part;
         R = Rn;
       }
-      const float Rr = max(R);
-      float rest = sum(s * fast_exp2(R - Rr));
-      // the list: the student's sums, and the teacher's
-      float zm = -INFINITY, vm = -INFINITY;
-      for (int k = tid; k < K; k += BLOCK)
-        if (sh.id[k] >= 0) {
-          zm = fmaxf(zm, sh.z[k]);
-          vm = fmaxf(vm, values[k]);
-        }
-      const float Rs = fmaxf(Rr, max(zm) * c);
-      rest *= fast_exp2(Rr - Rs);
-      const float tail = a.tail ? a.tail[row] * kLog2e : -INFINITY;
-      const float Rt = fmaxf(fmaxf(max(vm) * c, tail), kMinExp);
-      float es = 0.f, et = 0.f;
-      for (int k = tid; k < K; k += BLOCK)
-        if (sh.id[k] >= 0) {
-          es += fast_exp2(__builtin_fmaf(sh.z[k], c, -Rs));
-          et += fast_exp2(__builtin_fmaf(values[k], c, -Rt));
-        }
-      es = sum(es);
-      et = sum(et);
-      const float tr = fast_exp2(tail - Rt);
-      const float total = es + rest, ttotal = et + tr;
-      const float Ls = log2f(total), Lt = log2f(ttotal);
-      const float p_rest = rest / total, q_rest = tr / ttotal;
-      const float d_rest = log_rest(es, rest) - log_rest(et, tr);
-      auto lp_of = [&](int k) { return (__builtin_fmaf(sh.z[k], c, -Rs) - Ls) * kLn2; };
-      auto lq_of = [&](int k) { return (__builtin_fmaf(values[k], c, -Rt) - Lt) * kLn2; };
-      float kl = 0.f;
-      for (int k = tid; k < K; k += BLOCK)
-        if (sh.id[k] >= 0) {
-          const float lp = lp_of(k), lq = lq_of(k), p = expf(lp), q = expf(lq);
-          kl += reverse ? kl_part(p, lp - lq, q) : kl_part(q, lq - lp, p);
-        }
-      kl = sum(kl);
-      kl += reverse ? kl_part(p_rest, d_rest, q_rest) : kl_part(q_rest, -d_rest, p_rest);
-      // (kl_part takes a NaN share for 0)
-      const bool sums = total > 0.f && total < INFINITY && ttotal > 0.f && ttotal < INFINITY;
-      if (!sums) kl = NAN;
-      const float w = a.scale * (a.weight ? a.weight[row] : 1.f);
-      term = w == 0.f ? 0.f : w * kl;
-      nonfinite = !(isfinite(kl) && isfinite(term));
-      if (BWD) {
-        const float cf = w / a.temperature;
-        for (int k = tid; k < K; k += BLOCK)
-          if (sh.id[k] >= 0) {
-            const float lp = lp_of(k), lq = lq_of(k);
-            const float x = cf == 0.f ? 0.f : cf * listed_grad(reverse, expf(lp), expf(lq), lp - lq, kl);
-            sh.grad[k] = E::bits_of(x);
-          }
-        g = rest_grad(cf == 0.f ? 0.f : cf * others_grad(reverse, p_rest, q_rest, d_rest, kl), Rs,
-                      total);
-        __syncthreads();
-      }
+      wave_lse(R, s);
     }
-    if (tid == 0) {
-      if (a.terms_user) a.terms_user[row] = term;
-      a.terms_ws[row] = term;
-      a.flags_ws[row] = (valid ? kFlagValid : 0) | (on && bad ? kFlagBadId : 0) |
-                        (nonfinite ? kFlagNonFinite : 0);
-      a.logk_ws[row] = 0.f;
-      a.excess_ws[row] = 0.f;
+    const Teacher t = teacher_list(a, row, sh.list, lane);
+    st = student_list<E, BWD>(a, row, sh.list, lane, t, R, s);
+  }
+  if (lane == 0) put_row(a, row, st.term, valid, on && bad, st.finite);
+  if (BWD) {
+    if (lane == 0) {
+      a.rest[row] = st.rest;
+      a.valid[row] = valid ? 1 : 0;
     }
-    if (BWD) {
-      void* grow = (char*)a.dlogits + row * a.grow_bytes;
-      const __amdgpu_buffer_rsrc_t ws = make_rsrc(grow, (uint32_t)(nvec - (ragged ? 1 : 0)) * 16u);
-      const uint32_t sgn = g.neg ? E::kSignMask : 0u;
-      for (int v = tid; v < nvec; v += BLOCK) {
-        u32x4 out{0u, 0u, 0u, 0u};
-        if (valid) {
-          float f[EPV];
-          tok_vec<E>(rs, v, V, f);
-#pragma unroll
-          for (int e = 0; e < EPV; ++e) f[e] = fast_exp2(__builtin_fmaf(f[e], c, -g.b2));
-          out = E::pack(f) ^ u32x4{sgn, sgn, sgn, sgn};
-          for (uint32_t k = sh.head[v & (kDistillTable - 1)]; k != kNone; k = sh.next[k])
-            if (sh.id[k] / EPV == v) out = E::set(out, sh.id[k] % EPV, sh.grad[k]);
-        }
-        bstore(out, ws, (uint32_t)v * 16u, 0u);
-        if (ragged && v == nvec - 1)
-          for (int e = 0; e < V - v * EPV; ++e) E::store_elem(grow, v * EPV + e, E::elem_bits(out, e));
-      }
-      __syncthreads();
-    }
-    if (on)
-      for (int k = tid; k < K; k += BLOCK)
-        if (sh.id[k] >= 0) sh.head[(sh.id[k] / EPV) & (kDistillTable - 1)] = kNone;
-    __syncthreads();
+    for (int k = lane; k < K; k += 64)
+      a.grads[row * K + k] = valid && sh.list.id[k] >= 0 ? sh.list.grad[k] : 0u;
   }
 }
 
-const void* distill_kernel(int dtype, bool bwd) {
-  if (dtype == CIS_BF16)
-    return bwd ? (const void*)&cis_distill_kernel<Bf16, true>
-               : (const void*)&cis_distill_kernel<Bf16, false>;
-  return bwd ? (const void*)&cis_distill_kernel<F32, true>
-             : (const void*)&cis_distill_kernel<F32, false>;
+// ------------------------------------------------------------------------------------------
+// In parts, 3: the gradient by segments of kGradVecs vectors; listed tokens are put in by the segment
+// that they lie in, once its own stores are done.
+// ------------------------------------------------------------------------------------------
+template <class E>
+__global__ __launch_bounds__(kDistillGradBlock) void cis_distill_grad_kernel(const DistillArgs a) {
+  constexpr int EPV = E::kPerVec, BLOCK = kDistillGradBlock, K = kDistillGradVecs / BLOCK;
+  const int tid = threadIdx.x;
+  const int64_t b = a.row0 + blockIdx.x, row = b / a.nseg;
+  const int seg = (int)(b - row * a.nseg);
+  const bool valid = a.valid[row] != 0;
+  const RestGrad g = a.rest[row];
+  const bool ragged = a.r.V % EPV != 0;
+  const __amdgpu_buffer_rsrc_t rs =
+      make_rsrc((const char*)a.r.logits + row * a.r.row_bytes, valid ? (uint32_t)a.r.nvec * 16u : 0u);
+  void* grow = (char*)a.dlogits + row * a.grow_bytes;
+  const __amdgpu_buffer_rsrc_t ws =
+      make_rsrc(grow, (uint32_t)(a.r.nvec - (ragged ? 1 : 0)) * 16u);
+  const int v0 = seg * kDistillGradVecs + tid;
+  u32x4 r[K];
+  static_for<K>([&](auto I) { r[I] = bload(rs, (uint32_t)(v0 + I * BLOCK) * 16u, 0u); });
+  static_for<K>([&](auto I) {
+    const int v = v0 + I * BLOCK;
+    const u32x4 out = valid ? rest_vec<E>(r[I], a.c, g) : u32x4{0u, 0u, 0u, 0u};
+    bstore(out, ws, (uint32_t)v * 16u, 0u);
+    if (ragged && v == a.r.nvec - 1)
+      for (int e = 0; e < a.r.V - v * EPV; ++e)
+        E::store_elem(grow, v * EPV + e, E::elem_bits(out, e));
+  });
+  if (!valid) return;
+  asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
+  __syncthreads();
+  for (int k = tid; k < a.K; k += BLOCK) {
+    const int id = a.ids[row * a.ld_top + k];
+    if (id >= 0 && id / EPV / kDistillGradVecs == seg) E::store_elem(grow, id, a.grads[row * a.K + k]);
+  }
+}
+
+// Variants of the fused pass: the first that holds a row. 1024 x 19 vectors take 76 of a thread's
+// 128 registers; longer rows read the rest twice.
+struct FusedVariant {
+  int block, nv;
+  const void *few, *many;   // lists of up to 256 and 1024 entries
+};
+#define CIS_FUSED(E, B, N)                                         \
+  FusedVariant {                                                   \
+    B, N, (const void*)&cis_distill_kernel<E, B, N, 256>,          \
+        (const void*)&cis_distill_kernel<E, B, N, CIS_TOP_MAX_K>   \
+  }
+#define CIS_FUSED_TABLE(E)                                                                   \
+  {CIS_FUSED(E, 64, 5),   CIS_FUSED(E, 64, 10),  CIS_FUSED(E, 64, 18),   CIS_FUSED(E, 256, 8), \
+   CIS_FUSED(E, 256, 16), CIS_FUSED(E, 512, 12), CIS_FUSED(E, 512, 17), CIS_FUSED(E, 1024, 12), \
+   CIS_FUSED(E, 1024, 19)}
+static const FusedVariant kFusedBf16[] = CIS_FUSED_TABLE(Bf16);
+static const FusedVariant kFusedF32[] = CIS_FUSED_TABLE(F32);
+
+DistillVariant distill_fused(int dtype, int32_t nvec, int64_t K) {
+  const FusedVariant* t = dtype == CIS_BF16 ? kFusedBf16 : kFusedF32;
+  constexpr int n = sizeof(kFusedBf16) / sizeof(kFusedBf16[0]);
+  int i = 0;
+  while (i < n - 1 && (int64_t)t[i].block * t[i].nv < nvec) ++i;
+  return DistillVariant{t[i].block, K <= 256 ? t[i].few : t[i].many};
+}
+
+const void* distill_row_kernel(int dtype, bool bwd, int64_t K) {
+#define CIS_ROW(E, B)                                                 \
+  (K <= 64 ? (const void*)&cis_distill_row_kernel<E, B, 64>           \
+   : K <= 256 ? (const void*)&cis_distill_row_kernel<E, B, 256>       \
+              : (const void*)&cis_distill_row_kernel<E, B, CIS_TOP_MAX_K>)
+  if (dtype == CIS_BF16) return bwd ? CIS_ROW(Bf16, true) : CIS_ROW(Bf16, false);
+  return bwd ? CIS_ROW(F32, true) : CIS_ROW(F32, false);
+#undef CIS_ROW
+}
+const void* distill_grad_kernel(int dtype) {
+  return dtype == CIS_BF16 ? (const void*)&cis_distill_grad_kernel<Bf16>
+                           : (const void*)&cis_distill_grad_kernel<F32>;
 }
 
 }  // namespace cis

@@ -30,7 +30,7 @@ struct TokScan {
   void* gmax;      // [T, ngrp]
   float* cmax;     // [T, nch]
   double* csum;    // [T, nch]
-  int32_t nch, ngrp, gv;
+  int32_t nch, ngrp, gv;   // gv = 0: no groups
 };
 // Vectors per group, for the K largest logits of a row of nvec vectors: 8 (a 128-byte line),
 // where that leaves four times as many groups as logits are asked for, or each by itself. (The
@@ -46,7 +46,7 @@ inline ScanLayout scan_layout(int64_t T, int32_t nvec, int elem_bytes, int32_t g
   ScanLayout L{};
   L.nch = (nvec + kScanVecs - 1) / kScanVecs;
   L.gv = gv;
-  L.ngrp = (nvec + gv - 1) / gv;
+  L.ngrp = gv > 0 ? (nvec + gv - 1) / gv : 0;
   L.csum = 0;
   L.cmax = L.csum + align_up((size_t)T * L.nch * 8, 256);
   L.gmax = L.cmax + align_up((size_t)T * L.nch * 4, 256);
@@ -91,8 +91,21 @@ struct TopArgs {
   float* tail;                // nullable
 };
 
+// The gradient of a row's tokens that are not listed: exp2(fma(z, c, -b2)), negative with `neg`.
+struct RestGrad {
+  float b2;
+  uint32_t neg;
+};
+
 struct DistillArgs {
   TokRows r;
+  TokScan s;                  // in parts: the scan at this temperature, without groups
+  RestGrad* rest;             // [T] in parts, with the gradient, as the next two
+  uint8_t* valid;             // [T]
+  uint32_t* grads;            // [T, K] the listed tokens' gradients
+  int64_t row0;               // the launch's first row (cis_distill_grad_kernel: segment)
+  int32_t nseg;               // segments per row
+  float c;                    // scan_c(temperature)
   void* dlogits;              // nullable (forward)
   int64_t grow_bytes;
   const int32_t* ids;
@@ -120,6 +133,14 @@ const void* sample_kernel(int dtype, bool wide);
 const void* weigh_kernel(int dtype);
 const void* top_kernel(int dtype, int64_t K);
 int top_block(int64_t K);
-const void* distill_kernel(int dtype, bool bwd);
+constexpr int kDistillGradBlock = 128, kDistillGradVecs = 1024;   // 16 KiB of logits per workgroup
+struct DistillVariant {
+  int block;
+  const void* fn;
+};
+// The fused pass for rows of nvec vectors, and the kernels of the pass in parts.
+DistillVariant distill_fused(int dtype, int32_t nvec, int64_t K);
+const void* distill_row_kernel(int dtype, bool bwd, int64_t K);
+const void* distill_grad_kernel(int dtype);
 
 }  // namespace cis

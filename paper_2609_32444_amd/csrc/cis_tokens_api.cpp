@@ -71,6 +71,8 @@ cis::ScanLayout top_layout(int64_t T, int64_t V, int64_t K, int dtype) {
 }
 // Workgroups of 256 threads per launch of kernels that loop beyond (HIP refuses 2^32 work items).
 constexpr int64_t kMaxBlocks = int64_t(1) << 23;
+// Rows of a distillation call that may go in parts with the gradient.
+constexpr int64_t kFewRows = 192;
 // Logits that a draw may have to look at where its parameters do not say.
 constexpr int64_t kManyLogits = 256;
 
@@ -100,9 +102,6 @@ int launch_scan(const cis::TokRows& r, const cis::TokScan& s, int dtype, float c
 
 // Rows per launch of kernels of one workgroup per row (HIP refuses 2^32 work items).
 constexpr int64_t kMaxRows = int64_t(1) << 20;
-// Workgroups for T rows of one each; the kernels loop beyond that many.
-int64_t row_grid(int64_t T) { return T < (int64_t(1) << 20) ? T : int64_t(1) << 20; }
-
 // Temperatures of a softmax: log2(e) / temperature and a logit's exponent stay within float32.
 bool softmax_temperature(float t) { return t >= 0x1p-64f && t <= 0x1p64f; }
 
@@ -143,6 +142,54 @@ struct DistillCall {
   size_t workspace_bytes;
 };
 
+struct DistillLayout {
+  cis::WsLayout loss;
+  cis::ScanLayout scan;
+  size_t scan_off, rest, valid, grads, total;
+};
+DistillLayout distill_layout(int64_t T, int64_t V, int64_t K, int dtype) {
+  DistillLayout D{};
+  D.loss = cis::ws_layout(T, 0);
+  D.scan = cis::scan_layout(T, row_vecs(V, dtype), elem_bytes(dtype), 0);
+  D.scan_off = D.loss.total;
+  D.rest = D.scan_off + D.scan.total;
+  D.valid = D.rest + cis::align_up((size_t)T * sizeof(cis::RestGrad), 256);
+  D.grads = D.valid + cis::align_up((size_t)T, 256);
+  // (the fused pass over many rows does not come here)
+  const int64_t few = T < kFewRows ? T : kFewRows;
+  D.total = D.grads + cis::align_up((size_t)few * (size_t)K * 4, 256);
+  return D;
+}
+
+// With the gradient, one workgroup per row, unless the rows are too few to fill the chip: then, and
+// without the gradient, in parts.
+bool few_rows(int64_t T, int32_t nvec) {
+  return T <= (nvec > 19456 ? 192 : nvec >= 12288 ? 112 : nvec >= 6144 ? 32 : 0);
+}
+
+int launch_distill(const DistillCall& c, const DistillLayout& D, char* base, cis::DistillArgs& a,
+                   hipStream_t stream) {
+  auto by_rows = [&](const void* fn, int block, int64_t n) {
+    for (a.row0 = 0; a.row0 < n; a.row0 += kMaxRows)
+      if (int rc = launch(fn, n - a.row0 < kMaxRows ? n - a.row0 : kMaxRows, block, &a, stream))
+        return rc;
+    return (int)CIS_OK;
+  };
+  if (c.bwd && !few_rows(c.T, a.r.nvec)) {
+    const cis::DistillVariant v = cis::distill_fused(c.dtype, a.r.nvec, c.K);
+    return by_rows(v.fn, v.block, c.T);
+  }
+  a.s = scan_at(base + D.scan_off, D.scan);
+  a.rest = reinterpret_cast<cis::RestGrad*>(base + D.rest);
+  a.valid = reinterpret_cast<uint8_t*>(base + D.valid);
+  a.grads = reinterpret_cast<uint32_t*>(base + D.grads);
+  a.nseg = (a.r.nvec + cis::kDistillGradVecs - 1) / cis::kDistillGradVecs;
+  if (int rc = launch_scan(a.r, a.s, c.dtype, a.c, stream)) return rc;
+  if (int rc = by_rows(cis::distill_row_kernel(c.dtype, c.bwd, c.K), 64, c.T)) return rc;
+  if (!c.bwd) return CIS_OK;
+  return by_rows(cis::distill_grad_kernel(c.dtype), cis::kDistillGradBlock, c.T * a.nseg);
+}
+
 int run_distill(const DistillCall& c, hipStream_t stream) {
   if (!c.prm) return CIS_ERR_NULL;
   if (int rc = check_shape(c.dtype, c.T, c.V, c.ld)) return rc;
@@ -171,7 +218,8 @@ int run_distill(const DistillCall& c, hipStream_t stream) {
   if (const int cus = device_cus(); cus < 0) return cus;
 
   char* base = static_cast<char*>(c.workspace);
-  const cis::WsLayout L = cis::ws_layout(c.T, 0);
+  const DistillLayout D = distill_layout(c.T, c.V, c.K, c.dtype);
+  const cis::WsLayout& L = D.loss;
   if (c.T > 0) {
     cis::DistillArgs a{};
     a.r = tok_rows(c.logits, c.dtype, c.T, c.V, c.ld, c.mask);
@@ -191,9 +239,8 @@ int run_distill(const DistillCall& c, hipStream_t stream) {
     a.flags_ws = reinterpret_cast<uint8_t*>(base + L.flags);
     a.logk_ws = reinterpret_cast<float*>(base + L.logk);
     a.excess_ws = reinterpret_cast<float*>(base + L.excess);
-    if (int rc = launch(cis::distill_kernel(c.dtype, c.bwd), row_grid(c.T), cis::kTokBlock, &a,
-                        stream))
-      return rc;
+    a.c = cis::scan_c(p.temperature);
+    if (int rc = launch_distill(c, D, base, a, stream)) return rc;
   }
   return launch_finalize(base, L, c.T, c.loss, stream);
 }
@@ -220,7 +267,7 @@ size_t cis_top_logits_workspace_bytes(int64_t T, int64_t V, int64_t K, int dtype
 
 size_t cis_distill_workspace_bytes(int64_t T, int64_t V, int64_t K, int dtype) {
   if (T < 0 || V < 1 || V > kMaxV || K < 1 || K > CIS_TOP_MAX_K || !known(dtype)) return 0;
-  return cis::ws_layout(T, 0).total;
+  return distill_layout(T, V, K, dtype).total;
 }
 
 int cis_sample(const void* logits, int dtype, int64_t T, int64_t V, int64_t ld, const float* u,

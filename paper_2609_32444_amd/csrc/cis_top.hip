@@ -50,6 +50,7 @@ __global__ __launch_bounds__(kScanBlock) void cis_scan_kernel(const ScanArgs a) 
       a.s.csum[w] = s;
     }
     elem_t<E>* gm = (elem_t<E>*)a.s.gmax + row * ngrp;
+    if (GV == 0) continue;
     if (GV == 1) {
       static_for<K>([&](auto I) {
         const int g = v0 + I * 64;
@@ -72,9 +73,11 @@ __global__ __launch_bounds__(kScanBlock) void cis_scan_kernel(const ScanArgs a) 
 }
 
 const void* scan_kernel(int dtype, int32_t gv) {
-  if (dtype == CIS_BF16)
-    return gv == 1 ? (const void*)&cis_scan_kernel<Bf16, 1> : (const void*)&cis_scan_kernel<Bf16, 8>;
-  return gv == 1 ? (const void*)&cis_scan_kernel<F32, 1> : (const void*)&cis_scan_kernel<F32, 8>;
+#define CIS_SCAN(E)                                                                      \
+  (gv == 0 ? (const void*)&cis_scan_kernel<E, 0>                                         \
+           : gv == 1 ? (const void*)&cis_scan_kernel<E, 1> : (const void*)&cis_scan_kernel<E, 8>)
+  return dtype == CIS_BF16 ? CIS_SCAN(Bf16) : CIS_SCAN(F32);
+#undef CIS_SCAN
 }
 
 // ------------------------------------------------------------------------------------------
