@@ -13,10 +13,10 @@ namespace cis {
 // Lowest reference of a row's sum: finite where there is nothing but -inf.
 constexpr float kMinExp = -0x1p126f;
 constexpr float kLn2 = 0.693147180559945309417f;
-// expm1(d) - d >= 0, to a few units in the last place (near 0 by its series, which does not
-// cancel: nine terms, the first left out below 2^-24 of the sum up to |d| = 0.6).
+// expm1(d) - d for |d| <= kNearLog by its series (which does not cancel): nine terms, the first left
+// out below 2^-24 of the sum.
+constexpr float kNearLog = 0.6f;
 __device__ __forceinline__ float expm1_less(float d) {
-  if (fabsf(d) > 0.6f) return expm1f(d) - d;
   float s = 1.f / 3628800.f;
   s = __builtin_fmaf(s, d, 1.f / 362880.f);
   s = __builtin_fmaf(s, d, 1.f / 40320.f);
@@ -35,10 +35,11 @@ __device__ __forceinline__ float log_rest(float list, float rest) {
   return rest > 0.5f * total ? log1pf(-list / total) : logf(rest / total);
 }
 
-// A class's part of sum a log(a/b) for log a - log b = d: a log(a/b) - a + b, whose limit at a = 0
-// is b.
+// A class's part of sum a log(a/b) for log a - log b = d: a log(a/b) - a + b >= 0, where a and b are
+// near each other from the series, since the terms cancel there; b at a = 0.
 __device__ __forceinline__ float kl_part(float a, float d, float b) {
-  return a > 0.f ? a * expm1_less(-d) : b;
+  if (!(a > 0.f)) return b;
+  return fabsf(d) <= kNearLog ? a * expm1_less(-d) : __builtin_fmaf(a, d, b - a);
 }
 
 __device__ __forceinline__ RestGrad rest_grad(float coef, float R, float total) {
@@ -50,7 +51,7 @@ __device__ __forceinline__ RestGrad rest_grad(float coef, float R, float total) 
 // others.
 __device__ __forceinline__ float listed_grad(bool reverse, float p, float q, float d, float kl) {
   if (reverse) return p > 0.f ? p * (d - kl) : 0.f;
-  return q > 0.f && d < 1.f ? q * expm1f(d) : p - q;   // (p - q cancels where they are close)
+  return fabsf(d) <= kNearLog ? q * (d + expm1_less(d)) : p - q;   // (p - q cancels near 0)
 }
 __device__ __forceinline__ float others_grad(bool reverse, float p_rest, float q_rest, float d,
                                              float kl) {
@@ -70,6 +71,7 @@ struct ListShared {
   int32_t id[KMAX];       // -1: no entry
   float z[KMAX];          // the student's logits
   float lq[KMAX];         // log q
+  float q[KMAX];
   uint32_t grad[KMAX];    // gradient, in the logits' format
 };
 
@@ -108,7 +110,11 @@ __device__ __forceinline__ Teacher teacher_list(const DistillArgs& a, int64_t ro
   });
   s = wave_sum(s);
   const float rest = fast_exp2(tail - R), total = s + rest, L = log2f(total);
-  each_entry(sh.id, a.K, lane, [&](int k) { sh.lq[k] = (sh.lq[k] - L) * kLn2; });
+  each_entry(sh.id, a.K, lane, [&](int k) {
+    const float x = sh.lq[k] - L;
+    sh.lq[k] = x * kLn2;
+    sh.q[k] = fast_exp2(x);
+  });
   return Teacher{rest / total, log_rest(s, rest), total > 0.f && total < INFINITY};
 }
 
@@ -129,11 +135,17 @@ __device__ __forceinline__ Student student_list(const DistillArgs& a, int64_t ro
   s = wave_sum(s);
   const float total = s + rest, L = log2f(total);
   const float p_rest = rest / total, d_rest = log_rest(s, rest) - t.log_rest;
-  auto lp_of = [&](int k) { return (__builtin_fmaf(sh.z[k], c, -Rs) - L) * kLn2; };
+  // (the logits' exponents are formed once more for the gradient: nothing else of the entry is kept)
+  auto share = [&](int k, float& p) {
+    const float x = __builtin_fmaf(sh.z[k], c, -Rs) - L;
+    p = fast_exp2(x);
+    return x * kLn2 - sh.lq[k];   // log p - log q
+  };
   float kl = 0.f;
   each_entry(sh.id, a.K, lane, [&](int k) {
-    const float lp = lp_of(k), lq = sh.lq[k], p = expf(lp), q = expf(lq);
-    kl += reverse ? kl_part(p, lp - lq, q) : kl_part(q, lq - lp, p);
+    float p;
+    const float d = share(k, p), q = sh.q[k];
+    kl += reverse ? kl_part(p, d, q) : kl_part(q, -d, p);
   });
   kl = wave_sum(kl);
   kl += reverse ? kl_part(p_rest, d_rest, t.q_rest) : kl_part(t.q_rest, -d_rest, p_rest);
@@ -147,9 +159,9 @@ __device__ __forceinline__ Student student_list(const DistillArgs& a, int64_t ro
   if (BWD) {
     const float cf = w / a.temperature;
     each_entry(sh.id, a.K, lane, [&](int k) {
-      const float lp = lp_of(k), lq = sh.lq[k];
-      sh.grad[k] = E::bits_of(
-          cf == 0.f ? 0.f : cf * listed_grad(reverse, expf(lp), expf(lq), lp - lq, kl));
+      float p;
+      const float d = share(k, p);
+      sh.grad[k] = E::bits_of(cf == 0.f ? 0.f : cf * listed_grad(reverse, p, sh.q[k], d, kl));
     });
     out.rest = rest_grad(cf == 0.f ? 0.f : cf * others_grad(reverse, p_rest, t.q_rest, d_rest, kl),
                          Rs, total);

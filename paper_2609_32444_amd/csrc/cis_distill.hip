@@ -8,141 +8,192 @@ namespace cis {
 // ------------------------------------------------------------------------------------------
 // Fused forward and backward: one workgroup per row, which it reads once and holds in registers (the
 // first NV vectors of every thread; longer rows read the rest a second time). The list goes into a
-// table in LDS, hashed by the vector that a token lies in, with chains; both sweeps look every
-// vector up (one LDS read), the first to leave the listed tokens out of its sum and to note their
-// logits, the second to put their gradients in.
+// table in LDS, hashed by the vector that a token lies in, with chains, and every thread has a bit for
+// each of its vectors that holds one: the first sweep leaves the listed tokens out of its sum and notes
+// their logits, the second puts their gradients in.
 // ------------------------------------------------------------------------------------------
 template <int BLOCK, int KMAX>
 struct FusedShared {
   static constexpr int kTable = BLOCK == 1024 ? 8192 : BLOCK == 512 ? 4096 : BLOCK == 256 ? 2048 : 1024;
   uint32_t head[kTable];
   uint32_t next[KMAX];
+  uint32_t mine[BLOCK];   // a thread's vectors (the first 32) with listed tokens
   ListShared<KMAX> list;
   float f[16], g[16];
-  u64 u[16];
+  uint32_t u[16];
   RestGrad rest;
 };
 
+// A barrier for what lies in LDS: loads of the row stay in flight across it.
+__device__ __forceinline__ void lds_barrier() {
+  asm volatile("s_waitcnt lgkmcnt(0)\n\ts_barrier" ::: "memory");
+}
+
 template <class E, int BLOCK, int NV, int KMAX>
-__global__ __launch_bounds__(BLOCK) void cis_distill_kernel(const DistillArgs a) {
+__global__ __launch_bounds__(BLOCK) __attribute__((amdgpu_waves_per_eu(4))) void cis_distill_kernel(const DistillArgs a) {
   constexpr int NW = BLOCK / 64, EPV = E::kPerVec;
+  constexpr int FIRST = NV > 8 ? 8 : NV;   // vectors that are asked for before the list
   typedef FusedShared<BLOCK, KMAX> Shared;
   __shared__ Shared sh;
-  const int tid = threadIdx.x, lane = tid & 63, wid = __builtin_amdgcn_readfirstlane(tid) >> 6;
-  const int V = a.r.V, nvec = a.r.nvec, K = a.K;
-  const float c = a.c;
-  const int64_t row = a.row0 + blockIdx.x;
-  const bool on = tok_on(a.r, row);
-  const __amdgpu_buffer_rsrc_t rs =
-      make_rsrc((const char*)a.r.logits + row * a.r.row_bytes, on ? (uint32_t)nvec * 16u : 0u);
-  // the list's ids are asked for before the row, so that the table is built while the row comes in
+  for (int i = threadIdx.x; i < Shared::kTable; i += BLOCK) sh.head[i] = kNone;
+  sh.mine[threadIdx.x] = 0;
+  // Rows by rounds of the grid. From round to round a workgroup moves on by a few places, so that it does
+  // not meet the same place of every response (padding is periodic).
+  constexpr uint32_t kShift = 61;
+  uint32_t place = blockIdx.x;
   int32_t id0 = -1;
-  if (on && tid < K) id0 = a.ids[row * a.ld_top + tid];
-  u32x4 r[NV];
-  static_for<NV>([&](auto I) {
-    r[I] = bload(rs, (uint32_t)(I * BLOCK + tid) * 16u, 0u);
-    slot_fence();
-  });
-  for (int i = tid; i < Shared::kTable; i += BLOCK) sh.head[i] = kNone;
-  __syncthreads();
-  u64 seen = 0;   // entries, and above them ids out of range or repeated
-  if (on)
-    for (int k = tid; k < K; k += BLOCK) {
-      const int32_t id = k < BLOCK ? id0 : a.ids[row * a.ld_top + k];
-      const bool in = id >= 0 && id < V;
-      sh.list.id[k] = in ? id : -1;
-      sh.next[k] = kNone;
-      if (in) sh.next[k] = atomicExch(&sh.head[(id / EPV) & (Shared::kTable - 1)], (uint32_t)k);
-      seen += in ? 1 : id == -1 ? 0 : u64(1) << 32;
+  if ((int)threadIdx.x < a.K) id0 = a.ids[(int64_t)blockIdx.x * a.ld_top + threadIdx.x];
+  for (int64_t round = 0; round < a.r.T; round += gridDim.x) {
+    const int64_t row = round + place;
+    if (row >= a.r.T) break;   // (the last round)
+    if (gridDim.x > kShift) {
+      place += kShift;
+      if (place >= gridDim.x) place -= gridDim.x;
     }
-  __syncthreads();
-  if (on)
-    for (int k = tid; k < K; k += BLOCK)
-      if (sh.list.id[k] >= 0)
-        for (uint32_t o = sh.next[k]; o != kNone; o = sh.next[o])
-          if (sh.list.id[o] == sh.list.id[k]) seen += u64(1) << 32;
-  seen = block_sum<NW>(seen, sh.u);
-  const bool bad = (seen >> 32) != 0, valid = on && !bad && seen != 0;
-  Teacher teacher{};
-  if (valid && wid == 0) teacher = teacher_list(a, row, sh.list, lane);
-  auto head_of = [&](int v) { return sh.head[v & (Shared::kTable - 1)]; };
-  // sweep 1: the tokens that are not listed
-  float R = kMinExp, s = 0.f;
-  auto fold = [&](int v, u32x4 x) {
-    float f[EPV];
-    E::unpack(x, f);
-    if ((v + 1) * EPV > V) mask_past_end<E>(f, v, V);
-    for (uint32_t k = head_of(v); k != kNone; k = sh.next[k]) {
-      const int id = sh.list.id[k];
-      if (id / EPV != v) continue;
-#pragma unroll
-      for (int e = 0; e < EPV; ++e)
-        if (id % EPV == e) {
-          sh.list.z[k] = f[e];
-          f[e] = -INFINITY;
+    const int64_t next = round + gridDim.x + place;
+    // (what follows from these is formed again for every row: kept, it would take up the registers)
+    int tid = threadIdx.x, nvec = a.r.nvec;
+    asm volatile("" : "+v"(tid));
+    asm volatile("" : "+s"(nvec));
+    const int lane = tid & 63, wid = __builtin_amdgcn_readfirstlane(tid) >> 6;
+    const int V = a.r.V, K = a.K;
+    const float c = a.c;
+    const bool on = tok_on(a.r, row);
+    const __amdgpu_buffer_rsrc_t rs =
+        make_rsrc((const char*)a.r.logits + row * a.r.row_bytes, on ? (uint32_t)nvec * 16u : 0u);
+    u32x4 r[NV];
+    static_for<FIRST>([&](auto I) {
+      r[I] = bload(rs, (uint32_t)(I * BLOCK + tid) * 16u, 0u);
+      slot_fence();
+    });
+    // the table
+    uint32_t seen = 0, wrong = 0;   // entries; ids out of range or repeated
+    lds_barrier();   // (the last row's is cleared)
+    if (on)
+      for (int k = tid; k < K; k += BLOCK) {
+        const int32_t id = k < BLOCK ? id0 : a.ids[row * a.ld_top + k];
+        const bool in = id >= 0 && id < V;
+        sh.list.id[k] = in ? id : -1;
+        sh.next[k] = kNone;
+        if (in) {
+          const int v = id / EPV;
+          sh.next[k] = atomicExch(&sh.head[v & (Shared::kTable - 1)], (uint32_t)k);
+          if (v < NV * BLOCK) atomicOr(&sh.mine[v & (BLOCK - 1)], 1u << (v / BLOCK));
         }
+        seen |= in ? 1u : 0u;
+        wrong |= in || id == -1 ? 0u : 1u;
+      }
+    lds_barrier();
+    id0 = -1;
+    if (next < a.r.T && tid < K) id0 = a.ids[next * a.ld_top + tid];
+    if (on)
+      for (int k = tid; k < K; k += BLOCK)
+        if (sh.list.id[k] >= 0)
+          for (uint32_t o = sh.next[k]; o != kNone; o = sh.next[o])
+            wrong |= sh.list.id[o] == sh.list.id[k] ? 1u : 0u;
+    if (lane == 0) sh.u[wid] = 0;
+    if (__ballot(seen | wrong)) {
+      const uint32_t any = (__ballot(seen) ? 1u : 0u) | (__ballot(wrong) ? 2u : 0u);
+      if (lane == 0) sh.u[wid] = any;
     }
-    float m = f[0];
+    static_for<NV - FIRST>([&](auto I) {
+      r[FIRST + I] = bload(rs, (uint32_t)((FIRST + I) * BLOCK + tid) * 16u, 0u);
+      slot_fence();
+    });
+    lds_barrier();
+    uint32_t any = 0;
+    for (int w = 0; w < NW; ++w) any |= sh.u[w];
+    const bool bad = (any & 2u) != 0, valid = on && any == 1u;
+    // f(entry, element) for the listed tokens of vector v
+    auto each_listed = [&](int v, auto&& f) {
+      for (uint32_t k = sh.head[v & (Shared::kTable - 1)]; k != kNone; k = sh.next[k])
+        if (sh.list.id[k] / EPV == v) f(k, sh.list.id[k] % EPV);
+    };
+    const uint32_t mine = sh.mine[tid];
+    // sweep 1: the tokens that are not listed
+    float R = kMinExp, s = 0.f;
+    auto fold = [&](int v, u32x4 x, bool listed, bool last) {
+      float f[EPV];
+      E::unpack(x, f);
+      if (last) mask_past_end<E>(f, v, V);
+      if (listed)
+        each_listed(v, [&](uint32_t k, int at) {
 #pragma unroll
-    for (int e = 1; e < EPV; ++e) m = fmaxf(m, f[e]);
-    const float Rn = fmaxf(R, m * c);
-    float part = 0.f;
+          for (int e = 0; e < EPV; ++e)
+            if (at == e) {
+              sh.list.z[k] = f[e];
+              f[e] = -INFINITY;
+            }
+        });
+      float m = f[0];
 #pragma unroll
-    for (int e = 0; e < EPV; ++e) part += fast_exp2(__builtin_fmaf(f[e], c, -Rn));
-    s = s * fast_exp2(R - Rn) + part;
-    R = Rn;
-  };
-  if (valid) {
+      for (int e = 1; e < EPV; ++e) m = fmaxf(m, f[e]);
+      const float Rn = fmaxf(R, m * c);
+      float part = 0.f;
+#pragma unroll
+      for (int e = 0; e < EPV; ++e) part += fast_exp2(__builtin_fmaf(f[e], c, -Rn));
+      s = s * fast_exp2(R - Rn) + part;
+      R = Rn;
+    };
+    Teacher teacher{};
+    if (valid) {
+      if (wid == 0) teacher = teacher_list(a, row, sh.list, lane);
+      static_for<NV>([&](auto I) {
+        if (I * BLOCK < nvec)
+          fold(I * BLOCK + tid, r[I], mine >> I & 1, (I + 1) * BLOCK * EPV > V);
+        slot_fence();
+      });
+      for (int v = NV * BLOCK + tid; v < nvec; v += BLOCK)
+        fold(v, bload_aux<kAuxStream1>(rs, (uint32_t)v * 16u), true, (v + 1) * EPV > V);
+      wave_lse(R, s);
+      if (lane == 0) {
+        sh.f[wid] = R;
+        sh.g[wid] = s;
+      }
+    }
+    lds_barrier();
+    if (wid == 0) {
+      Student st{0.f, RestGrad{INFINITY, 0u}, true};
+      if (valid) {
+        R = lane < NW ? sh.f[lane] : kMinExp;
+        s = lane < NW ? sh.g[lane] : 0.f;
+        wave_lse(R, s);
+        st = student_list<E, true>(a, row, sh.list, lane, teacher, R, s);
+      }
+      if (lane == 0) {
+        put_row(a, row, st.term, valid, on && bad, st.finite);
+        sh.rest = st.rest;
+      }
+    }
+    lds_barrier();
+    // sweep 2
+    const RestGrad g = sh.rest;
+    opaque(r);
+    void* grow = (char*)a.dlogits + row * a.grow_bytes;
+    const bool ragged = V % EPV != 0;
+    const __amdgpu_buffer_rsrc_t ws = make_rsrc(grow, (uint32_t)(nvec - (ragged ? 1 : 0)) * 16u);
+    auto put = [&](int v, u32x4 x, bool listed, bool last) {
+      u32x4 out{0u, 0u, 0u, 0u};
+      if (valid) {
+        out = rest_vec<E>(x, c, g);
+        if (listed) each_listed(v, [&](uint32_t k, int e) { out = E::set(out, e, sh.list.grad[k]); });
+      }
+      bstore(out, ws, (uint32_t)v * 16u, 0u);
+      if (last && ragged && v == nvec - 1)
+        for (int e = 0; e < V - v * EPV; ++e) E::store_elem(grow, v * EPV + e, E::elem_bits(out, e));
+    };
     static_for<NV>([&](auto I) {
-      if (I * BLOCK < nvec) fold(I * BLOCK + tid, r[I]);
+      if (I * BLOCK < nvec) put(I * BLOCK + tid, r[I], mine >> I & 1, (I + 1) * BLOCK >= nvec);
       slot_fence();
     });
     for (int v = NV * BLOCK + tid; v < nvec; v += BLOCK)
-      fold(v, bload_aux<kAuxStream1>(rs, (uint32_t)v * 16u));
-    wave_lse(R, s);
-    if (lane == 0) {
-      sh.f[wid] = R;
-      sh.g[wid] = s;
-    }
+      put(v, bload_aux<kAuxStream2>(rs, (uint32_t)v * 16u), true, true);
+    sh.mine[tid] = 0;
+    lds_barrier();   // nobody looks a vector up any more
+    if (on)
+      for (int k = tid; k < K; k += BLOCK)
+        if (sh.list.id[k] >= 0) sh.head[(sh.list.id[k] / EPV) & (Shared::kTable - 1)] = kNone;
   }
-  __syncthreads();
-  if (wid == 0) {
-    Student st{0.f, RestGrad{INFINITY, 0u}, true};
-    if (valid) {
-      R = lane < NW ? sh.f[lane] : kMinExp;
-      s = lane < NW ? sh.g[lane] : 0.f;
-      wave_lse(R, s);
-      st = student_list<E, true>(a, row, sh.list, lane, teacher, R, s);
-    }
-    if (lane == 0) {
-      put_row(a, row, st.term, valid, on && bad, st.finite);
-      sh.rest = st.rest;
-    }
-  }
-  __syncthreads();
-  // sweep 2
-  const RestGrad g = sh.rest;
-  opaque(r);
-  void* grow = (char*)a.dlogits + row * a.grow_bytes;
-  const bool ragged = V % EPV != 0;
-  const __amdgpu_buffer_rsrc_t ws = make_rsrc(grow, (uint32_t)(nvec - (ragged ? 1 : 0)) * 16u);
-  auto put = [&](int v, u32x4 x) {
-    u32x4 out{0u, 0u, 0u, 0u};
-    if (valid) {
-      out = rest_vec<E>(x, c, g);
-      for (uint32_t k = head_of(v); k != kNone; k = sh.next[k])
-        if (sh.list.id[k] / EPV == v) out = E::set(out, sh.list.id[k] % EPV, sh.list.grad[k]);
-    }
-    bstore(out, ws, (uint32_t)v * 16u, 0u);
-    if (ragged && v == nvec - 1)
-      for (int e = 0; e < V - v * EPV; ++e) E::store_elem(grow, v * EPV + e, E::elem_bits(out, e));
-  };
-  static_for<NV>([&](auto I) {
-    if (I * BLOCK < nvec) put(I * BLOCK + tid, r[I]);
-    slot_fence();
-  });
-  for (int v = NV * BLOCK + tid; v < nvec; v += BLOCK)
-    put(v, bload_aux<kAuxStream2>(rs, (uint32_t)v * 16u));
 }
 
 // ------------------------------------------------------------------------------------------

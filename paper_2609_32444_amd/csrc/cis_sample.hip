@@ -58,12 +58,6 @@ __device__ __forceinline__ uint32_t vec_weight(const float (&f)[E::kPerVec], flo
   return s;
 }
 
-__device__ __forceinline__ u64 wave_total(u64 x) {
-#pragma unroll
-  for (int off = 32; off >= 1; off >>= 1) x += __shfl_xor(x, off, 64);
-  return x;
-}
-
 // ------------------------------------------------------------------------------------------
 // One wave per chunk: the sum of its weights. A chunk whose largest logit has no weight is not read.
 // ------------------------------------------------------------------------------------------
@@ -93,7 +87,7 @@ __global__ __launch_bounds__(kWeighBlock) void cis_weigh_kernel(const SampleArgs
         s += vec_weight<E>(f, M, p.c, least);
         slot_fence();
       });
-      s = wave_total(s);
+      s = wave_sum(s);
     }
     if (lane == 0) a.draw[w] = s;
   }
@@ -300,7 +294,7 @@ struct RowDraw {
       return (i < sel.nch ? mass[i] : 0) + (nt < left ? nt : left) * wt;
     };
     u64 N = 0, tb = 0, nt;
-    for (int i0 = 0; i0 < sel.nch; i0 += 64) N += wave_total(chunk_mass(i0, tb, nt));
+    for (int i0 = 0; i0 < sel.nch; i0 += 64) N += wave_sum(chunk_mass(i0, tb, nt));
     u64 at = (u64)((double)p.u * (double)N);
     if (at >= N) at = N - 1;
     u64 before = 0;
@@ -571,7 +565,7 @@ struct RowDraw {
           }
           slot_fence();
         });
-        s = wave_total(s);
+        s = wave_sum(s);
         t = wave_sum(t);
       }
       if (lane == 0) {

@@ -6,26 +6,6 @@
 
 namespace cis {
 
-__device__ __forceinline__ double row16_sum(double x) {
-  auto step = [](double x, auto ctrl) {
-    constexpr int C = ctrl;
-    const u64 b = __builtin_bit_cast(u64, x);
-    const uint32_t lo = (uint32_t)__builtin_amdgcn_update_dpp(0, (int)(uint32_t)b, C, 0xF, 0xF, false);
-    const uint32_t hi = (uint32_t)__builtin_amdgcn_update_dpp(0, (int)(b >> 32), C, 0xF, 0xF, false);
-    return x + __builtin_bit_cast(double, ((u64)hi << 32) | lo);
-  };
-  x = step(x, std::integral_constant<int, kDppXor1>{});
-  x = step(x, std::integral_constant<int, kDppXor2>{});
-  x = step(x, std::integral_constant<int, kDppHalfMirror>{});
-  return step(x, std::integral_constant<int, kDppRowMirror>{});
-}
-__device__ __forceinline__ double lane_double(double x, int lane) {
-  const u64 b = __builtin_bit_cast(u64, x);
-  const uint32_t lo = (uint32_t)__builtin_amdgcn_readlane((int)(uint32_t)b, lane);
-  const uint32_t hi = (uint32_t)__builtin_amdgcn_readlane((int)(b >> 32), lane);
-  return __builtin_bit_cast(double, ((u64)hi << 32) | lo);
-}
-
 // The logits' format as whole numbers.
 template <class E>
 using elem_t = std::conditional_t<E::kPerVec == 8, uint16_t, uint32_t>;

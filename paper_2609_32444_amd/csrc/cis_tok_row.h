@@ -58,11 +58,41 @@ __device__ __forceinline__ float vec_sum(const float (&f)[E::kPerVec], float c, 
 // The reference of a sum whose largest logit is m: finite where there is nothing but -inf.
 __device__ __forceinline__ float sum_ref(float m) { return fmaxf(m, -FLT_MAX); }
 
+// Sums over a wave, in every lane: within rows of 16 lanes by permutations, then over the four rows.
+template <class T, class F>
+__device__ __forceinline__ T wave_reduce(T x, F&& step) {
+  x += step(x, std::integral_constant<int, kDppXor1>{});
+  x += step(x, std::integral_constant<int, kDppXor2>{});
+  x += step(x, std::integral_constant<int, kDppHalfMirror>{});
+  return x + step(x, std::integral_constant<int, kDppRowMirror>{});
+}
+template <int CTRL>
+__device__ __forceinline__ uint32_t dpp_word(uint32_t x) {
+  return (uint32_t)__builtin_amdgcn_update_dpp(0, (int)x, CTRL, 0xF, 0xF, false);
+}
+__device__ __forceinline__ uint32_t lane_word(uint32_t x, int lane) {
+  return (uint32_t)__builtin_amdgcn_readlane((int)x, lane);
+}
 template <class T>
 __device__ __forceinline__ T wave_sum(T x) {
-#pragma unroll
-  for (int off = 32; off >= 1; off >>= 1) x += __shfl_xor(x, off, 64);
-  return x;
+  if constexpr (sizeof(T) == 4) {
+    x = wave_reduce(x, [](T y, auto ctrl) {
+      return __builtin_bit_cast(T, dpp_word<ctrl>(__builtin_bit_cast(uint32_t, y)));
+    });
+    auto at = [&](int l) { return __builtin_bit_cast(T, lane_word(__builtin_bit_cast(uint32_t, x), l)); };
+    return (at(0) + at(16)) + (at(32) + at(48));
+  } else {
+    auto both = [](T y, auto&& f) {
+      const u64 b = __builtin_bit_cast(u64, y);
+      return __builtin_bit_cast(T, ((u64)f((uint32_t)(b >> 32)) << 32) | f((uint32_t)b));
+    };
+    x = wave_reduce(x, [&](T y, auto ctrl) {
+      constexpr int C = ctrl;
+      return both(y, [](uint32_t w) { return dpp_word<C>(w); });
+    });
+    auto at = [&](int l) { return both(x, [l](uint32_t w) { return lane_word(w, l); }); };
+    return (at(0) + at(16)) + (at(32) + at(48));
+  }
 }
 __device__ __forceinline__ float wave_max(float x) {
   const float m = row16_max(x);

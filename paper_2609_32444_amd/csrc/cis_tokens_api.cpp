@@ -30,6 +30,23 @@ int device_cus() {
   return cus[dev];
 }
 
+// Workgroups of a kernel that a compute unit holds at once. (The devices are all gfx950.)
+int blocks_per_cu(const void* fn, int block) {
+  static std::mutex mu;
+  static struct {
+    const void* fn;
+    int n;
+  } seen[64];
+  static int count = 0;
+  std::lock_guard<std::mutex> lk(mu);
+  for (int i = 0; i < count; ++i)
+    if (seen[i].fn == fn) return seen[i].n;
+  int n = 0;
+  if (hipOccupancyMaxActiveBlocksPerMultiprocessor(&n, fn, block, 0) != hipSuccess || n < 1) n = 1;
+  if (count < 64) seen[count++] = {fn, n};
+  return n;
+}
+
 bool aligned(const void* p, size_t a) { return ((uintptr_t)p % a) == 0; }
 bool known(int dtype) { return dtype == CIS_BF16 || dtype == CIS_F32; }
 int elem_bytes(int dtype) { return dtype == CIS_BF16 ? 2 : 4; }
@@ -168,7 +185,7 @@ bool few_rows(int64_t T, int32_t nvec) {
 }
 
 int launch_distill(const DistillCall& c, const DistillLayout& D, char* base, cis::DistillArgs& a,
-                   hipStream_t stream) {
+                   int cus, hipStream_t stream) {
   auto by_rows = [&](const void* fn, int block, int64_t n) {
     for (a.row0 = 0; a.row0 < n; a.row0 += kMaxRows)
       if (int rc = launch(fn, n - a.row0 < kMaxRows ? n - a.row0 : kMaxRows, block, &a, stream))
@@ -177,7 +194,8 @@ int launch_distill(const DistillCall& c, const DistillLayout& D, char* base, cis
   };
   if (c.bwd && !few_rows(c.T, a.r.nvec)) {
     const cis::DistillVariant v = cis::distill_fused(c.dtype, a.r.nvec, c.K);
-    return by_rows(v.fn, v.block, c.T);
+    const int64_t resident = (int64_t)blocks_per_cu(v.fn, v.block) * cus;
+    return launch(v.fn, c.T < resident ? c.T : resident, v.block, &a, stream);
   }
   a.s = scan_at(base + D.scan_off, D.scan);
   a.rest = reinterpret_cast<cis::RestGrad*>(base + D.rest);
@@ -215,7 +233,8 @@ int run_distill(const DistillCall& c, hipStream_t stream) {
       if (a0 == b0 ? c.ld_g != c.ld : a0 < b1 && b0 < a1) return CIS_ERR_ALIAS;
     }
   }
-  if (const int cus = device_cus(); cus < 0) return cus;
+  const int cus = device_cus();
+  if (cus < 0) return cus;
 
   char* base = static_cast<char*>(c.workspace);
   const DistillLayout D = distill_layout(c.T, c.V, c.K, c.dtype);
@@ -240,7 +259,7 @@ int run_distill(const DistillCall& c, hipStream_t stream) {
     a.logk_ws = reinterpret_cast<float*>(base + L.logk);
     a.excess_ws = reinterpret_cast<float*>(base + L.excess);
     a.c = cis::scan_c(p.temperature);
-    if (int rc = launch_distill(c, D, base, a, stream)) return rc;
+    if (int rc = launch_distill(c, D, base, a, cus, stream)) return rc;
   }
   return launch_finalize(base, L, c.T, c.loss, stream);
 }

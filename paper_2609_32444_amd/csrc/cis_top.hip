@@ -43,8 +43,7 @@ __global__ __launch_bounds__(kScanBlock) void cis_scan_kernel(const ScanArgs a) 
       s += (double)vec_sum<E>(f, a.c, ref);
       slot_fence();
     });
-    s = row16_sum(s);
-    s = (lane_double(s, 0) + lane_double(s, 16)) + (lane_double(s, 32) + lane_double(s, 48));
+    s = wave_sum(s);
     if (lane == 0) {
       a.s.cmax[w] = m;
       a.s.csum[w] = s;
