@@ -70,7 +70,7 @@ template <int KMAX>
 struct ListShared {
   int32_t id[KMAX];       // -1: no entry
   float z[KMAX];          // the student's logits
-  float lq[KMAX];         // log q
+  float lq[KMAX];         // the teacher's logits; from teacher_list() on log q
   float q[KMAX];
   uint32_t grad[KMAX];    // gradient, in the logits' format
 };
@@ -93,18 +93,25 @@ __device__ __forceinline__ void each_entry(const int32_t* id, int K, int lane, F
     if (id[k] >= 0) f(k);
 }
 
+__device__ __forceinline__ float row_tail(const DistillArgs& a, int64_t row) {
+  return a.tail ? sload(a.tail + row) : -INFINITY;
+}
+__device__ __forceinline__ float row_weight(const DistillArgs& a, int64_t row) {
+  return a.weight ? sload(a.weight + row) : 1.f;
+}
+
 // log q of the listed tokens, and of the tail.
 template <int KMAX>
-__device__ __forceinline__ Teacher teacher_list(const DistillArgs& a, int64_t row,
+__device__ __forceinline__ Teacher teacher_list(const DistillArgs& a, float tail,
                                                 ListShared<KMAX>& sh, int lane) {
-  const float* values = a.values + row * a.ld_top;
-  const float c = a.c, tail = a.tail ? a.tail[row] * kLog2e : -INFINITY;
+  const float c = a.c;
+  tail *= kLog2e;
   float m = -INFINITY;
-  each_entry(sh.id, a.K, lane, [&](int k) { m = fmaxf(m, values[k]); });
+  each_entry(sh.id, a.K, lane, [&](int k) { m = fmaxf(m, sh.lq[k]); });
   const float R = fmaxf(fmaxf(wave_max(m) * c, tail), kMinExp);
   float s = 0.f;
   each_entry(sh.id, a.K, lane, [&](int k) {
-    const float x = __builtin_fmaf(values[k], c, -R);
+    const float x = __builtin_fmaf(sh.lq[k], c, -R);
     s += fast_exp2(x);
     sh.lq[k] = x;
   });
@@ -121,7 +128,7 @@ __device__ __forceinline__ Teacher teacher_list(const DistillArgs& a, int64_t ro
 // The loss of a row whose listed logits are at sh.z and whose other tokens sum up to rest 2^R, and with
 // BWD its gradient: of the listed tokens at sh.grad.
 template <class E, bool BWD, int KMAX>
-__device__ __forceinline__ Student student_list(const DistillArgs& a, int64_t row,
+__device__ __forceinline__ Student student_list(const DistillArgs& a, float weight,
                                                 ListShared<KMAX>& sh, int lane, const Teacher& t,
                                                 float R, float rest) {
   const float c = a.c;
@@ -151,7 +158,7 @@ __device__ __forceinline__ Student student_list(const DistillArgs& a, int64_t ro
   kl += reverse ? kl_part(p_rest, d_rest, t.q_rest) : kl_part(t.q_rest, -d_rest, p_rest);
   // (kl_part takes a NaN share for 0)
   if (!(total > 0.f && total < INFINITY) || !t.finite) kl = NAN;
-  const float w = a.scale * (a.weight ? a.weight[row] : 1.f);
+  const float w = a.scale * weight;
   Student out;
   out.term = w == 0.f ? 0.f : w * kl;
   out.finite = isfinite(kl) && isfinite(out.term);

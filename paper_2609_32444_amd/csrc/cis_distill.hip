@@ -22,6 +22,7 @@ struct FusedShared {
   float f[16], g[16];
   uint32_t u[16];
   RestGrad rest;
+  Teacher teacher;
 };
 
 // A barrier for what lies in LDS: loads of the row stay in flight across it.
@@ -32,7 +33,9 @@ __device__ __forceinline__ void lds_barrier() {
 template <class E, int BLOCK, int NV, int KMAX>
 __global__ __launch_bounds__(BLOCK) __attribute__((amdgpu_waves_per_eu(4))) void cis_distill_kernel(const DistillArgs a) {
   constexpr int NW = BLOCK / 64, EPV = E::kPerVec;
-  constexpr int FIRST = NV > 8 ? 8 : NV;   // vectors that are asked for before the list
+  // vectors that are asked for before the list, and stay in flight ahead of sweep 1 (16384 rows of
+  // V = 151936: 4 1981 us, 8 1902, 12 2056; 3001 of V = 50257: 142, 146, 153)
+  constexpr int MOST = BLOCK == 1024 ? 8 : 4, FIRST = NV > MOST ? MOST : NV;
   typedef FusedShared<BLOCK, KMAX> Shared;
   __shared__ Shared sh;
   for (int i = threadIdx.x; i < Shared::kTable; i += BLOCK) sh.head[i] = kNone;
@@ -41,8 +44,17 @@ __global__ __launch_bounds__(BLOCK) __attribute__((amdgpu_waves_per_eu(4))) void
   // not meet the same place of every response (padding is periodic).
   constexpr uint32_t kShift = 61;
   uint32_t place = blockIdx.x;
+  // a thread's first entry of the list is fetched a row ahead
   int32_t id0 = -1;
-  if ((int)threadIdx.x < a.K) id0 = a.ids[(int64_t)blockIdx.x * a.ld_top + threadIdx.x];
+  float value0 = 0.f;
+  auto fetch = [&](int64_t row, int tid) {
+    if (row < a.r.T && tid < a.K) {
+      id0 = a.ids[row * a.ld_top + tid];
+      value0 = a.values[row * a.ld_top + tid];
+    }
+  };
+  fetch(blockIdx.x, threadIdx.x);
+  bool old = false;   // the table holds the last row's list
   for (int64_t round = 0; round < a.r.T; round += gridDim.x) {
     const int64_t row = round + place;
     if (row >= a.r.T) break;   // (the last round)
@@ -66,12 +78,19 @@ __global__ __launch_bounds__(BLOCK) __attribute__((amdgpu_waves_per_eu(4))) void
       r[I] = bload(rs, (uint32_t)(I * BLOCK + tid) * 16u, 0u);
       slot_fence();
     });
+    const float tail = row_tail(a, row), weight = row_weight(a, row);
     // the table
     uint32_t seen = 0, wrong = 0;   // entries; ids out of range or repeated
-    lds_barrier();   // (the last row's is cleared)
+    lds_barrier();   // (nobody looks the last row's vectors up any more)
+    if (old)
+      for (int k = tid; k < K; k += BLOCK)
+        if (sh.list.id[k] >= 0) sh.head[(sh.list.id[k] / EPV) & (Shared::kTable - 1)] = kNone;
+    old = on;
+    lds_barrier();
     if (on)
       for (int k = tid; k < K; k += BLOCK) {
         const int32_t id = k < BLOCK ? id0 : a.ids[row * a.ld_top + k];
+        sh.list.lq[k] = k < BLOCK ? value0 : a.values[row * a.ld_top + k];
         const bool in = id >= 0 && id < V;
         sh.list.id[k] = in ? id : -1;
         sh.next[k] = kNone;
@@ -84,8 +103,6 @@ __global__ __launch_bounds__(BLOCK) __attribute__((amdgpu_waves_per_eu(4))) void
         wrong |= in || id == -1 ? 0u : 1u;
       }
     lds_barrier();
-    id0 = -1;
-    if (next < a.r.T && tid < K) id0 = a.ids[next * a.ld_top + tid];
     if (on)
       for (int k = tid; k < K; k += BLOCK)
         if (sh.list.id[k] >= 0)
@@ -96,10 +113,6 @@ __global__ __launch_bounds__(BLOCK) __attribute__((amdgpu_waves_per_eu(4))) void
       const uint32_t any = (__ballot(seen) ? 1u : 0u) | (__ballot(wrong) ? 2u : 0u);
       if (lane == 0) sh.u[wid] = any;
     }
-    static_for<NV - FIRST>([&](auto I) {
-      r[FIRST + I] = bload(rs, (uint32_t)((FIRST + I) * BLOCK + tid) * 16u, 0u);
-      slot_fence();
-    });
     lds_barrier();
     uint32_t any = 0;
     for (int w = 0; w < NW; ++w) any |= sh.u[w];
@@ -135,14 +148,21 @@ __global__ __launch_bounds__(BLOCK) __attribute__((amdgpu_waves_per_eu(4))) void
       s = s * fast_exp2(R - Rn) + part;
       R = Rn;
     };
-    Teacher teacher{};
-    if (valid) {
-      if (wid == 0) teacher = teacher_list(a, row, sh.list, lane);
-      static_for<NV>([&](auto I) {
-        if (I * BLOCK < nvec)
-          fold(I * BLOCK + tid, r[I], mine >> I & 1, (I + 1) * BLOCK * EPV > V);
+    if (valid && wid == 0) {
+      const Teacher t = teacher_list(a, tail, sh.list, lane);
+      if (lane == 0) sh.teacher = t;   // (rather than in every thread's registers)
+    }
+    // (a row that does not count has no records: nothing is read)
+    static_for<NV>([&](auto I) {
+      if constexpr (I + FIRST < NV) {
+        r[I + FIRST] = bload(rs, (uint32_t)((I + FIRST) * BLOCK + tid) * 16u, 0u);
         slot_fence();
-      });
+      }
+      if (valid && I * BLOCK < nvec)
+        fold(I * BLOCK + tid, r[I], mine >> I & 1, (I + 1) * BLOCK * EPV > V);
+      slot_fence();
+    });
+    if (valid) {
       for (int v = NV * BLOCK + tid; v < nvec; v += BLOCK)
         fold(v, bload_aux<kAuxStream1>(rs, (uint32_t)v * 16u), true, (v + 1) * EPV > V);
       wave_lse(R, s);
@@ -158,7 +178,7 @@ __global__ __launch_bounds__(BLOCK) __attribute__((amdgpu_waves_per_eu(4))) void
         R = lane < NW ? sh.f[lane] : kMinExp;
         s = lane < NW ? sh.g[lane] : 0.f;
         wave_lse(R, s);
-        st = student_list<E, true>(a, row, sh.list, lane, teacher, R, s);
+        st = student_list<E, true>(a, weight, sh.list, lane, sh.teacher, R, s);
       }
       if (lane == 0) {
         put_row(a, row, st.term, valid, on && bad, st.finite);
@@ -169,6 +189,7 @@ __global__ __launch_bounds__(BLOCK) __attribute__((amdgpu_waves_per_eu(4))) void
     // sweep 2
     const RestGrad g = sh.rest;
     opaque(r);
+    fetch(next, tid);
     void* grow = (char*)a.dlogits + row * a.grow_bytes;
     const bool ragged = V % EPV != 0;
     const __amdgpu_buffer_rsrc_t ws = make_rsrc(grow, (uint32_t)(nvec - (ragged ? 1 : 0)) * 16u);
@@ -189,10 +210,6 @@ __global__ __launch_bounds__(BLOCK) __attribute__((amdgpu_waves_per_eu(4))) void
     for (int v = NV * BLOCK + tid; v < nvec; v += BLOCK)
       put(v, bload_aux<kAuxStream2>(rs, (uint32_t)v * 16u), true, true);
     sh.mine[tid] = 0;
-    lds_barrier();   // nobody looks a vector up any more
-    if (on)
-      for (int k = tid; k < K; k += BLOCK)
-        if (sh.list.id[k] >= 0) sh.head[(sh.list.id[k] / EPV) & (Shared::kTable - 1)] = kNone;
   }
 }
 
@@ -231,6 +248,7 @@ __global__ __launch_bounds__(64) void cis_distill_row_kernel(const DistillArgs a
   if (on)
     for (int k = lane; k < K; k += 64) {
       const int32_t id = a.ids[row * a.ld_top + k];
+      sh.list.lq[k] = a.values[row * a.ld_top + k];
       const bool in = id >= 0 && id < V;
       sh.list.id[k] = in ? id : -1;
       if (in) {
@@ -310,8 +328,8 @@ __global__ __launch_bounds__(64) void cis_distill_row_kernel(const DistillArgs a
       }
       wave_lse(R, s);
     }
-    const Teacher t = teacher_list(a, row, sh.list, lane);
-    st = student_list<E, BWD>(a, row, sh.list, lane, t, R, s);
+    const Teacher t = teacher_list(a, row_tail(a, row), sh.list, lane);
+    st = student_list<E, BWD>(a, row_weight(a, row), sh.list, lane, t, R, s);
   }
   if (lane == 0) put_row(a, row, st.term, valid, on && bad, st.finite);
   if (BWD) {
@@ -374,9 +392,9 @@ struct FusedVariant {
         (const void*)&cis_distill_kernel<E, B, N, CIS_TOP_MAX_K>   \
   }
 #define CIS_FUSED_TABLE(E)                                                                   \
-  {CIS_FUSED(E, 64, 5),   CIS_FUSED(E, 64, 10),  CIS_FUSED(E, 64, 18),   CIS_FUSED(E, 256, 8), \
-   CIS_FUSED(E, 256, 16), CIS_FUSED(E, 512, 12), CIS_FUSED(E, 512, 17), CIS_FUSED(E, 1024, 12), \
-   CIS_FUSED(E, 1024, 19)}
+  {CIS_FUSED(E, 64, 5),    CIS_FUSED(E, 64, 10),   CIS_FUSED(E, 64, 18),  CIS_FUSED(E, 256, 8),  \
+   CIS_FUSED(E, 256, 12),  CIS_FUSED(E, 256, 16),  CIS_FUSED(E, 512, 10), CIS_FUSED(E, 512, 13), \
+   CIS_FUSED(E, 512, 17),  CIS_FUSED(E, 1024, 12), CIS_FUSED(E, 1024, 15), CIS_FUSED(E, 1024, 19)}
 static const FusedVariant kFusedBf16[] = CIS_FUSED_TABLE(Bf16);
 static const FusedVariant kFusedF32[] = CIS_FUSED_TABLE(F32);
 
