@@ -5,8 +5,10 @@
 //     cuts and the draw run on that list.
 //   * nothing but min_p cuts: the weights' sums by chunks (cis_weigh_kernel), the chunk that the
 //     random number falls into, and the token within it.
-//   * top_p: the same sums give the target; if the collected candidates reach it, the list decides.
-//   * otherwise a histogram of the weights' exponents over the row narrows the cut down to one step of
+//   * top_p without a count: a histogram of the weights over the whole row (cis_hist_kernel) gives the
+//     target and the step of 1/64 octave that the cut falls into; cis_weigh_kernel sums up what lies
+//     above it and lists the step's tokens, which are put in order here.
+//   * otherwise (top_k beyond kDrawK, or a step of more tokens than a list holds) a histogram of the weights' exponents over the row narrows the cut down to one step of
 //     1/64 octave, whose tokens are sorted; then the sums by chunks of what is kept. Where a
 //     step overflows the list (many equal logits), the cut is found byte by byte (radix_cut).
 #include "cis_select.h"
@@ -40,64 +42,194 @@ __device__ __forceinline__ RowParams row_params(const SampleArgs& a, int64_t row
   p.least_w = (uint32_t)ceil((double)p.min_p * kDrawOne);
   return p;
 }
-// Rows that cis_weigh_kernel sums up: those that no count cuts.
-__device__ __forceinline__ bool row_weighed(const RowParams& p, int V) {
-  return p.ok && !p.counted && p.top_k == V;
+// Rows that cis_weigh_kernel sums up: those that no count cuts. (The draw adds up the kept part of
+// a step by chunks at WideShared::mass.)
+__device__ __forceinline__ bool row_stepped(const RowParams& p, const SampleArgs& a) {
+  return p.ok && !p.counted && p.top_k == a.r.V && p.top_p < 1.f && a.s.nch <= kFineSteps;
+}
+__device__ __forceinline__ bool row_weighed(const RowParams& p, const SampleArgs& a) {
+  return row_stepped(p, a) || (p.ok && !p.counted && p.top_k == a.r.V && p.top_p == 1.f);
 }
 
-// Weights of a vector, at least `least_w` or 0; their sum stays below 2^32.
-template <class E>
-__device__ __forceinline__ uint32_t vec_weight(const float (&f)[E::kPerVec], float M, float c,
-                                               uint32_t least_w) {
-  uint32_t s = 0;
+// A logit's exponent, and the step of the histogram of weights that it falls into: steps rise as
+// logits fall; kFineSteps: no weight.
+__device__ __forceinline__ float draw_exponent(float f, float M, float c) { return (f - M) * c; }
+__device__ __forceinline__ int draw_step(float e) {
+  const float t = e * -(float)kFine;
+  return t < (float)kFineSteps ? (int)t : kFineSteps;
+}
+__device__ __forceinline__ uint32_t exponent_weight(float e) {
+  return (uint32_t)(fast_exp2(e) * (float)kDrawOne);
+}
+// A row's largest logit, by one wave. (-inf: no token.)
+__device__ __forceinline__ float row_max(const float* cmax, int nch, int lane) {
+  float M = -INFINITY;
+  for (int i = lane; i < nch; i += 64) M = fmaxf(M, cmax[i]);
+  return wave_max(M);
+}
+
+// The first step at which the sum of mass[] reaches top_p of the whole, by one wave.
+__device__ __forceinline__ DrawStep step_of_cut(const u64* mass, float top_p, int lane) {
+  constexpr int S = kFineSteps / 64;
+  static_assert(kFineSteps % 64 == 0 && S <= 64, "a lane has the same number of steps");
+  u64 s = 0;
 #pragma unroll
-  for (int e = 0; e < E::kPerVec; ++e) {
-    const uint32_t w = draw_weight(f[e], M, c);
-    s += w >= least_w ? w : 0u;
-  }
-  return s;
+  for (int i = 0; i < S; ++i) s += mass[lane * S + i];
+  const u64 upto = wave_scan(s, lane), total = __shfl(upto, 63, 64);
+  const u64 want = (u64)ceil((double)top_p * (double)total);
+  const u64 who = __ballot(upto >= want);
+  DrawStep d{0, kFineSteps, 0};
+  if (total == 0) return d;   // (a row without weights)
+  const int at = __ffsll(who) - 1;   // the first lane that reaches it has the step
+  const u64 before = __shfl(upto - s, at, 64);
+  const u64 m = lane < S ? mass[at * S + lane] : 0, to = before + wave_scan(m, lane);
+  const int in = __ffsll((u64)__ballot(to >= want)) - 1;
+  d.step = at * S + in;
+  d.left = want - __shfl(to - m, in, 64);
+  return d;
 }
 
 // ------------------------------------------------------------------------------------------
-// One wave per chunk: the sum of its weights. A chunk whose largest logit has no weight is not read.
+// The histogram of a row's weights by their exponents, in a part of the row's chunks per workgroup:
+// whole numbers in LDS, so that the order of the additions is of no account. Where a row has one
+// workgroup, the step of its cut too.
+// ------------------------------------------------------------------------------------------
+template <class E>
+__global__ __launch_bounds__(kHistBlock) void cis_hist_kernel(const SampleArgs a) {
+  constexpr int NW = kHistBlock / 64, EPV = E::kPerVec;
+  __shared__ u64 mass[kFineSteps];
+  const int tid = threadIdx.x, lane = tid & 63,
+            wid = __builtin_amdgcn_readfirstlane(threadIdx.x) >> 6;
+  const int64_t at = blockIdx.x / a.parts, row = a.row0 + at;
+  const int part = (int)(blockIdx.x - at * a.parts), nch = a.s.nch;
+  const RowParams p = row_params(a, row);
+  if (!row_stepped(p, a)) return;
+  for (int i = tid; i < kFineSteps; i += kHistBlock) mass[i] = 0;
+  const float* cmax = a.s.cmax + row * nch;
+  const float M = row_max(cmax, nch, lane);
+  const __amdgpu_buffer_rsrc_t rs = tok_rsrc(a.r, row);
+  __syncthreads();
+  for (int ch = part * NW + wid; ch < nch; ch += a.parts * NW) {
+    if (!(draw_exponent(cmax[ch], M, p.c) >= -28.f)) continue;
+    u32x4 x[kScanSlots];
+    load_chunk<E, 0>(rs, a.r, ch, lane, x);
+    static_for<kScanSlots>([&](auto I) {
+      float f[EPV];
+      E::unpack(x[I], f);
+#pragma unroll
+      for (int e = 0; e < EPV; ++e) {
+        const float t = draw_exponent(f[e], M, p.c);
+        const int st = draw_step(t);
+        if (st < kFineSteps) atomicAdd(&mass[st], (u64)exponent_weight(t));
+      }
+      slot_fence();
+    });
+  }
+  __syncthreads();
+  if (a.parts == 1) {
+    if (tid < 64) {
+      const DrawStep d = step_of_cut(mass, p.top_p, lane);
+      if (lane == 0) a.steps[at] = d;
+    }
+  } else {
+    u64* out = a.hist + (int64_t)blockIdx.x * kFineSteps;
+    for (int i = tid; i < kFineSteps; i += kHistBlock) out[i] = mass[i];
+  }
+}
+
+// The step of a row's cut from its parts' histograms.
+__global__ __launch_bounds__(kHistBlock) void cis_step_kernel(const SampleArgs a) {
+  __shared__ u64 mass[kFineSteps];
+  const int64_t at = blockIdx.x, row = a.row0 + at;
+  const RowParams p = row_params(a, row);
+  if (!row_stepped(p, a)) return;
+  const u64* in = a.hist + at * a.parts * kFineSteps;
+  for (int i = threadIdx.x; i < kFineSteps; i += kHistBlock) {
+    u64 s = 0;
+#pragma unroll 4
+    for (int k = 0; k < a.parts; ++k) s += in[k * kFineSteps + i];
+    mass[i] = s;
+  }
+  __syncthreads();
+  if (threadIdx.x < 64) {
+    const DrawStep d = step_of_cut(mass, p.top_p, threadIdx.x);
+    if (threadIdx.x == 0) a.steps[at] = d;
+  }
+}
+
+// ------------------------------------------------------------------------------------------
+// One wave per chunk: the sum of its weights, of a row that top_p cuts those above the step of the
+// cut, whose tokens are listed. A chunk whose largest logit does not reach that far is not read.
 // ------------------------------------------------------------------------------------------
 template <class E>
 __global__ __launch_bounds__(kWeighBlock) void cis_weigh_kernel(const SampleArgs a) {
   constexpr int NW = kWeighBlock / 64, EPV = E::kPerVec;
   const int lane = threadIdx.x & 63, wid = __builtin_amdgcn_readfirstlane(threadIdx.x) >> 6;
   const int nch = a.s.nch;
-  const int64_t total = a.r.T * (int64_t)nch;
+  const int64_t total = a.rows * (int64_t)nch;
   for (int64_t w = (int64_t)blockIdx.x * NW + wid; w < total; w += (int64_t)gridDim.x * NW) {
-    const int64_t row = w / nch;
-    const int ch = (int)(w - row * nch);
+    const int64_t at = w / nch, row = a.row0 + at;
+    const int ch = (int)(w - at * nch);
     const RowParams p = row_params(a, row);
-    if (!row_weighed(p, a.r.V)) continue;
-    u32x4 x[kScanSlots];
-    load_chunk<E, 0>(tok_rsrc(a.r, row), a.r, ch, lane, x);
+    if (!row_weighed(p, a)) continue;
     const float* cmax = a.s.cmax + row * nch;
-    float M = -INFINITY;
-    for (int i = lane; i < nch; i += 64) M = fmaxf(M, cmax[i]);
-    M = wave_max(M);
+    const float M = row_max(cmax, nch, lane), top = draw_exponent(cmax[ch], M, p.c);
+    const int step = p.top_p < 1.f ? sload(&a.steps[at].step) : kFineSteps;
     u64 s = 0;
-    if ((cmax[ch] - M) * p.c >= -28.f) {
-      const uint32_t least = p.top_p < 1.f ? 0u : p.least_w;   // (top_p counts every weight)
+    if (top >= -28.f && draw_step(top) <= step) {
+      u32x4 x[kScanSlots];
+      load_chunk<E, 0>(tok_rsrc(a.r, row), a.r, ch, lane, x);
+      uint32_t mine = 0;
+      // exponents above the step, and in it (multiples of 1 / kFine: exact)
+      const float above = step * (-1.f / kFine), within = (step + 1) * (-1.f / kFine);
+      const bool every = step == kFineSteps && p.least_w == 0;
       static_for<kScanSlots>([&](auto I) {
         float f[EPV];
         E::unpack(x[I], f);
-        s += vec_weight<E>(f, M, p.c, least);
+        uint32_t vs = 0;   // (8 weights stay below 2^32)
+        if (every) {
+#pragma unroll
+          for (int e = 0; e < EPV; ++e) vs += draw_weight(f[e], M, p.c);
+        } else {
+#pragma unroll
+          for (int e = 0; e < EPV; ++e) {
+            const float t = draw_exponent(f[e], M, p.c);
+            const uint32_t q = exponent_weight(t);
+            vs += t > above && q >= p.least_w ? q : 0u;
+            mine += t > within && t <= above ? 1 : 0;
+          }
+        }
+        s += vs;
         slot_fence();
       });
       s = wave_sum(s);
+      if (step < kFineSteps && __ballot(mine != 0)) {
+        const uint32_t upto = wave_scan(mine, lane);
+        uint32_t to = 0;
+        if (lane == 63) to = atomicAdd(&a.steps[at].count, upto);
+        to = __builtin_amdgcn_readlane(to, 63) + upto - mine;
+        uint32_t* ids = a.step_ids + at * a.step_ld;
+        static_for<kScanSlots>([&](auto I) {
+          float f[EPV];
+          E::unpack(x[I], f);
+#pragma unroll
+          for (int e = 0; e < EPV; ++e)
+            if (const float t = draw_exponent(f[e], M, p.c); t > within && t <= above) {
+              if (to < (uint32_t)a.step_ld)
+                ids[to] = (uint32_t)((ch * kScanVecs + I * 64 + lane) * EPV + e);
+              ++to;
+            }
+          slot_fence();
+        });
+      }
     }
-    if (lane == 0) a.draw[w] = s;
+    if (lane == 0) a.draw[row * nch + ch] = s;
   }
 }
 
 // ------------------------------------------------------------------------------------------
 // The draw.
 // ------------------------------------------------------------------------------------------
-constexpr int kFine = 64;                  // histogram steps per octave
-constexpr int kFineSteps = 29 * kFine;     // (a weight's exponent is at least -28, or it is 0)
 struct WideShared {
   u64 mass[kFineSteps];
   uint32_t count[kFineSteps];
@@ -359,10 +491,8 @@ struct RowDraw {
     });
   }
 
-  // The step of the histogram of weights that a logit falls into; kFineSteps: it has no weight.
   __device__ __forceinline__ int fine_step(float f) const {
-    const float t = (sel.M - f) * p.c * (float)kFine;
-    return t < (float)kFineSteps ? (int)t : kFineSteps;
+    return draw_step(draw_exponent(f, sel.M, p.c));
   }
 
   // f(logits, vector) for the row's chunks that hold a weight, whole waves together.
@@ -577,6 +707,115 @@ struct RowDraw {
     from_chunks(cut, ties, p.least_w);
   }
 
+  // Draws a row whose cut falls into a step: the step's kept tokens join the chunks' sums above it.
+  // False where the list does not hold the step.
+  __device__ __forceinline__ bool from_step(WideShared& ws) {
+    const int tid = threadIdx.x, lane = tid & 63, wid = tid >> 6;
+    constexpr int PT = LIST / BLOCK;
+    const int64_t at = row - a.row0;
+    const uint32_t n_step = a.steps[at].count;
+    const u64 left = a.steps[at].left;
+    if (n_step > (uint32_t)a.step_ld || n_step > LIST) return false;
+    const int count = (int)n_step, step = a.steps[at].step;
+    const uint32_t* ids = a.step_ids + at * a.step_ld;
+    for (int i = tid; i < count; i += BLOCK) {
+      const int id = (int)ids[i];
+      float f[EPV], fy = 0.f;
+      tok_vec<E>(sel.rs, id / EPV, sel.V, f);
+#pragma unroll
+      for (int e = 0; e < EPV; ++e) fy = id % EPV == e ? f[e] : fy;
+      sh.list[i] = token_of(fy, id);
+    }
+    for (int i = tid; i < sel.nch; i += BLOCK) ws.mass[i] = a.draw[row * sel.nch + i];
+    __syncthreads();
+    sort_list<BLOCK>(sh.list, count);
+    // the first tokens that reach `left`, of min_p's weight at least
+    u64 s = 0;
+    for (int j = 0; j < PT && tid * PT + j < count; ++j)
+      s += weight(token_value(sh.list[tid * PT + j]));
+    u64 b = wave_scan(s, lane);
+    if (lane == 63) sh.u[wid] = b;
+    __syncthreads();
+    b -= s;
+    for (int w = 0; w < wid; ++w) b += sh.u[w];
+    u64 keep = 0;
+    for (int j = 0; j < PT && tid * PT + j < count; ++j) {
+      const uint32_t q = weight(token_value(sh.list[tid * PT + j]));
+      if (b < left && q >= p.least_w) {
+        ++keep;
+        atomicAdd(&ws.mass[token_id(sh.list[tid * PT + j]) / (EPV * kScanVecs)], (u64)q);
+      }
+      b += q;
+    }
+    __syncthreads();
+    keep = block_sum<NW>(keep, sh.u);
+    if (tid >= 64) return true;
+    const u64 last = keep > 0 ? sh.list[keep - 1] : ~u64(0);
+    u64 N = 0;
+    for (int i = lane; i < sel.nch; i += 64) N += ws.mass[i];
+    N = wave_sum(N);
+    u64 to = (u64)((double)p.u * (double)N);
+    if (to >= N) to = N - 1;
+    u64 before = 0;
+    int ch = 0;
+    for (int i0 = 0; i0 < sel.nch; i0 += 64) {
+      const u64 m = i0 + lane < sel.nch ? ws.mass[i0 + lane] : 0, upto = before + wave_scan(m, lane);
+      const u64 hit = __ballot(upto > to);
+      if (hit) {
+        const int who = __ffsll(hit) - 1;
+        ch = i0 + who;
+        before = __shfl(upto - m, who, 64);
+        break;
+      }
+      before = __shfl(upto, 63, 64);
+    }
+    in_chunk(ch, before, to, N, [&](float f, int id) {
+      const float t = draw_exponent(f, sel.M, p.c);
+      const int st = draw_step(t);
+      const uint32_t q = exponent_weight(t);
+      const bool in = st < step ? q >= p.least_w : st == step && token_of(f, id) >= last;
+      return in ? q : 0u;
+    });
+    return true;
+  }
+
+  // Draws within chunk ch, whose weights are kept(logit, id), `before` them all; by one wave.
+  template <class W>
+  __device__ __forceinline__ void in_chunk(int ch, u64 before, u64 to, u64 N, W&& kept) const {
+    const int lane = threadIdx.x & 63;
+    u32x4 x[kScanSlots];
+    load_chunk<E, 0>(sel.rs, a.r, ch, lane, x);
+    bool done = false;
+    static_for<kScanSlots>([&](auto I) {
+      if (done) return;
+      float f[EPV];
+      E::unpack(x[I], f);
+      const int v = ch * kScanVecs + I * 64 + lane;
+      uint32_t w[EPV], sum = 0;   // (8 weights stay below 2^32)
+#pragma unroll
+      for (int e = 0; e < EPV; ++e) sum += w[e] = kept(f[e], v * EPV + e);
+      const u64 upto = before + wave_scan((u64)sum, lane);
+      const u64 hit = __ballot(upto > to);
+      if (hit) {
+        if (lane == __ffsll(hit) - 1) {
+          u64 b = upto - sum;
+          bool found = false;
+#pragma unroll
+          for (int e = 0; e < EPV; ++e) {
+            if (!found && b + w[e] > to) {
+              found = true;
+              put_row(v * EPV + e, f[e], w[e], N);
+            }
+            b += w[e];
+          }
+        }
+        done = true;
+      }
+      before = __shfl(upto, 63, 64);
+      slot_fence();
+    });
+  }
+
   __device__ __forceinline__ void run(WideShared* ws) {
     const int tid = threadIdx.x;
     sum_rest();
@@ -595,25 +834,7 @@ struct RowDraw {
         return;
       }
       if constexpr (WIDE) {
-        u64 sum = 0;
-        for (int i = tid; i < sel.nch; i += BLOCK) sum += a.draw[row * sel.nch + i];
-        __syncthreads();
-        sum = block_sum<NW>(sum, sh.u);
-        const u64 want = (u64)ceil((double)p.top_p * (double)sum);
-        for (int n = 64; n <= kDrawK; n *= 16) {
-          __syncthreads();
-          if (!sel.collect(n)) break;
-          u64 s = 0;
-          for (int i = tid; i < sel.count; i += BLOCK) s += weight(token_value(sh.list[i]));
-          s = block_sum<NW>(s, sh.u);
-          __syncthreads();
-          if (s >= want) {
-            sel.order(LIST);
-            from_list(sel.count, want);
-            return;
-          }
-          if (sel.bin == 256) break;
-        }
+        if (row_stepped(p, a) && from_step(*ws)) return;
       }
     }
     if constexpr (WIDE) {
@@ -654,7 +875,7 @@ __global__ __launch_bounds__(BLOCK) __attribute__((amdgpu_waves_per_eu(4))) void
   __shared__ std::conditional_t<WIDE, WideShared, uint32_t> ws;
   const int64_t row = a.row0 + blockIdx.x;
   const RowParams p = row_params(a, row);
-  RowSelect<E, BLOCK, LIST> sel(sh, a.r, a.s, row, p.ok);
+  RowSelect<E, BLOCK, LIST> sel(sh, a.r, a.s, row, p.ok, p.counted);
   if (!p.ok || !sel.tokens()) {
     if (threadIdx.x == 0) {
       a.ids[row] = -1;
@@ -674,6 +895,11 @@ const void* weigh_kernel(int dtype) {
   return dtype == CIS_BF16 ? (const void*)&cis_weigh_kernel<Bf16>
                            : (const void*)&cis_weigh_kernel<F32>;
 }
+const void* hist_kernel(int dtype) {
+  return dtype == CIS_BF16 ? (const void*)&cis_hist_kernel<Bf16>
+                           : (const void*)&cis_hist_kernel<F32>;
+}
+const void* step_kernel() { return (const void*)&cis_step_kernel; }
 const void* sample_kernel(int dtype, bool wide) {
   if (dtype == CIS_BF16)
     return wide ? (const void*)&cis_sample_kernel<Bf16, kTokBlock, 8192, true>

@@ -105,14 +105,14 @@ struct RowSelect {
   int count;        // logits in the list
 
   __device__ __forceinline__ RowSelect(SelectShared<LIST>& s, const TokRows& r, const TokScan& t,
-                                       int64_t row, bool on)
+                                       int64_t row, bool on, bool groups)
       : sh(s), rs(tok_rsrc(r, row)), V(r.V), nvec(r.nvec), ngrp(t.ngrp), gv(t.gv), nch(t.nch),
         gm((const elem_t<E>*)t.gmax + row * t.ngrp), cmax(t.cmax + row * t.nch),
         csum(t.csum + row * t.nch) {
     const int tid = threadIdx.x, lane = tid & 63, wid = tid >> 6;
     // the groups' largest logits, kept where a thread has few of them
     kept = ngrp <= kGroupRegs * BLOCK;
-    if (on && kept)
+    if (on && groups && kept)
       static_for<kGroupRegs>([&](auto I) {
         const int g = tid + I * BLOCK;
         gr[I] = I * BLOCK < ngrp && g < ngrp ? group_max(g) : -INFINITY;

@@ -63,12 +63,28 @@ struct ScanArgs {
   float c;         // log2(e) / temperature
 };
 
+// Where the running sum of a row's weights, in falling order of its logits, reaches top_p of the whole:
+// the step of the histogram of weights, what the step has to bring, and how many tokens it holds.
+struct DrawStep {
+  unsigned long long left;
+  int32_t step;      // kFineSteps: the row has no token
+  uint32_t count;
+};
+constexpr int kFine = 64;                  // histogram steps per octave
+constexpr int kFineSteps = 29 * kFine;     // (a weight's exponent is at least -28, or it is 0)
+constexpr int kHistBlock = 1024;
+constexpr int kStepTokens = 8192;          // tokens of its step that a row's list holds
+
 struct SampleArgs {
   TokRows r;
   TokScan s;                  // of the rows at temperature 1
-  unsigned long long* draw;                // [T, nch] the chunks' weights
+  unsigned long long* draw;   // [T, nch] the chunks' weights
   uint32_t* ties;             // [T, nch] their tokens of a cut's key
-  int64_t row0;               // the launch's first row
+  DrawStep* steps;            // [rows]
+  uint32_t* step_ids;         // [rows, step_ld] the tokens of the rows' steps
+  unsigned long long* hist;   // [rows, parts, kFineSteps] with parts > 1
+  int32_t step_ld, parts;
+  int64_t row0, rows;         // the launch's first row, and how many
   const float* u;
   cis_sample_params_t prm;
   const float* temperature;   // nullable, as the next three
@@ -131,6 +147,8 @@ const void* scan_kernel(int dtype, int32_t gv);
 // wide: any parameters; else top_k in [1, 128] for every row or nothing to cut but min_p
 const void* sample_kernel(int dtype, bool wide);
 const void* weigh_kernel(int dtype);
+const void* hist_kernel(int dtype);
+const void* step_kernel();
 const void* top_kernel(int dtype, int64_t K);
 int top_block(int64_t K);
 constexpr int kDistillGradBlock = 128, kDistillGradVecs = 1024;   // 16 KiB of logits per workgroup

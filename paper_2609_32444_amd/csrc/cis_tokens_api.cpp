@@ -93,16 +93,30 @@ constexpr int64_t kFewRows = 192;
 // Logits that a draw may have to look at where its parameters do not say.
 constexpr int64_t kManyLogits = 256;
 
+// Rows whose steps of a cut are listed at once, and workgroups that the histograms of few rows take.
+constexpr int64_t kStepRows = 2048;
+constexpr int64_t kHistBlocks = 256;
+
 struct SampleLayout {
   cis::ScanLayout scan;
-  size_t draw, ties, total;
+  size_t draw, ties, steps, step_ids, hist, total;
+  int32_t step_ld, parts;
 };
-SampleLayout sample_layout(int64_t T, int32_t nvec, int es, int32_t gv) {
+SampleLayout sample_layout(int64_t T, int64_t V, int32_t nvec, int es, int32_t gv) {
   SampleLayout L{};
   L.scan = cis::scan_layout(T, nvec, es, gv);
   L.draw = L.scan.total;
   L.ties = L.draw + cis::align_up((size_t)T * L.scan.nch * 8, 256);
-  L.total = L.ties + cis::align_up((size_t)T * L.scan.nch * 4, 256);
+  L.steps = L.ties + cis::align_up((size_t)T * L.scan.nch * 4, 256);
+  const int64_t rows = T < kStepRows ? T : kStepRows;
+  L.step_ld = (int32_t)(V < cis::kStepTokens ? V : cis::kStepTokens);
+  L.step_ids = L.steps + cis::align_up((size_t)rows * sizeof(cis::DrawStep), 256);
+  L.hist = L.step_ids + cis::align_up((size_t)rows * L.step_ld * 4, 256);
+  // a row's histogram by one workgroup, or in parts where there are few rows: of a chunk per wave
+  const int64_t most = (L.scan.nch + cis::kHistBlock / 64 - 1) / (cis::kHistBlock / 64),
+                fill = T > 0 ? kHistBlocks / T : 1;
+  L.parts = (int32_t)(fill < 1 ? 1 : fill < most ? fill : most);
+  L.total = L.hist + (L.parts > 1 ? (size_t)T * L.parts * cis::kFineSteps * 8 : 0);
   return L;
 }
 cis::TokScan scan_at(char* base, const cis::ScanLayout& L) {
@@ -272,8 +286,8 @@ size_t cis_sample_workspace_bytes(int64_t T, int64_t V, int dtype) {
   if (T < 0 || V < 1 || V > kMaxV || !known(dtype)) return 0;
   // (the shape of the scan goes by the call's parameters: the larger of its two)
   const int32_t nvec = row_vecs(V, dtype);
-  const SampleLayout a = sample_layout(T, nvec, elem_bytes(dtype), 1),
-                     b = sample_layout(T, nvec, elem_bytes(dtype), 8);
+  const SampleLayout a = sample_layout(T, V, nvec, elem_bytes(dtype), 1),
+                     b = sample_layout(T, V, nvec, elem_bytes(dtype), 8);
   const size_t n = a.total > b.total ? a.total : b.total;
   return n < 256 ? 256 : n;
 }
@@ -316,26 +330,50 @@ int cis_sample(const void* logits, int dtype, int64_t T, int64_t V, int64_t ld, 
   const bool uncut = !counted && !top_k && k == V && !top_p && p.top_p == 1.f;
   const bool wide = !counted && !uncut;
   const bool weighed = !counted && (top_k || k == V);
+  const bool stepped = weighed && (top_p || p.top_p < 1.f);
   const cis::TokRows r = tok_rows(logits, dtype, T, V, ld, mask);
   char* base = static_cast<char*>(workspace);
-  const SampleLayout L = sample_layout(T, r.nvec, elem_bytes(dtype),
+  const SampleLayout L = sample_layout(T, V, r.nvec, elem_bytes(dtype),
                                        cis::scan_group(r.nvec, counted ? k : kManyLogits));
   const cis::TokScan s = scan_at(base, L.scan);
   if (int rc = launch_scan(r, s, dtype, cis::scan_c(1.f), stream)) return rc;
-  cis::SampleArgs a{r, s, reinterpret_cast<unsigned long long*>(base + L.draw),
-                    reinterpret_cast<uint32_t*>(base + L.ties), 0, u, p, temperature, top_k, top_p,
-                    min_p, ids_out, logp_out, logp_kept_out};
-  if (weighed) {
-    const int64_t per = cis::kWeighBlock / 64, need = (T * s.nch + per - 1) / per;
-    if (int rc = launch(cis::weigh_kernel(dtype), need < kMaxBlocks ? need : kMaxBlocks,
-                        cis::kWeighBlock, &a, stream))
-      return rc;
-  }
+  cis::SampleArgs a{};
+  a.r = r;
+  a.s = s;
+  a.draw = reinterpret_cast<unsigned long long*>(base + L.draw);
+  a.ties = reinterpret_cast<uint32_t*>(base + L.ties);
+  a.steps = reinterpret_cast<cis::DrawStep*>(base + L.steps);
+  a.step_ids = reinterpret_cast<uint32_t*>(base + L.step_ids);
+  a.hist = reinterpret_cast<unsigned long long*>(base + L.hist);
+  a.step_ld = L.step_ld;
+  a.parts = L.parts;
+  a.u = u;
+  a.prm = p;
+  a.temperature = temperature;
+  a.top_k = top_k;
+  a.top_p = top_p;
+  a.min_p = min_p;
+  a.ids = ids_out;
+  a.logp = logp_out;
+  a.logp_kept = logp_kept_out;
   const int block = wide ? cis::kTokBlock : cis::kTopBlock;
-  for (; a.row0 < T; a.row0 += kMaxRows)
-    if (int rc = launch(cis::sample_kernel(dtype, wide),
-                        T - a.row0 < kMaxRows ? T - a.row0 : kMaxRows, block, &a, stream))
-      return rc;
+  const int64_t most = stepped ? kStepRows : kMaxRows;
+  for (; a.row0 < T; a.row0 += most) {
+    a.rows = T - a.row0 < most ? T - a.row0 : most;
+    if (stepped) {
+      if (int rc = launch(cis::hist_kernel(dtype), a.rows * L.parts, cis::kHistBlock, &a, stream))
+        return rc;
+      if (L.parts > 1)
+        if (int rc = launch(cis::step_kernel(), a.rows, cis::kHistBlock, &a, stream)) return rc;
+    }
+    if (weighed) {
+      const int64_t per = cis::kWeighBlock / 64, need = (a.rows * s.nch + per - 1) / per;
+      if (int rc = launch(cis::weigh_kernel(dtype), need < kMaxBlocks ? need : kMaxBlocks,
+                          cis::kWeighBlock, &a, stream))
+        return rc;
+    }
+    if (int rc = launch(cis::sample_kernel(dtype, wide), a.rows, block, &a, stream)) return rc;
+  }
   return CIS_OK;
 }
 

@@ -102,7 +102,7 @@ __global__ __launch_bounds__(BLOCK) __attribute__((amdgpu_waves_per_eu(4))) void
   const float c = a.c;
   const int64_t row = a.row0 + blockIdx.x;
   const bool on = tok_on(a.r, row);
-  RowSelect<E, BLOCK, LIST> sel(sh, a.r, a.s, row, on);
+  RowSelect<E, BLOCK, LIST> sel(sh, a.r, a.s, row, on, on);
   const __amdgpu_buffer_rsrc_t rs = sel.rs;
   const float M = sel.M;
   const bool any = sel.tokens(), bad = sel.bad;

@@ -144,6 +144,32 @@ def test_sample_orders_of_a_row(order, dtype):
         _check_sample(logits, u, out, **kw)
 
 
+@pytest.mark.parametrize("dtype", DTYPES)
+@pytest.mark.parametrize("T,V", [(1, 1025), (1, 40000), (5, 262144), (130, 9000), (600, 4097),
+                                 (2100, 1500)])
+def test_sample_top_p_over_rows_and_parts(T, V, dtype):
+    """The cut of top_p by few rows in parts, by one workgroup per row, and by more rows than are
+    listed at once; wide and narrow steps, min_p above and below the cut."""
+    pick = slice(None, None, max(1, T // 40))
+    for kind in ("normal", "ties", "peaked"):
+        logits = _store(_logits(T, V, 7, kind), dtype)
+        u = torch.rand(T, generator=_gen(T + V), device=DEV)
+        u[0], u[-1] = 0.0, 1 - 2.0 ** -24
+        for s in (dict(top_p=0.95), dict(top_p=0.5, temperature=0.7), dict(top_p=1e-6),
+                  dict(top_p=0.9, min_p=0.3), dict(top_p=0.8, min_p=1e-4, temperature=2.0)):
+            out = cis.sample(logits, u, **s)
+            kw = {{"temperature": "temp"}.get(k, k): v for k, v in s.items()}
+            _check_sample(logits[pick], u[pick],
+                          {k: v[pick] for k, v in out.items() if k != "workspace"}, **kw)
+
+
+def test_sample_top_p_of_a_very_long_row():
+    V = 3_900_001
+    logits = _store(_logits(1, V, 2), torch.float32)
+    u = torch.full((1,), 0.7, device=DEV)
+    _check_sample(logits, u, cis.sample(logits, u, top_p=0.9), top_p=0.9)
+
+
 def test_sample_signed_zeros_are_ties():
     z = torch.zeros(4, 32, device=DEV)
     z[:, ::2] = -0.0
