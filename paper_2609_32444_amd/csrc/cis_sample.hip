@@ -27,11 +27,11 @@ struct RowParams {
 };
 __device__ __forceinline__ RowParams row_params(const SampleArgs& a, int64_t row) {
   RowParams p;
-  p.u = a.u[row];
-  p.temp = a.temperature ? a.temperature[row] : a.prm.temperature;
-  const int k = a.top_k ? a.top_k[row] : a.prm.top_k;
-  p.top_p = a.top_p ? a.top_p[row] : a.prm.top_p;
-  p.min_p = a.min_p ? a.min_p[row] : a.prm.min_p;
+  p.u = sload(a.u + row);
+  p.temp = a.temperature ? sload(a.temperature + row) : a.prm.temperature;
+  const int k = a.top_k ? sload(a.top_k + row) : a.prm.top_k;
+  p.top_p = a.top_p ? sload(a.top_p + row) : a.prm.top_p;
+  p.min_p = a.min_p ? sload(a.min_p + row) : a.prm.min_p;
   p.ok = tok_on(a.r, row) && p.u >= 0.f && p.u < 1.f && p.temp >= 0.f && p.temp < INFINITY &&
          k >= 0 && p.top_p > 0.f && p.top_p <= 1.f && p.min_p >= 0.f && p.min_p <= 1.f;
   p.c = kLog2e / p.temp;
@@ -158,69 +158,68 @@ __global__ __launch_bounds__(kHistBlock) void cis_step_kernel(const SampleArgs a
 }
 
 // ------------------------------------------------------------------------------------------
-// One wave per chunk: the sum of its weights, of a row that top_p cuts those above the step of the
-// cut, whose tokens are listed. A chunk whose largest logit does not reach that far is not read.
+// A wave's chunks one after the other, of one row in a workgroup: the sum of their weights, of a row
+// that top_p cuts those above the step of the cut, whose tokens are listed. A chunk whose largest logit
+// does not reach that far is not read. Without STEP, no row is cut by top_p.
 // ------------------------------------------------------------------------------------------
-template <class E>
+template <class E, bool STEP>
 __global__ __launch_bounds__(kWeighBlock) void cis_weigh_kernel(const SampleArgs a) {
   constexpr int NW = kWeighBlock / 64, EPV = E::kPerVec;
-  const int lane = threadIdx.x & 63, wid = __builtin_amdgcn_readfirstlane(threadIdx.x) >> 6;
-  const int nch = a.s.nch;
-  const int64_t total = a.rows * (int64_t)nch;
-  for (int64_t w = (int64_t)blockIdx.x * NW + wid; w < total; w += (int64_t)gridDim.x * NW) {
-    const int64_t at = w / nch, row = a.row0 + at;
-    const int ch = (int)(w - at * nch);
-    const RowParams p = row_params(a, row);
-    if (!row_weighed(p, a)) continue;
-    const float* cmax = a.s.cmax + row * nch;
-    const float M = row_max(cmax, nch, lane), top = draw_exponent(cmax[ch], M, p.c);
-    const int step = p.top_p < 1.f ? sload(&a.steps[at].step) : kFineSteps;
+  const int wid = __builtin_amdgcn_readfirstlane(threadIdx.x) >> 6, nch = a.s.nch;
+  const uint32_t at = blockIdx.x / (uint32_t)a.weigh_parts;
+  const int part = (int)(blockIdx.x - at * (uint32_t)a.weigh_parts);
+  const int64_t row = a.row0 + at;
+  const RowParams p = row_params(a, row);
+  if (!row_weighed(p, a)) return;
+  const float* cmax = a.s.cmax + row * nch;
+  const float M = row_max(cmax, nch, threadIdx.x & 63);
+  const int step = STEP && p.top_p < 1.f ? sload(&a.steps[at].step) : kFineSteps;
+  // exponents above the step, and in it (multiples of 1 / kFine: exact)
+  const float above = step * (-1.f / kFine), within = (step + 1) * (-1.f / kFine);
+  for (int ch = part * NW + wid; ch < nch; ch += a.weigh_parts * NW) {
+    int lane = threadIdx.x & 63;
+    asm volatile("" : "+v"(lane));   // (else what follows from it is kept for all chunks)
+    const float top = draw_exponent(cmax[ch], M, p.c);
     u64 s = 0;
     if (top >= -28.f && draw_step(top) <= step) {
       u32x4 x[kScanSlots];
       load_chunk<E, 0>(tok_rsrc(a.r, row), a.r, ch, lane, x);
-      uint32_t mine = 0;
-      // exponents above the step, and in it (multiples of 1 / kFine: exact)
-      const float above = step * (-1.f / kFine), within = (step + 1) * (-1.f / kFine);
-      const bool every = step == kFineSteps && p.least_w == 0;
+      // which of the lane's tokens are in the step: a bit each, of 4 vectors to a word, the first token's
+      // highest
+      constexpr int kBits = 4 * EPV;
+      static_assert(kScanSlots == 8, "two words");
+      uint32_t in[2] = {0, 0};
       static_for<kScanSlots>([&](auto I) {
         float f[EPV];
         E::unpack(x[I], f);
         uint32_t vs = 0;   // (8 weights stay below 2^32)
-        if (every) {
 #pragma unroll
-          for (int e = 0; e < EPV; ++e) vs += draw_weight(f[e], M, p.c);
-        } else {
-#pragma unroll
-          for (int e = 0; e < EPV; ++e) {
-            const float t = draw_exponent(f[e], M, p.c);
-            const uint32_t q = exponent_weight(t);
-            vs += t > above && q >= p.least_w ? q : 0u;
-            mine += t > within && t <= above ? 1 : 0;
-          }
+        for (int e = 0; e < EPV; ++e) {
+          const float t = draw_exponent(f[e], M, p.c);
+          const uint32_t q = exponent_weight(t);
+          if (STEP) in[I / 4] = in[I / 4] * 2 + (t > within && t <= above ? 1 : 0);
+          vs += (!STEP || t > above) && q >= p.least_w ? q : 0u;
         }
         s += vs;
+        if (STEP) asm volatile("" : "+v"(in[I / 4]));   // (else all vectors are unpacked first)
         slot_fence();
       });
       s = wave_sum(s);
-      if (step < kFineSteps && __ballot(mine != 0)) {
-        const uint32_t upto = wave_scan(mine, lane);
+      if (STEP && step < kFineSteps && __ballot((in[0] | in[1]) != 0)) {
+        const uint32_t mine = __popc(in[0]) + __popc(in[1]), upto = wave_scan(mine, lane);
         uint32_t to = 0;
         if (lane == 63) to = atomicAdd(&a.steps[at].count, upto);
         to = __builtin_amdgcn_readlane(to, 63) + upto - mine;
-        uint32_t* ids = a.step_ids + at * a.step_ld;
-        static_for<kScanSlots>([&](auto I) {
-          float f[EPV];
-          E::unpack(x[I], f);
+        uint32_t* ids = a.step_ids + (int64_t)at * a.step_ld;
 #pragma unroll
-          for (int e = 0; e < EPV; ++e)
-            if (const float t = draw_exponent(f[e], M, p.c); t > within && t <= above) {
-              if (to < (uint32_t)a.step_ld)
-                ids[to] = (uint32_t)((ch * kScanVecs + I * 64 + lane) * EPV + e);
-              ++to;
-            }
-          slot_fence();
-        });
+        for (int h = 0; h < 2; ++h)
+          for (uint32_t left = in[h]; left;) {
+            const int b = 31 - __clz(left), k = kBits - 1 - b;
+            left &= ~(1u << b);
+            if (to < (uint32_t)a.step_ld)
+              ids[to] = (uint32_t)((ch * kScanVecs + (h * 4 + k / EPV) * 64 + lane) * EPV + k % EPV);
+            ++to;
+          }
       }
     }
     if (lane == 0) a.draw[row * nch + ch] = s;
@@ -246,6 +245,7 @@ struct RowDraw {
   SelectShared<LIST>& sh;
   int64_t row;
   float rest;   // sum of exp(z - M) over the row but one of its largest logits
+  u64 mass0;    // the sum of chunk `lane`, asked for ahead of what comes before its use
 
   __device__ __forceinline__ uint32_t weight(float f) const { return draw_weight(f, sel.M, p.c); }
 
@@ -261,8 +261,13 @@ struct RowDraw {
     const int tid = threadIdx.x, lane = tid & 63;
     int first = sel.nch;
     double s = 0.0;
-    for (int i = tid; i < sel.nch; i += BLOCK)
-      if (sel.cmax[i] == sel.M) first = first < i ? first : i;
+    auto each = [&](auto&& f) {   // f(chunk, its largest logit, its sum)
+      if (tid < sel.nch) f(tid, sel.cmax0, sel.csum0);
+      for (int i = BLOCK + tid; i < sel.nch; i += BLOCK) f(i, sel.cmax[i], sel.csum[i]);
+    };
+    each([&](int i, float m, double) {
+      if (m == sel.M) first = first < i ? first : i;
+    });
 #pragma unroll
     for (int off = 32; off >= 1; off >>= 1) {
       const int o = __shfl_xor(first, off, 64);
@@ -271,9 +276,9 @@ struct RowDraw {
     if (lane == 0) sh.u[tid >> 6] = (u64)first;
     __syncthreads();
     for (int w = 0; w < NW; ++w) first = first < (int)sh.u[w] ? first : (int)sh.u[w];
-    for (int i = tid; i < sel.nch; i += BLOCK)
-      if (i != first)
-        s += sel.csum[i] * (double)fast_exp2((sel.cmax[i] - sel.M) * kLog2e);
+    each([&](int i, float m, double sum) {
+      if (i != first) s += sum * (double)fast_exp2((m - sel.M) * kLog2e);
+    });
     if (tid < 64) {
       u32x4 x[kScanSlots];
       load_chunk<E, 0>(sel.rs, a.r, first, lane, x);
@@ -423,7 +428,7 @@ struct RowDraw {
       const u64 upto = tb + (ties ? wave_scan(nt, lane) : 0), b = upto - nt;
       const u64 left = cut.ties > b ? cut.ties - b : 0;
       if (ties) tb = __shfl(upto, 63, 64);
-      return (i < sel.nch ? mass[i] : 0) + (nt < left ? nt : left) * wt;
+      return (i >= sel.nch ? 0 : ties || i0 > 0 ? mass[i] : mass0) + (nt < left ? nt : left) * wt;
     };
     u64 N = 0, tb = 0, nt;
     for (int i0 = 0; i0 < sel.nch; i0 += 64) N += wave_sum(chunk_mass(i0, tb, nt));
@@ -444,66 +449,105 @@ struct RowDraw {
       }
       before = __shfl(upto, 63, 64);
     }
+    auto above = [&](float f, int) {
+      const uint32_t q = weight(f);
+      return order_key(f) > cut.key && q >= least ? q : 0u;
+    };
+    if (ties)
+      in_chunk<true>(ch, before, at, N, above, cut, tb, wt);
+    else
+      in_chunk<false>(ch, before, at, N, above, cut, 0, 0);
+  }
+
+  // Draws within chunk ch, by one wave: weights kept(logit, id) of the tokens, `before` the sum ahead of
+  // the chunk. With TIES, tokens of the cut's key weigh wt (kept() gives them 0) as long as they are
+  // among its first cut.ties, tb of them ahead of the chunk.
+  template <bool TIES, class W>
+  __device__ __forceinline__ void in_chunk(int ch, u64 before, u64 to, u64 N, W&& kept,
+                                           const Cut& cut, u64 tb, uint32_t wt) const {
+    const int lane = threadIdx.x & 63;
     u32x4 x[kScanSlots];
     load_chunk<E, 0>(sel.rs, a.r, ch, lane, x);
-    bool done = false;
+    int slot = -1;   // the 64 vectors that it falls into
     static_for<kScanSlots>([&](auto I) {
-      if (done) return;
       float f[EPV];
       E::unpack(x[I], f);
       const int v = ch * kScanVecs + I * 64 + lane;
-      uint32_t n = 0;
-      if (ties) {
-#pragma unroll
-        for (int e = 0; e < EPV; ++e) n += order_key(f[e]) == cut.key ? 1 : 0;
-      }
-      const u64 tupto = ties ? tb + wave_scan(n, lane) : 0;
-      u64 t = tupto - n;
-      uint32_t w[EPV];
-      u64 sum = 0;
+      uint32_t lane_sum = 0, n = 0;   // (8 weights stay below 2^32)
 #pragma unroll
       for (int e = 0; e < EPV; ++e) {
-        const uint32_t key = order_key(f[e]), q = weight(f[e]);
-        w[e] = key > cut.key && q >= least ? q : 0;
-        if (ties && key == cut.key) w[e] = t++ < cut.ties ? wt : 0;
-        sum += w[e];
+        lane_sum += kept(f[e], v * EPV + e);
+        if (TIES) n += order_key(f[e]) == cut.key ? 1 : 0;
       }
-      const u64 upto = before + wave_scan(sum, lane);
-      const u64 hit = __ballot(upto > at);
-      if (hit) {
-        if (lane == __ffsll(hit) - 1) {
-          u64 b = upto - sum;
-          bool found = false;
-#pragma unroll
-          for (int e = 0; e < EPV; ++e) {
-            if (!found && b + w[e] > at) {
-              found = true;
-              put_row(v * EPV + e, f[e], w[e], N);
-            }
-            b += w[e];
-          }
-        }
-        done = true;
+      u64 sum = wave_sum((u64)lane_sum);
+      if (TIES) {
+        n = wave_sum(n);
+        const u64 left = cut.ties > tb ? cut.ties - tb : 0;
+        sum += (n < left ? n : left) * wt;
       }
-      before = __shfl(upto, 63, 64);
-      tb = ties ? __shfl(tupto, 63, 64) : 0;
+      const bool here = slot < 0 && before + sum > to;
+      if (here) slot = I;
+      if (slot < 0) {
+        before += sum;
+        tb += n;
+      }
       slot_fence();
     });
+    const int v = ch * kScanVecs + slot * 64 + lane;
+    float f[EPV];
+    tok_vec<E>(sel.rs, v, sel.V, f);
+    uint32_t w[EPV], n = 0;
+#pragma unroll
+    for (int e = 0; e < EPV; ++e)
+      if (TIES) n += order_key(f[e]) == cut.key ? 1 : 0;
+    u64 t = TIES ? tb + wave_scan((u64)n, lane) - n : 0, sum = 0;
+#pragma unroll
+    for (int e = 0; e < EPV; ++e) {
+      w[e] = kept(f[e], v * EPV + e);
+      if (TIES && order_key(f[e]) == cut.key) w[e] = t++ < cut.ties ? wt : 0;
+      sum += w[e];
+    }
+    const u64 upto = before + wave_scan(sum, lane);
+    if (upto > to && upto - sum <= to) {
+      u64 b = upto - sum;
+      bool found = false;
+#pragma unroll
+      for (int e = 0; e < EPV; ++e) {
+        if (!found && b + w[e] > to) {
+          found = true;
+          put_row(v * EPV + e, f[e], w[e], N);
+        }
+        b += w[e];
+      }
+    }
   }
 
   __device__ __forceinline__ int fine_step(float f) const {
     return draw_step(draw_exponent(f, sel.M, p.c));
   }
 
-  // f(logits, vector) for the row's chunks that hold a weight, whole waves together.
-  template <class F>
-  __device__ __forceinline__ void each_chunk(F&& f) const {
+  // f(logits of vector v, v) for the row's chunks that hold a weight, whole waves together; then
+  // end(chunk), of the others too.
+  template <class F, class G>
+  __device__ __forceinline__ void each_chunk(F&& f, G&& end) const {
     const int lane = threadIdx.x & 63, wid = __builtin_amdgcn_readfirstlane(threadIdx.x) >> 6;
+    constexpr int U = 4;   // loads in flight (8: the float32 kernels spill)
     for (int ch = wid; ch < sel.nch; ch += NW) {
-      const bool any = (sel.cmax[ch] - sel.M) * p.c >= -28.f;
-      u32x4 x[kScanSlots];
-      if (any) load_chunk<E, 0>(sel.rs, a.r, ch, lane, x);
-      f(ch, any, x);
+      if (draw_exponent(sel.cmax[ch], sel.M, p.c) >= -28.f)
+#pragma unroll 1
+        for (int v0 = ch * kScanVecs + lane; v0 < (ch + 1) * kScanVecs; v0 += U * 64) {
+          u32x4 x[U];
+          static_for<U>([&](auto I) { x[I] = bload_aux<0>(sel.rs, (uint32_t)(v0 + I * 64) * 16u); });
+          static_for<U>([&](auto I) {
+            const int v = v0 + I * 64;
+            float l[EPV];
+            E::unpack(x[I], l);
+            if ((v + 1) * EPV > sel.V) mask_past_end<E>(l, v, sel.V);
+            f(l, v);
+            slot_fence();
+          });
+        }
+      end(ch);
     }
   }
 
@@ -536,21 +580,16 @@ struct RowDraw {
     __syncthreads();
     if (threadIdx.x == 0) sh.count = 0;
     __syncthreads();
-    each_chunk([&](int ch, bool any, u32x4 (&x)[kScanSlots]) {
-      if (!any) return;
-      static_for<kScanSlots>([&](auto I) {
-        float f[EPV];
-        E::unpack(x[I], f);
+    each_chunk(
+        [&](const float (&f)[EPV], int v) {
 #pragma unroll
-        for (int e = 0; e < EPV; ++e) {
-          const bool take = fine_step(f[e]) == step;
-          const uint32_t at = take_place(take, &sh.count, lane);
-          if (take && at < LIST)
-            sh.list[at] = token_of(f[e], (ch * kScanVecs + I * 64 + lane) * EPV + e);
-        }
-        slot_fence();
-      });
-    });
+          for (int e = 0; e < EPV; ++e) {
+            const bool take = fine_step(f[e]) == step;
+            const uint32_t at = take_place(take, &sh.count, lane);
+            if (take && at < LIST) sh.list[at] = token_of(f[e], v * EPV + e);
+          }
+        },
+        [](int) {});
     __syncthreads();
     sel.count = (int)sh.count;
     if (sel.count > LIST) return false;
@@ -567,22 +606,18 @@ struct RowDraw {
       ws.count[i] = 0;
     }
     __syncthreads();
-    each_chunk([&](int, bool any, u32x4 (&x)[kScanSlots]) {
-      if (!any) return;
-      static_for<kScanSlots>([&](auto I) {
-        float f[EPV];
-        E::unpack(x[I], f);
+    each_chunk(
+        [&](const float (&f)[EPV], int) {
 #pragma unroll
-        for (int e = 0; e < EPV; ++e) {
-          const int st = fine_step(f[e]);
-          if (st < kFineSteps) {
-            atomicAdd(&ws.mass[st], (u64)weight(f[e]));
-            if (by_count) atomicAdd(&ws.count[st], 1u);
+          for (int e = 0; e < EPV; ++e) {
+            const int st = fine_step(f[e]);
+            if (st < kFineSteps) {
+              atomicAdd(&ws.mass[st], (u64)weight(f[e]));
+              if (by_count) atomicAdd(&ws.count[st], 1u);
+            }
           }
-        }
-        slot_fence();
-      });
-    });
+        },
+        [](int) {});
     __syncthreads();
     // the list's first n logits as a cut
     auto cut_at = [&](int n) {
@@ -676,14 +711,10 @@ struct RowDraw {
     const int lane = threadIdx.x & 63;
     u64* mass = a.draw + row * sel.nch;
     uint32_t* ties = a.ties + row * sel.nch;
-    const float least_f = key_value(cut.key);
-    each_chunk([&](int ch, bool any, u32x4 (&x)[kScanSlots]) {
-      u64 s = 0;
-      uint32_t t = 0;
-      if (any && sel.cmax[ch] + 0.f >= least_f) {
-        static_for<kScanSlots>([&](auto I) {
-          float f[EPV];
-          E::unpack(x[I], f);
+    u64 s = 0;
+    uint32_t t = 0;
+    each_chunk(
+        [&](const float (&f)[EPV], int) {
 #pragma unroll
           for (int e = 0; e < EPV; ++e) {
             const uint32_t key = order_key(f[e]);
@@ -693,16 +724,17 @@ struct RowDraw {
             }
             t += key == cut.key ? 1 : 0;
           }
-          slot_fence();
+        },
+        [&](int ch) {
+          s = wave_sum(s);
+          t = wave_sum(t);
+          if (lane == 0) {
+            mass[ch] = s;
+            ties[ch] = t;
+          }
+          s = 0;
+          t = 0;
         });
-        s = wave_sum(s);
-        t = wave_sum(t);
-      }
-      if (lane == 0) {
-        mass[ch] = s;
-        ties[ch] = t;
-      }
-    });
     __syncthreads();
     from_chunks(cut, ties, p.least_w);
   }
@@ -769,51 +801,15 @@ struct RowDraw {
       }
       before = __shfl(upto, 63, 64);
     }
-    in_chunk(ch, before, to, N, [&](float f, int id) {
+    auto kept = [&](float f, int id) {
       const float t = draw_exponent(f, sel.M, p.c);
       const int st = draw_step(t);
       const uint32_t q = exponent_weight(t);
       const bool in = st < step ? q >= p.least_w : st == step && token_of(f, id) >= last;
       return in ? q : 0u;
-    });
+    };
+    in_chunk<false>(ch, before, to, N, kept, Cut{}, 0, 0);
     return true;
-  }
-
-  // Draws within chunk ch, whose weights are kept(logit, id), `before` them all; by one wave.
-  template <class W>
-  __device__ __forceinline__ void in_chunk(int ch, u64 before, u64 to, u64 N, W&& kept) const {
-    const int lane = threadIdx.x & 63;
-    u32x4 x[kScanSlots];
-    load_chunk<E, 0>(sel.rs, a.r, ch, lane, x);
-    bool done = false;
-    static_for<kScanSlots>([&](auto I) {
-      if (done) return;
-      float f[EPV];
-      E::unpack(x[I], f);
-      const int v = ch * kScanVecs + I * 64 + lane;
-      uint32_t w[EPV], sum = 0;   // (8 weights stay below 2^32)
-#pragma unroll
-      for (int e = 0; e < EPV; ++e) sum += w[e] = kept(f[e], v * EPV + e);
-      const u64 upto = before + wave_scan((u64)sum, lane);
-      const u64 hit = __ballot(upto > to);
-      if (hit) {
-        if (lane == __ffsll(hit) - 1) {
-          u64 b = upto - sum;
-          bool found = false;
-#pragma unroll
-          for (int e = 0; e < EPV; ++e) {
-            if (!found && b + w[e] > to) {
-              found = true;
-              put_row(v * EPV + e, f[e], w[e], N);
-            }
-            b += w[e];
-          }
-        }
-        done = true;
-      }
-      before = __shfl(upto, 63, 64);
-      slot_fence();
-    });
   }
 
   __device__ __forceinline__ void run(WideShared* ws) {
@@ -875,6 +871,9 @@ __global__ __launch_bounds__(BLOCK) __attribute__((amdgpu_waves_per_eu(4))) void
   __shared__ std::conditional_t<WIDE, WideShared, uint32_t> ws;
   const int64_t row = a.row0 + blockIdx.x;
   const RowParams p = row_params(a, row);
+  const int lane = threadIdx.x & 63;
+  u64 mass0 = 0;
+  if (row_weighed(p, a) && lane < a.s.nch) mass0 = a.draw[row * a.s.nch + lane];
   RowSelect<E, BLOCK, LIST> sel(sh, a.r, a.s, row, p.ok, p.counted);
   if (!p.ok || !sel.tokens()) {
     if (threadIdx.x == 0) {
@@ -884,16 +883,18 @@ __global__ __launch_bounds__(BLOCK) __attribute__((amdgpu_waves_per_eu(4))) void
     }
     return;
   }
-  RowDraw<E, BLOCK, LIST, WIDE> draw{a, p, sel, sh, row, 0.f};
+  RowDraw<E, BLOCK, LIST, WIDE> draw{a, p, sel, sh, row, 0.f, mass0};
   if constexpr (WIDE)
     draw.run(&ws);
   else
     draw.run(nullptr);
 }
 
-const void* weigh_kernel(int dtype) {
-  return dtype == CIS_BF16 ? (const void*)&cis_weigh_kernel<Bf16>
-                           : (const void*)&cis_weigh_kernel<F32>;
+const void* weigh_kernel(int dtype, bool step) {
+#define CIS_WEIGH(E) \
+  (step ? (const void*)&cis_weigh_kernel<E, true> : (const void*)&cis_weigh_kernel<E, false>)
+  return dtype == CIS_BF16 ? CIS_WEIGH(Bf16) : CIS_WEIGH(F32);
+#undef CIS_WEIGH
 }
 const void* hist_kernel(int dtype) {
   return dtype == CIS_BF16 ? (const void*)&cis_hist_kernel<Bf16>

@@ -10,6 +10,20 @@ namespace cis {
 template <class E>
 using elem_t = std::conditional_t<E::kPerVec == 8, uint16_t, uint32_t>;
 
+// A vector's first n elements, and -inf for the others (n <= 0: all of them).
+template <class E>
+__device__ __forceinline__ u32x4 tail_vec(u32x4 x, int n) {
+  constexpr int per = E::kPerVec / 4;   // elements per word
+  const u32x4 none = E::neg_inf_vec();
+#pragma unroll
+  for (int k = 0; k < 4; ++k) {
+    uint32_t keep = n > k * per ? ~0u : 0u;
+    if (per == 2 && n == 2 * k + 1) keep = 0xFFFFu;
+    x[k] = (x[k] & keep) | (none[k] & ~keep);
+  }
+  return x;
+}
+
 // A chunk's vectors, 8 per lane; past the row's end -inf.
 constexpr int kScanSlots = kScanVecs / 64;
 template <class E, int AUX>
@@ -19,9 +33,7 @@ __device__ __forceinline__ void load_chunk(__amdgpu_buffer_rsrc_t rs, const TokR
   static_for<kScanSlots>([&](auto I) { x[I] = bload_aux<AUX>(rs, (uint32_t)(v0 + I * 64) * 16u); });
   if ((ch + 1) * kScanVecs * E::kPerVec > r.V)
     static_for<kScanSlots>([&](auto I) {
-      const int v = v0 + I * 64;
-      if (v >= r.nvec - 1)
-        x[I] = v < r.nvec ? E::mask_tail(x[I], r.V - v * E::kPerVec) : E::neg_inf_vec();
+      x[I] = tail_vec<E>(x[I], r.V - (v0 + I * 64) * E::kPerVec);
     });
 }
 
@@ -96,6 +108,8 @@ struct RowSelect {
   const elem_t<E>* gm;
   const float* cmax;
   const double* csum;
+  float cmax0;      // of chunk `tid`
+  double csum0;
   float gr[kGroupRegs];
   bool kept;
   float M;          // the row's largest logit
@@ -117,10 +131,16 @@ struct RowSelect {
         const int g = tid + I * BLOCK;
         gr[I] = I * BLOCK < ngrp && g < ngrp ? group_max(g) : -INFINITY;
       });
-    M = -INFINITY;
-    bad = false;
+    cmax0 = -INFINITY;
+    csum0 = 0.0;
+    if (on && tid < nch) {
+      cmax0 = cmax[tid];
+      csum0 = csum[tid];
+    }
+    M = cmax0;
+    bad = !(csum0 < INFINITY);
     if (on)
-      for (int i = tid; i < nch; i += BLOCK) {
+      for (int i = BLOCK + tid; i < nch; i += BLOCK) {
         M = fmaxf(M, cmax[i]);
         bad |= !(csum[i] < INFINITY);
       }

@@ -84,6 +84,7 @@ struct SampleArgs {
   uint32_t* step_ids;         // [rows, step_ld] the tokens of the rows' steps
   unsigned long long* hist;   // [rows, parts, kFineSteps] with parts > 1
   int32_t step_ld, parts;
+  int32_t weigh_parts;        // workgroups of a row in cis_weigh_kernel
   int64_t row0, rows;         // the launch's first row, and how many
   const float* u;
   cis_sample_params_t prm;
@@ -146,7 +147,7 @@ constexpr int kDrawListK = 128;   // top_k that the kernel for short lists takes
 const void* scan_kernel(int dtype, int32_t gv);
 // wide: any parameters; else top_k in [1, 128] for every row or nothing to cut but min_p
 const void* sample_kernel(int dtype, bool wide);
-const void* weigh_kernel(int dtype);
+const void* weigh_kernel(int dtype, bool step);
 const void* hist_kernel(int dtype);
 const void* step_kernel();
 const void* top_kernel(int dtype, int64_t K);

@@ -96,6 +96,8 @@ constexpr int64_t kManyLogits = 256;
 // Rows whose steps of a cut are listed at once, and workgroups that the histograms of few rows take.
 constexpr int64_t kStepRows = 2048;
 constexpr int64_t kHistBlocks = 256;
+// Workgroups of cis_weigh_kernel beyond which a wave takes several chunks.
+constexpr int64_t kWeighBlocks = 2048;
 
 struct SampleLayout {
   cis::ScanLayout scan;
@@ -367,9 +369,12 @@ int cis_sample(const void* logits, int dtype, int64_t T, int64_t V, int64_t ld, 
         if (int rc = launch(cis::step_kernel(), a.rows, cis::kHistBlock, &a, stream)) return rc;
     }
     if (weighed) {
-      const int64_t per = cis::kWeighBlock / 64, need = (a.rows * s.nch + per - 1) / per;
-      if (int rc = launch(cis::weigh_kernel(dtype), need < kMaxBlocks ? need : kMaxBlocks,
-                          cis::kWeighBlock, &a, stream))
+      // a chunk per wave, or more of them where the chip is filled all the same
+      const int64_t per = cis::kWeighBlock / 64, most = (s.nch + per - 1) / per,
+                    fill = (kWeighBlocks + a.rows - 1) / a.rows;
+      a.weigh_parts = (int32_t)(fill < most ? fill : most);
+      if (int rc = launch(cis::weigh_kernel(dtype, stepped), a.rows * a.weigh_parts, cis::kWeighBlock, &a,
+                          stream))
         return rc;
     }
     if (int rc = launch(cis::sample_kernel(dtype, wide), a.rows, block, &a, stream)) return rc;
