@@ -114,8 +114,8 @@ struct RowSelect {
   bool kept;
   float M;          // the row's largest logit
   bool bad;         // a NaN or a +inf in it
-  float scale;      // of the steps below M that the last collect() took logits from ...
-  uint32_t bin;     // ... up to this one (256: every logit)
+  float top, least; // the last collect() took the logits from `least`; few of them lie above `top`
+  uint32_t bin;     // 256: it took every logit
   int count;        // logits in the list
 
   __device__ __forceinline__ RowSelect(SelectShared<LIST>& s, const TokRows& r, const TokScan& t,
@@ -175,17 +175,22 @@ struct RowSelect {
   // not hold them.
   __device__ __forceinline__ bool collect(int K) {
     const int tid = threadIdx.x, lane = tid & 63, wid = tid >> 6;
-    scale = 16.f;
+    // 256 steps below `top`, of the groups that do not lie above it; those that do are `prior`. From
+    // pass to pass the step that holds the K-th group is looked at more closely, or what lies
+    // beyond the steps.
+    float scale = 16.f;
+    uint32_t prior = 0;
+    top = M;
     for (;;) {
       each_group([&](int, float x) {
-        if (x > -INFINITY) atomicAdd(&sh.hist[below(x, M, scale, 255.f)], 1u);
+        if (x > -INFINITY && x <= top) atomicAdd(&sh.hist[below(x, top, scale, 255.f)], 1u);
       });
       __syncthreads();
       if (tid < 64) {
         uint32_t b[4], s = 0;
 #pragma unroll
         for (int i = 0; i < 4; ++i) s += b[i] = sh.hist[4 * tid + i];
-        const uint32_t upto = wave_scan(s, tid), total = __shfl(upto, 63, 64);
+        const uint32_t upto = wave_scan(s, tid) + prior, total = __shfl(upto, 63, 64);
         uint32_t before = upto - s;
         if (total < (uint32_t)K) {   // every logit is taken
           if (tid == 0) sh.bin = 256;
@@ -194,27 +199,52 @@ struct RowSelect {
           while (before + b[i] < (uint32_t)K) before += b[i++];
           sh.bin = 4 * tid + i;
           sh.groups = before + b[i];
+          sh.count = before;
         }
       }
       __syncthreads();
       bin = sh.bin;
+      const uint32_t reach = sh.groups, before = sh.count;
       // too coarse a step takes in many more groups than it has to
-      const bool finer = bin < 15 && sh.groups > 2u * (uint32_t)K + 64 && scale < 0x1p40f;
+      const bool finer = bin < 255 && reach > 2u * (uint32_t)K + 64 && scale < 0x1p40f;
       const bool coarser = bin == 255 && scale > 0x1p-140f;
+      float hi = -INFINITY, lo = INFINITY;   // of the step's groups
+      if (finer || coarser) {
+        each_group([&](int, float x) {
+          if (x > -INFINITY && x <= top && (uint32_t)below(x, top, scale, 255.f) == bin) {
+            hi = fmaxf(hi, x);
+            lo = fminf(lo, x);
+          }
+        });
+        hi = wave_max(hi);
+        lo = -wave_max(-lo);
+        if (lane == 0) {
+          sh.f[wid] = hi;
+          sh.d[wid] = lo;
+        }
+      }
       __syncthreads();
       if (tid == 0) sh.groups = sh.count = 0;
       if (tid < 256) sh.hist[tid] = 0;
+      if (finer || coarser)
+        for (int w = 0; w < NW; ++w) {
+          hi = fmaxf(hi, sh.f[w]);
+          lo = fminf(lo, (float)sh.d[w]);
+        }
       __syncthreads();
-      if (!finer && !coarser) break;
-      scale *= finer ? 16.f : 0.0625f;
+      if (!(finer || coarser) || hi == lo) break;
+      top = hi;
+      prior = before;
+      scale *= finer ? 16.f : 0.25f;
     }
     // what is taken reaches the smallest of the groups' largest logits within the steps
-    float least = INFINITY;
+    least = INFINITY;
     if (bin == 256)
       least = -FLT_MAX;
     else
       each_group([&](int, float x) {
-        if (x > -INFINITY && (uint32_t)below(x, M, scale, 255.f) <= bin) least = fminf(least, x);
+        if (x > -INFINITY && (x > top || (uint32_t)below(x, top, scale, 255.f) <= bin))
+          least = fminf(least, x);
       });
     least = -wave_max(-least);
     if (lane == 0) sh.f[wid] = least;
@@ -275,15 +305,21 @@ struct RowSelect {
     return count <= LIST;
   }
 
-  // The first K of the collected list in order: counted into fine steps of the distance from M,
-  // moved to the steps' places, and ranked among the few that share a step.
+  // The first K of the collected list in order: counted into fine steps (a quarter of them above
+  // `top`), moved to the steps' places, and ranked among the few that share a step.
   __device__ __forceinline__ void order(int K) {
     const int tid = threadIdx.x, lane = tid & 63, wid = tid >> 6;
     constexpr int R = LIST / BLOCK, S = kSteps / BLOCK;
     bool ranked = bin < 256;
     if (ranked) {
-      const float fine = scale * ((float)kSteps / (float)(bin + 1));
-      auto step_of = [&](u64 t) { return below(token_value(t), M, fine, (float)(kSteps - 1)); };
+      const int first = top < M ? kSteps / 4 : 0;
+      const float above = (float)first / fmaxf(M - top, FLT_MIN),
+                  fine = (float)(kSteps - first) / fmaxf(top - least, FLT_MIN);
+      auto step_of = [&](u64 t) {
+        const float f = token_value(t);
+        return f > top ? below(f, M, above, (float)(first - 1))
+                       : first + below(f, top, fine, (float)(kSteps - first - 1));
+      };
       for (int i = tid; i < kSteps; i += BLOCK) sh.step[i] = 0;
       __syncthreads();
       u64 t[R];

@@ -287,6 +287,27 @@ def test_top_orders_of_a_row(order, dtype):
         _check_top(logits, K, cis.top_logits(logits, K))
 
 
+@pytest.mark.parametrize("dtype", DTYPES)
+def test_top_of_spread_rows(dtype):
+    """Rows whose K-th logit lies far below the largest, near it, or among logits of every size."""
+    V = 30000
+    g = _gen(21)
+    z = torch.randn(8, V, generator=g, device=DEV) * 3
+    z[0, 5000] += 40.0                                     # one logit stands out
+    z[1, torch.arange(0, V, 97, device=DEV)] += 300.0      # some 300 do
+    z[2] = z[2] * 1e30
+    z[3] = z[3] * 1e-30
+    z[4] = torch.sign(z[4]) * torch.exp(z[4] * 10)         # every size
+    z[5] = z[5] * 1e-3 + 100.0                             # close together
+    z[6, 17], z[6, 18] = 3e38, 2.9e38
+    z[7] = torch.where(z[7] > 6, z[7] + 1000, z[7] / 1000)
+    logits = _store(z, dtype)
+    u = torch.rand(8, generator=g, device=DEV)
+    for K in (1, 5, 64, 256, 310, 1000):
+        _check_top(logits, K, cis.top_logits(logits, K))
+        _check_sample(logits, u, cis.sample(logits, u, top_k=K), top_k=K)
+
+
 def test_top_masked_and_not_finite():
     V, K = 3000, 40
     z = _logits(8, V, 12)
