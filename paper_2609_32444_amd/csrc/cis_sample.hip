@@ -92,7 +92,9 @@ __device__ __forceinline__ DrawStep step_of_cut(const u64* mass, float top_p, in
 // ------------------------------------------------------------------------------------------
 // The histogram of a row's weights by their exponents, in a part of the row's chunks per workgroup:
 // whole numbers in LDS, so that the order of the additions is of no account. Where a row has one
-// workgroup, the step of its cut too.
+// workgroup, the step of its cut too. Tokens that the cut cannot reach are added up in registers: at
+// most V of them have a weight of `lowest` each, and the whole sum is that of the chunks' largest
+// logits at least, so that they stay below 1 - top_p of it.
 // ------------------------------------------------------------------------------------------
 template <class E>
 __global__ __launch_bounds__(kHistBlock) void cis_hist_kernel(const SampleArgs a) {
@@ -108,6 +110,12 @@ __global__ __launch_bounds__(kHistBlock) void cis_hist_kernel(const SampleArgs a
   const float* cmax = a.s.cmax + row * nch;
   const float M = row_max(cmax, nch, lane);
   const __amdgpu_buffer_rsrc_t rs = tok_rsrc(a.r, row);
+  float least = 0.f;
+  for (int i = lane; i < nch; i += 64) least += fast_exp2(draw_exponent(cmax[i], M, p.c));
+  least = 0.99f * wave_sum(least);
+  const float octaves = log2f((float)a.r.V / ((1.f - p.top_p) * least)),
+              lowest = octaves < 29.f ? ceilf(octaves * kFine) * (-1.f / kFine) : -29.f;
+  u64 rest = 0;
   __syncthreads();
   for (int ch = part * NW + wid; ch < nch; ch += a.parts * NW) {
     if (!(draw_exponent(cmax[ch], M, p.c) >= -28.f)) continue;
@@ -116,15 +124,22 @@ __global__ __launch_bounds__(kHistBlock) void cis_hist_kernel(const SampleArgs a
     static_for<kScanSlots>([&](auto I) {
       float f[EPV];
       E::unpack(x[I], f);
+      uint32_t vs = 0;   // (8 weights stay below 2^32)
 #pragma unroll
       for (int e = 0; e < EPV; ++e) {
         const float t = draw_exponent(f[e], M, p.c);
-        const int st = draw_step(t);
-        if (st < kFineSteps) atomicAdd(&mass[st], (u64)exponent_weight(t));
+        const uint32_t q = exponent_weight(t);
+        if (t > lowest)
+          atomicAdd(&mass[(int)(t * -(float)kFine)], (u64)q);
+        else
+          vs += q;
       }
+      rest += vs;
       slot_fence();
     });
   }
+  rest = wave_sum(rest);
+  if (lane == 0 && rest) atomicAdd(&mass[kFineSteps - 1], rest);
   __syncthreads();
   if (a.parts == 1) {
     if (tid < 64) {
