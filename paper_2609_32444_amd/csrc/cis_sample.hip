@@ -270,6 +270,25 @@ struct RowDraw {
     if (a.logp_kept) a.logp_kept[row] = (float)log((double)w / (double)N);
   }
 
+  // f(logits of vector v, v) for a thread's vectors of chunk ch, which follow each other.
+  static constexpr int kChunkVecs = kScanVecs < BLOCK ? 1 : kScanVecs / BLOCK;
+  template <class F>
+  __device__ __forceinline__ void each_in_chunk(int ch, F&& f) const {
+    const int v0 = threadIdx.x * kChunkVecs;
+    if (v0 >= kScanVecs) return;
+    u32x4 x[kChunkVecs];
+    static_for<kChunkVecs>([&](auto J) {
+      x[J] = bload_aux<0>(sel.rs, (uint32_t)(ch * kScanVecs + v0 + J) * 16u);
+    });
+    static_for<kChunkVecs>([&](auto J) {
+      const int v = ch * kScanVecs + v0 + J;
+      float l[EPV];
+      E::unpack(x[J], l);
+      if ((v + 1) * EPV > sel.V) mask_past_end<E>(l, v, sel.V);
+      f(l, v);
+    });
+  }
+
   // Sum over the row but one largest logit, relative to it: the chunks' sums, except for the
   // first chunk that holds it, which is summed again without it.
   __device__ __forceinline__ void sum_rest() {
@@ -294,24 +313,19 @@ struct RowDraw {
     each([&](int i, float m, double sum) {
       if (i != first) s += sum * (double)fast_exp2((m - sel.M) * kLog2e);
     });
-    if (tid < 64) {
-      u32x4 x[kScanSlots];
-      load_chunk<E, 0>(sel.rs, a.r, first, lane, x);
-      uint32_t n = 0;
-      static_for<kScanSlots>([&](auto I) {
-        float f[EPV], t = 0.f;
-        E::unpack(x[I], f);
+    u64 n = 0;   // largest ones in the chunk (counted apart: 1 would swallow what is far smaller)
+    each_in_chunk(first, [&](const float (&f)[EPV], int) {
+      float t = 0.f;
 #pragma unroll
-        for (int e = 0; e < EPV; ++e) {
-          t += f[e] == sel.M ? 0.f : fast_exp2((f[e] - sel.M) * kLog2e);
-          n += f[e] == sel.M ? 1 : 0;
-        }
-        s += (double)t;
-        slot_fence();
-      });
-      n = wave_sum(n);
-      if (tid == 0) s += (double)(n - 1);
-    }
+      for (int e = 0; e < EPV; ++e) {
+        t += f[e] == sel.M ? 0.f : fast_exp2((f[e] - sel.M) * kLog2e);
+        n += f[e] == sel.M ? 1 : 0;
+      }
+      s += (double)t;
+    });
+    __syncthreads();
+    n = block_sum<NW>(n, sh.u);
+    if (tid == 0) s += (double)(n - 1);
     rest = (float)block_sum<NW>(s, sh.d);
   }
 
@@ -432,108 +446,134 @@ struct RowDraw {
   // chunk of which the row's first cut.ties count.
   __device__ __forceinline__ void from_chunks(const Cut& cut, const uint32_t* ties, uint32_t least) {
     const int tid = threadIdx.x, lane = tid & 63;
-    if (tid >= 64) return;
     const u64* mass = a.draw + row * sel.nch;
     uint32_t wt = ties && cut.ties > 0 ? weight(key_value(cut.key)) : 0;
     if (wt < least) wt = 0;
-    // (chunk i0 + lane's kept mass, and the ties up to it)
-    auto chunk_mass = [&](int i0, u64& tb, u64& nt) {
-      const int i = i0 + lane;
-      nt = ties && i < sel.nch ? ties[i] : 0;
-      const u64 upto = tb + (ties ? wave_scan(nt, lane) : 0), b = upto - nt;
-      const u64 left = cut.ties > b ? cut.ties - b : 0;
-      if (ties) tb = __shfl(upto, 63, 64);
-      return (i >= sel.nch ? 0 : ties || i0 > 0 ? mass[i] : mass0) + (nt < left ? nt : left) * wt;
-    };
-    u64 N = 0, tb = 0, nt;
-    for (int i0 = 0; i0 < sel.nch; i0 += 64) N += wave_sum(chunk_mass(i0, tb, nt));
-    u64 at = (u64)((double)p.u * (double)N);
-    if (at >= N) at = N - 1;
-    u64 before = 0;
-    tb = 0;
-    int ch = 0;
-    for (int i0 = 0; i0 < sel.nch; i0 += 64) {
-      const u64 tb0 = tb, m = chunk_mass(i0, tb, nt), upto = before + wave_scan(m, lane);
-      const u64 hit = __ballot(upto > at);
-      if (hit) {
-        const int who = __ffsll(hit) - 1;
-        ch = i0 + who;
-        before = __shfl(upto - m, who, 64);
-        tb = ties ? tb0 + __shfl(wave_scan(nt, lane) - nt, who, 64) : 0;
-        break;
+    __syncthreads();
+    if (tid < 64) {
+      // (chunk i0 + lane's kept mass, and the ties up to it)
+      auto chunk_mass = [&](int i0, u64& tb, u64& nt) {
+        const int i = i0 + lane;
+        nt = ties && i < sel.nch ? ties[i] : 0;
+        const u64 upto = tb + (ties ? wave_scan(nt, lane) : 0), b = upto - nt;
+        const u64 left = cut.ties > b ? cut.ties - b : 0;
+        if (ties) tb = __shfl(upto, 63, 64);
+        return (i >= sel.nch ? 0 : ties || i0 > 0 ? mass[i] : mass0) + (nt < left ? nt : left) * wt;
+      };
+      Place at{0, 0, 0, 0, 0};
+      u64 tb = 0, nt;
+      for (int i0 = 0; i0 < sel.nch; i0 += 64) at.N += wave_sum(chunk_mass(i0, tb, nt));
+      at.to = (u64)((double)p.u * (double)at.N);
+      if (at.to >= at.N) at.to = at.N - 1;
+      tb = 0;
+      for (int i0 = 0; i0 < sel.nch; i0 += 64) {
+        const u64 tb0 = tb, m = chunk_mass(i0, tb, nt), upto = at.before + wave_scan(m, lane);
+        const u64 hit = __ballot(upto > at.to);
+        if (hit) {
+          const int who = __ffsll(hit) - 1;
+          at.ch = i0 + who;
+          at.before = __shfl(upto - m, who, 64);
+          at.tb = ties ? tb0 + __shfl(wave_scan(nt, lane) - nt, who, 64) : 0;
+          break;
+        }
+        at.before = __shfl(upto, 63, 64);
       }
-      before = __shfl(upto, 63, 64);
+      if (lane == 0) put_place(at);
     }
     auto above = [&](float f, int) {
       const uint32_t q = weight(f);
       return order_key(f) > cut.key && q >= least ? q : 0u;
     };
     if (ties)
-      in_chunk<true>(ch, before, at, N, above, cut, tb, wt);
+      in_chunk<true>(above, cut, wt);
     else
-      in_chunk<false>(ch, before, at, N, above, cut, 0, 0);
+      in_chunk<false>(above, cut, 0);
   }
 
-  // Draws within chunk ch, by one wave: weights kept(logit, id) of the tokens, `before` the sum ahead of
-  // the chunk. With TIES, tokens of the cut's key weigh wt (kept() gives them 0) as long as they are
-  // among its first cut.ties, tb of them ahead of the chunk.
+  // What the first wave found: the chunk, the sum ahead of it, the draw, the whole sum, and the ties
+  // ahead of the chunk.
+  struct Place {
+    u64 ch, before, to, N, tb;
+  };
+  __device__ __forceinline__ void put_place(const Place& p) const {
+    sh.u[0] = p.ch;
+    sh.u[1] = p.before;
+    sh.u[2] = p.to;
+    sh.u[3] = p.N;
+    sh.u[4] = p.tb;
+  }
+
+  // Sum over the threads ahead of this one; `u` may be used again after the next barrier.
+  __device__ __forceinline__ u64 ahead(u64 x, u64* u) const {
+    const int lane = threadIdx.x & 63, wid = threadIdx.x >> 6;
+    const u64 upto = wave_scan(x, lane);
+    if (lane == 63) u[wid] = upto;
+    __syncthreads();
+    u64 b = upto - x;
+    for (int w = 0; w < wid; ++w) b += u[w];
+    return b;
+  }
+
+  // Draws within a chunk, at put_place's values: weights kept(logit, id) of the tokens. With TIES,
+  // tokens of the cut's key weigh wt (kept() gives them 0) as long as they are among its first
+  // cut.ties.
   template <bool TIES, class W>
-  __device__ __forceinline__ void in_chunk(int ch, u64 before, u64 to, u64 N, W&& kept,
-                                           const Cut& cut, u64 tb, uint32_t wt) const {
-    const int lane = threadIdx.x & 63;
-    u32x4 x[kScanSlots];
-    load_chunk<E, 0>(sel.rs, a.r, ch, lane, x);
-    int slot = -1;   // the 64 vectors that it falls into
-    static_for<kScanSlots>([&](auto I) {
-      float f[EPV];
-      E::unpack(x[I], f);
-      const int v = ch * kScanVecs + I * 64 + lane;
-      uint32_t lane_sum = 0, n = 0;   // (8 weights stay below 2^32)
+  __device__ __forceinline__ void in_chunk(W&& kept, const Cut& cut, uint32_t wt) const {
+    __syncthreads();
+    const int ch = (int)sh.u[0];
+    const u64 to = sh.u[2], N = sh.u[3];
+    u64 before = sh.u[1], t = sh.u[4];
+    uint32_t w[kChunkVecs][EPV];
+    float l[kChunkVecs][EPV];
+    u64 n = 0, sum = 0;
+    int j = 0;
+    static_for<kChunkVecs>([&](auto J) {
 #pragma unroll
-      for (int e = 0; e < EPV; ++e) {
-        lane_sum += kept(f[e], v * EPV + e);
-        if (TIES) n += order_key(f[e]) == cut.key ? 1 : 0;
-      }
-      u64 sum = wave_sum((u64)lane_sum);
-      if (TIES) {
-        n = wave_sum(n);
-        const u64 left = cut.ties > tb ? cut.ties - tb : 0;
-        sum += (n < left ? n : left) * wt;
-      }
-      const bool here = slot < 0 && before + sum > to;
-      if (here) slot = I;
-      if (slot < 0) {
-        before += sum;
-        tb += n;
-      }
-      slot_fence();
+      for (int e = 0; e < EPV; ++e) w[J][e] = 0;
     });
-    const int v = ch * kScanVecs + slot * 64 + lane;
-    float f[EPV];
-    tok_vec<E>(sel.rs, v, sel.V, f);
-    uint32_t w[EPV], n = 0;
-#pragma unroll
-    for (int e = 0; e < EPV; ++e)
-      if (TIES) n += order_key(f[e]) == cut.key ? 1 : 0;
-    u64 t = TIES ? tb + wave_scan((u64)n, lane) - n : 0, sum = 0;
-#pragma unroll
-    for (int e = 0; e < EPV; ++e) {
-      w[e] = kept(f[e], v * EPV + e);
-      if (TIES && order_key(f[e]) == cut.key) w[e] = t++ < cut.ties ? wt : 0;
-      sum += w[e];
-    }
-    const u64 upto = before + wave_scan(sum, lane);
-    if (upto > to && upto - sum <= to) {
-      u64 b = upto - sum;
-      bool found = false;
+    const int v0 = ch * kScanVecs + threadIdx.x * kChunkVecs;
+    each_in_chunk(ch, [&](const float (&f)[EPV], int v) {
 #pragma unroll
       for (int e = 0; e < EPV; ++e) {
-        if (!found && b + w[e] > to) {
-          found = true;
-          put_row(v * EPV + e, f[e], w[e], N);
-        }
-        b += w[e];
+        const uint32_t q = kept(f[e], v * EPV + e);
+        const bool tie = TIES && order_key(f[e]) == cut.key;
+        static_for<kChunkVecs>([&](auto J) {
+          if (j == J) {
+            w[J][e] = q;
+            l[J][e] = f[e];
+          }
+        });
+        n += tie ? 1 : 0;
+        sum += q;
       }
+      ++j;
+    });
+    if (TIES) {
+      __syncthreads();   // (every thread has read its own)
+      t += ahead(n, sh.u);
+      static_for<kChunkVecs>([&](auto J) {
+#pragma unroll
+        for (int e = 0; e < EPV; ++e)
+          if (threadIdx.x * kChunkVecs < kScanVecs && order_key(l[J][e]) == cut.key) {
+            w[J][e] = t++ < cut.ties ? wt : 0;
+            sum += w[J][e];
+          }
+      });
+    }
+    __syncthreads();
+    before += ahead(sum, sh.u);
+    if (before <= to && to < before + sum) {
+      bool found = false;
+      static_for<kChunkVecs>([&](auto J) {
+#pragma unroll
+        for (int e = 0; e < EPV; ++e) {
+          if (!found && before + w[J][e] > to) {
+            found = true;
+            put_row((v0 + J) * EPV + e, l[J][e], w[J][e], N);
+          }
+          before += w[J][e];
+        }
+      });
     }
   }
 
@@ -757,14 +797,13 @@ struct RowDraw {
   // Draws a row whose cut falls into a step: the step's kept tokens join the chunks' sums above it.
   // False where the list does not hold the step.
   __device__ __forceinline__ bool from_step(WideShared& ws) {
-    const int tid = threadIdx.x, lane = tid & 63, wid = tid >> 6;
-    constexpr int PT = LIST / BLOCK;
-    const int64_t at = row - a.row0;
-    const uint32_t n_step = a.steps[at].count;
-    const u64 left = a.steps[at].left;
+    const int tid = threadIdx.x, lane = tid & 63;
+    const int64_t which = row - a.row0;
+    const uint32_t n_step = a.steps[which].count;
+    const u64 left = a.steps[which].left;
     if (n_step > (uint32_t)a.step_ld || n_step > LIST) return false;
-    const int count = (int)n_step, step = a.steps[at].step;
-    const uint32_t* ids = a.step_ids + at * a.step_ld;
+    const int count = (int)n_step, step = a.steps[which].step;
+    const uint32_t* ids = a.step_ids + which * a.step_ld;
     for (int i = tid; i < count; i += BLOCK) {
       const int id = (int)ids[i];
       float f[EPV], fy = 0.f;
@@ -777,44 +816,40 @@ struct RowDraw {
     __syncthreads();
     sort_list<BLOCK>(sh.list, count);
     // the first tokens that reach `left`, of min_p's weight at least
+    const int per = (count + BLOCK - 1) / BLOCK, i0 = tid * per, i1 = i0 + per < count ? i0 + per : count;
     u64 s = 0;
-    for (int j = 0; j < PT && tid * PT + j < count; ++j)
-      s += weight(token_value(sh.list[tid * PT + j]));
-    u64 b = wave_scan(s, lane);
-    if (lane == 63) sh.u[wid] = b;
-    __syncthreads();
-    b -= s;
-    for (int w = 0; w < wid; ++w) b += sh.u[w];
-    u64 keep = 0;
-    for (int j = 0; j < PT && tid * PT + j < count; ++j) {
-      const uint32_t q = weight(token_value(sh.list[tid * PT + j]));
+    for (int i = i0; i < i1; ++i) s += weight(token_value(sh.list[i]));
+    u64 b = ahead(s, sh.u), keep = 0;
+    for (int i = i0; i < i1; ++i) {
+      const uint32_t q = weight(token_value(sh.list[i]));
       if (b < left && q >= p.least_w) {
         ++keep;
-        atomicAdd(&ws.mass[token_id(sh.list[tid * PT + j]) / (EPV * kScanVecs)], (u64)q);
+        atomicAdd(&ws.mass[token_id(sh.list[i]) / (EPV * kScanVecs)], (u64)q);
       }
       b += q;
     }
     __syncthreads();
     keep = block_sum<NW>(keep, sh.u);
-    if (tid >= 64) return true;
     const u64 last = keep > 0 ? sh.list[keep - 1] : ~u64(0);
-    u64 N = 0;
-    for (int i = lane; i < sel.nch; i += 64) N += ws.mass[i];
-    N = wave_sum(N);
-    u64 to = (u64)((double)p.u * (double)N);
-    if (to >= N) to = N - 1;
-    u64 before = 0;
-    int ch = 0;
-    for (int i0 = 0; i0 < sel.nch; i0 += 64) {
-      const u64 m = i0 + lane < sel.nch ? ws.mass[i0 + lane] : 0, upto = before + wave_scan(m, lane);
-      const u64 hit = __ballot(upto > to);
-      if (hit) {
-        const int who = __ffsll(hit) - 1;
-        ch = i0 + who;
-        before = __shfl(upto - m, who, 64);
-        break;
+    __syncthreads();
+    if (tid < 64) {
+      Place at{0, 0, 0, 0, 0};
+      for (int i = lane; i < sel.nch; i += 64) at.N += ws.mass[i];
+      at.N = wave_sum(at.N);
+      at.to = (u64)((double)p.u * (double)at.N);
+      if (at.to >= at.N) at.to = at.N - 1;
+      for (int i0 = 0; i0 < sel.nch; i0 += 64) {
+        const u64 m = i0 + lane < sel.nch ? ws.mass[i0 + lane] : 0,
+                  upto = at.before + wave_scan(m, lane), hit = __ballot(upto > at.to);
+        if (hit) {
+          const int who = __ffsll(hit) - 1;
+          at.ch = i0 + who;
+          at.before = __shfl(upto - m, who, 64);
+          break;
+        }
+        at.before = __shfl(upto, 63, 64);
       }
-      before = __shfl(upto, 63, 64);
+      if (lane == 0) put_place(at);
     }
     auto kept = [&](float f, int id) {
       const float t = draw_exponent(f, sel.M, p.c);
@@ -823,7 +858,7 @@ struct RowDraw {
       const bool in = st < step ? q >= p.least_w : st == step && token_of(f, id) >= last;
       return in ? q : 0u;
     };
-    in_chunk<false>(ch, before, to, N, kept, Cut{}, 0, 0);
+    in_chunk<false>(kept, Cut{}, 0);
     return true;
   }
 

@@ -77,10 +77,23 @@ __device__ __forceinline__ uint32_t take_place(bool take, uint32_t* counter, int
   return at;
 }
 
-// Bitonic sort, falling, of the list's next power of two (0 sorts last).
+// The list in falling order of its different entries: by counting those above each where there are
+// few (29 entries by 16 waves: 2.8 us in steps, 0.5 us counted), else a bitonic sort of the list's next
+// power of two (0 sorts last).
 template <int BLOCK>
 __device__ __forceinline__ void sort_list(u64* list, int count) {
   const int tid = threadIdx.x;
+  if (count <= 256) {
+    __syncthreads();
+    const u64 x = tid < count ? list[tid] : 0;
+    int at = 0;
+    if (tid < count)
+      for (int j = 0; j < count; ++j) at += list[j] > x ? 1 : 0;
+    __syncthreads();
+    if (tid < count) list[at] = x;
+    __syncthreads();
+    return;
+  }
   int P = 1;
   while (P < count) P <<= 1;
   for (int i = count + tid; i < P; i += BLOCK) list[i] = 0;
@@ -250,11 +263,21 @@ struct RowSelect {
     if (lane == 0) sh.f[wid] = least;
     __syncthreads();
     for (int w = 0; w < NW; ++w) least = fminf(least, sh.f[w]);
-    each_group([&](int g, float x) {
-      const bool take = x >= least;
-      const uint32_t at = take_place(take, &sh.groups, lane);
-      if (take && at < LIST / 2) sh.group[at] = (uint32_t)g;
-    });
+    {
+      uint32_t mine = 0;
+      each_group([&](int, float x) { mine += x >= least ? 1 : 0; });
+      const uint32_t upto = wave_scan(mine, lane);
+      uint32_t at = 0;
+      if (lane == 63 && upto) at = atomicAdd(&sh.groups, upto);
+      at = __builtin_amdgcn_readlane(at, 63) + upto - mine;
+      if (mine)
+        each_group([&](int g, float x) {
+          if (x >= least) {
+            if (at < LIST / 2) sh.group[at] = (uint32_t)g;
+            ++at;
+          }
+        });
+    }
     __syncthreads();
     const uint32_t ng = sh.groups;
     if (ng > LIST / 2) return false;
