@@ -245,24 +245,20 @@ struct RowSelect {
           lo = fminf(lo, (float)sh.d[w]);
         }
       __syncthreads();
-      if (!(finer || coarser) || hi == lo) break;
+      if (!(finer || coarser) || hi == lo) {
+        least = hi == lo ? lo : -FLT_MAX;   // (the last step has no end)
+        break;
+      }
       top = hi;
       prior = before;
       scale *= finer ? 16.f : 0.25f;
     }
-    // what is taken reaches the smallest of the groups' largest logits within the steps
-    least = INFINITY;
-    if (bin == 256)
-      least = -FLT_MAX;
-    else
-      each_group([&](int, float x) {
-        if (x > -INFINITY && (x > top || (uint32_t)below(x, top, scale, 255.f) <= bin))
-          least = fminf(least, x);
-      });
-    least = -wave_max(-least);
-    if (lane == 0) sh.f[wid] = least;
-    __syncthreads();
-    for (int w = 0; w < NW; ++w) least = fminf(least, sh.f[w]);
+    // what is taken reaches the steps' end, or falls a few roundings short of it: no group of the
+    // steps is left out
+    if (bin < 255) {
+      const float end = top - (float)(bin + 1) / scale * (1.f + 0x1p-20f);
+      least = fmaxf(end - fabsf(end) * 0x1p-22f, -FLT_MAX);
+    }
     {
       uint32_t mine = 0;
       each_group([&](int, float x) { mine += x >= least ? 1 : 0; });

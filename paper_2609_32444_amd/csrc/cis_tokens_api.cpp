@@ -196,7 +196,7 @@ DistillLayout distill_layout(int64_t T, int64_t V, int64_t K, int dtype) {
 
 // With the gradient, one workgroup per row, unless the rows are too few to fill the chip: then, and
 // without the gradient, in parts.
-bool few_rows(int64_t T, int32_t nvec) {
+bool distill_in_parts(int64_t T, int32_t nvec) {
   return T <= (nvec > 19456 ? 192 : nvec >= 12288 ? 112 : nvec >= 6144 ? 32 : 0);
 }
 
@@ -208,7 +208,7 @@ int launch_distill(const DistillCall& c, const DistillLayout& D, char* base, cis
         return rc;
     return (int)CIS_OK;
   };
-  if (c.bwd && !few_rows(c.T, a.r.nvec)) {
+  if (c.bwd && !distill_in_parts(c.T, a.r.nvec)) {
     const cis::DistillVariant v = cis::distill_fused(c.dtype, a.r.nvec, c.K);
     const int64_t resident = (int64_t)blocks_per_cu(v.fn, v.block) * cus;
     return launch(v.fn, c.T < resident ? c.T : resident, v.block, &a, stream);

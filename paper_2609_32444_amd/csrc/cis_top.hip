@@ -219,7 +219,8 @@ __global__ __launch_bounds__(BLOCK) __attribute__((amdgpu_waves_per_eu(4))) void
   }
 }
 
-// The list holds 8 K logits at least: all of a row of fewer groups than K.
+// The list holds 8 K logits at least: all of a row of fewer groups than K. (16 waves for few rows, whose
+// barriers wait for more of them: 96 rows, K = 8: 21.2 us for 21.5; a draw of one token 21.0 for 19.5.)
 int top_block(int64_t K) { return K <= 256 ? kTopBlock : kTokBlock; }
 const void* top_kernel(int dtype, int64_t K) {
 #define CIS_TOP(E)                                                                \
