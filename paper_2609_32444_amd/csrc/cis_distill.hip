@@ -10,7 +10,9 @@ namespace cis {
 // first NV vectors of every thread; longer rows read the rest a second time). The list goes into a
 // table in LDS, hashed by the vector that a token lies in, with chains, and every thread has a bit for
 // each of its vectors that holds one: the first sweep leaves the listed tokens out of its sum and notes
-// their logits, the second puts their gradients in.
+// their logits, the second puts their gradients in. Bound by the memory: 16384 rows of V = 151936 in
+// 1.83 ms (5.4 TB/s of reads and writes); the list's table and the loss by one wave lie between the
+// sweeps of a row, where the compute unit has no other row's loads to turn to.
 // ------------------------------------------------------------------------------------------
 template <int BLOCK, int KMAX>
 struct FusedShared {
@@ -31,7 +33,8 @@ __device__ __forceinline__ void lds_barrier() {
 }
 
 template <class E, int BLOCK, int NV, int KMAX>
-__global__ __launch_bounds__(BLOCK) __attribute__((amdgpu_waves_per_eu(4))) void cis_distill_kernel(const DistillArgs a) {
+__global__ __launch_bounds__(BLOCK) __attribute__((amdgpu_waves_per_eu(4))) void cis_distill_kernel(
+    const DistillArgs a) {
   constexpr int NW = BLOCK / 64, EPV = E::kPerVec;
   // vectors that are asked for before the list, and stay in flight ahead of sweep 1 (16384 rows of
   // V = 151936: 4 1981 us, 8 1902, 12 2056; 3001 of V = 50257: 142, 146, 153)
@@ -218,7 +221,8 @@ __global__ __launch_bounds__(BLOCK) __attribute__((amdgpu_waves_per_eu(4))) void
 // hold listed ones are read again, and taken out of the sums but for what else they hold (the sums
 // are in double, and a vector's sum is the same bits wherever it is formed). Where less than 2^-28
 // of the row remains, the row is summed again without the listed tokens. The vectors are found
-// in a table in LDS: open addressing, a key and the listed tokens of the vector as bits.
+// in a table in LDS: open addressing, a key and the listed tokens of the vector as bits. Bound by the
+// latency of a row's steps: 8192 rows, K = 64, in 14 us.
 // ------------------------------------------------------------------------------------------
 template <int KMAX>
 struct RowShared {
@@ -344,7 +348,7 @@ __global__ __launch_bounds__(64) void cis_distill_row_kernel(const DistillArgs a
 
 // ------------------------------------------------------------------------------------------
 // In parts, 3: the gradient by segments of kGradVecs vectors; listed tokens are put in by the segment
-// that they lie in, once its own stores are done.
+// that they lie in, once its own stores are done. 96 rows of V = 151936 in 12 us (4.7 TB/s).
 // ------------------------------------------------------------------------------------------
 template <class E>
 __global__ __launch_bounds__(kDistillGradBlock) void cis_distill_grad_kernel(const DistillArgs a) {

@@ -22,8 +22,9 @@ constexpr uint32_t kDrawOne = 1u << 28;
 
 // What a scan of the rows leaves in the workspace: the row in chunks of kScanVecs vectors (one wave's),
 // each with its largest logit m and the sum of exp2((z - m) c) over its tokens, added up in double
-// from the float32 sums of its vectors; and the largest logit of every group of `gv` vectors, in the logits' format. A chunk with a NaN or a +inf has a NaN sum;
-// one without tokens the largest logit -inf.
+// from the float32 sums of its vectors; and the largest logit of every group of `gv` vectors, in the
+// logits' format. A chunk with a NaN or a +inf has a NaN sum; one without tokens the largest logit
+// -inf.
 constexpr int kScanVecs = 512;
 constexpr int kScanBlock = 256;
 struct TokScan {

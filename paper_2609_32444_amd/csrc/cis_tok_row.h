@@ -204,41 +204,4 @@ __device__ __forceinline__ Cut radix_cut(__amdgpu_buffer_rsrc_t rs, int nvec, in
   return Cut{prefix, target};
 }
 
-// What a first sweep finds out about a row.
-struct RowFacts {
-  float M;        // its largest logit
-  bool finite;    // no NaN, no +inf
-  u64 tokens;
-};
-template <class E, int BLOCK>
-__device__ __forceinline__ RowFacts row_facts(__amdgpu_buffer_rsrc_t rs, int nvec, int V,
-                                              float* shf, u64* shu) {
-  constexpr int EPV = E::kPerVec, NW = BLOCK / 64;
-  float m = -INFINITY;
-  u64 n = 0, bad = 0;
-  for (int v = threadIdx.x; v < nvec; v += BLOCK) {
-    float f[EPV];
-    tok_vec<E>(rs, v, V, f);
-#pragma unroll
-    for (int e = 0; e < EPV; ++e) {
-      m = fmaxf(m, f[e]);
-      n += f[e] > -INFINITY ? 1 : 0;
-      bad += f[e] < INFINITY ? 0 : 1;   // NaN too
-    }
-  }
-  RowFacts r;
-  r.M = block_max<NW>(m, shf);
-  r.tokens = block_sum<NW>(n, shu);
-  __syncthreads();
-  r.finite = block_sum<NW>(bad, shu) == 0;
-  __syncthreads();
-  return r;
-}
-
-// The row in pieces of whole waves' loads that follow each other: at most kChunks of them.
-constexpr int kChunks = 256;
-__device__ __forceinline__ int chunk_vecs(int nvec) {
-  return (nvec + 64 * kChunks - 1) / (64 * kChunks) * 64;
-}
-
 }  // namespace cis
