@@ -2,6 +2,7 @@
 // parts (scan, one wave per row, gradient by segments) for the forward direction and for few rows.
 #include "cis_distill.h"
 #include "cis_select.h"
+#include "cis_stats.h"
 
 namespace cis {
 
@@ -217,7 +218,7 @@ __global__ __launch_bounds__(BLOCK) __attribute__((amdgpu_waves_per_eu(4))) void
 }
 
 // ------------------------------------------------------------------------------------------
-// In parts, 2: one wave per row. The scan has left the chunks' sums over all tokens; the vectors that
+// In parts, 2: NW waves per row (4 for few rows). The scan has left the chunks' sums over all tokens; the vectors that
 // hold listed ones are read again, and taken out of the sums but for what else they hold (the sums
 // are in double, and a vector's sum is the same bits wherever it is formed). Where less than 2^-28
 // of the row remains, the row is summed again without the listed tokens. The vectors are found
@@ -231,14 +232,17 @@ struct RowShared {
   uint32_t bits[kTable];
   uint16_t slot[KMAX];
   ListShared<KMAX> list;
+  Teacher teacher;
+  uint32_t u[4];
+  double d[4];
 };
 
-template <class E, bool BWD, int KMAX>
-__global__ __launch_bounds__(64) void cis_distill_row_kernel(const DistillArgs a) {
-  constexpr int EPV = E::kPerVec;
+template <class E, bool BWD, int KMAX, int NW>
+__global__ __launch_bounds__(64 * NW) void cis_distill_row_kernel(const DistillArgs a) {
+  constexpr int EPV = E::kPerVec, BLOCK = 64 * NW;
   typedef RowShared<KMAX> Shared;
   __shared__ Shared sh;
-  const int lane = threadIdx.x;
+  const int tid = threadIdx.x, lane = tid & 63, wid = __builtin_amdgcn_readfirstlane(tid) >> 6;
   const int V = a.r.V, nvec = a.r.nvec, K = a.K, nch = a.s.nch;
   const float c = a.c;
   const int64_t row = a.row0 + blockIdx.x;
@@ -246,11 +250,11 @@ __global__ __launch_bounds__(64) void cis_distill_row_kernel(const DistillArgs a
   const float* cmax = a.s.cmax + row * nch;
   const double* csum = a.s.csum + row * nch;
   uint32_t seen = 0, wrong = 0;
-  for (int i = lane; i < Shared::kTable; i += 64) sh.key[i] = kNone;
-  for (int i = lane; i < Shared::kTable; i += 64) sh.bits[i] = 0;
-  __syncthreads();   // (one wave)
+  for (int i = tid; i < Shared::kTable; i += BLOCK) sh.key[i] = kNone;
+  for (int i = tid; i < Shared::kTable; i += BLOCK) sh.bits[i] = 0;
+  __syncthreads();
   if (on)
-    for (int k = lane; k < K; k += 64) {
+    for (int k = tid; k < K; k += BLOCK) {
       const int32_t id = a.ids[row * a.ld_top + k];
       sh.list.lq[k] = a.values[row * a.ld_top + k];
       const bool in = id >= 0 && id < V;
@@ -270,10 +274,9 @@ __global__ __launch_bounds__(64) void cis_distill_row_kernel(const DistillArgs a
         wrong += id != -1 ? 1 : 0;
       }
     }
-  seen = wave_sum(seen);
-  const bool bad = wave_sum(wrong) != 0, valid = on && !bad && seen != 0;
+  seen = block_sum<NW>(seen | wrong << 16, sh.u);   // (K entries at most, in each)
+  const bool bad = seen >> 16 != 0, valid = on && !bad && seen != 0;
   Student st{0.f, RestGrad{INFINITY, 0u}, true};
-  __syncthreads();
   if (valid) {
     const __amdgpu_buffer_rsrc_t rs = tok_rsrc(a.r, row);
     float M = -INFINITY;
@@ -283,7 +286,11 @@ __global__ __launch_bounds__(64) void cis_distill_row_kernel(const DistillArgs a
     for (int i = lane; i < nch; i += 64)
       if (!(cmax[i] == -INFINITY && csum[i] == 0.0))
         whole += csum[i] * (double)fast_exp2((cmax[i] - M) * c);
-    for (int k = lane; k < K; k += 64) {
+    if (wid == NW - 1) {
+      const Teacher t = teacher_list(a, row_tail(a, row), sh.list, lane);
+      if (lane == 0) sh.teacher = t;
+    }
+    for (int k = tid; k < K; k += BLOCK) {
       const int id = sh.list.id[k];
       if (id < 0) continue;
       const int v = id / EPV;
@@ -301,7 +308,8 @@ __global__ __launch_bounds__(64) void cis_distill_row_kernel(const DistillArgs a
         less += ((double)all - (double)vec_sum<E>(f, c, m)) * (double)fast_exp2((m - M) * c);
     }
     whole = wave_sum(whole);
-    double rest = whole - wave_sum(less);
+    double rest = whole - block_sum<NW>(less, sh.d);
+    if (wid != 0) return;   // (no barrier follows)
     float R = fmaxf(M * c, kMinExp), s;
     // rest is relative to M; the loss takes it relative to 2^R
     const float shift = fast_exp2(__builtin_fmaf(M, c, -R));
@@ -332,9 +340,9 @@ __global__ __launch_bounds__(64) void cis_distill_row_kernel(const DistillArgs a
       }
       wave_lse(R, s);
     }
-    const Teacher t = teacher_list(a, row_tail(a, row), sh.list, lane);
-    st = student_list<E, BWD>(a, row_weight(a, row), sh.list, lane, t, R, s);
+    st = student_list<E, BWD>(a, row_weight(a, row), sh.list, lane, sh.teacher, R, s);
   }
+  if (wid != 0) return;
   if (lane == 0) put_row(a, row, st.term, valid, on && bad, st.finite);
   if (BWD) {
     if (lane == 0) {
@@ -348,7 +356,8 @@ __global__ __launch_bounds__(64) void cis_distill_row_kernel(const DistillArgs a
 
 // ------------------------------------------------------------------------------------------
 // In parts, 3: the gradient by segments of kGradVecs vectors; listed tokens are put in by the segment
-// that they lie in, once its own stores are done. 96 rows of V = 151936 in 12 us (4.7 TB/s).
+// that they lie in, once its own stores are done. The first workgroup sums up the call's statistics
+// too: there are few rows, and they were done before the launch. 96 rows of V = 151936 in 12 us (4.7 TB/s).
 // ------------------------------------------------------------------------------------------
 template <class E>
 __global__ __launch_bounds__(kDistillGradBlock) void cis_distill_grad_kernel(const DistillArgs a) {
@@ -375,13 +384,21 @@ __global__ __launch_bounds__(kDistillGradBlock) void cis_distill_grad_kernel(con
       for (int e = 0; e < a.r.V - v * EPV; ++e)
         E::store_elem(grow, v * EPV + e, E::elem_bits(out, e));
   });
-  if (!valid) return;
-  asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
-  __syncthreads();
-  for (int k = tid; k < a.K; k += BLOCK) {
-    const int id = a.ids[row * a.ld_top + k];
-    if (id >= 0 && id / EPV / kDistillGradVecs == seg) E::store_elem(grow, id, a.grads[row * a.K + k]);
+  if (valid) {
+    asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
+    __syncthreads();
+    for (int k = tid; k < a.K; k += BLOCK) {
+      const int id = a.ids[row * a.ld_top + k];
+      if (id >= 0 && id / EPV / kDistillGradVecs == seg)
+        E::store_elem(grow, id, a.grads[row * a.K + k]);
+    }
   }
+  if (b != 0) return;
+  RowStats st{};
+  for (int64_t t = tid; t < a.r.T; t += BLOCK)
+    take_row(st, a.terms_ws[t], a.flags_ws[t], a.logk_ws[t], a.excess_ws[t]);
+  st = block_stats<BLOCK>(st);
+  if (tid == 0) write_stats(a.fin, st);
 }
 
 // Variants of the fused pass: the first that holds a row. 1024 x 19 vectors take 76 of a thread's
@@ -410,14 +427,17 @@ DistillVariant distill_fused(int dtype, int32_t nvec, int64_t K) {
   return DistillVariant{t[i].block, K <= 256 ? t[i].few : t[i].many};
 }
 
-const void* distill_row_kernel(int dtype, bool bwd, int64_t K) {
-#define CIS_ROW(E, B)                                                 \
-  (K <= 64 ? (const void*)&cis_distill_row_kernel<E, B, 64>           \
-   : K <= 256 ? (const void*)&cis_distill_row_kernel<E, B, 256>       \
-              : (const void*)&cis_distill_row_kernel<E, B, CIS_TOP_MAX_K>)
+// (96 rows of V = 151936, K = 256: 8.5 us by 4 waves a row, 11.5 by one)
+const void* distill_row_kernel(int dtype, bool bwd, int64_t K, bool few) {
+#define CIS_ROW_N(E, B, N)                                               \
+  (K <= 64 ? (const void*)&cis_distill_row_kernel<E, B, 64, N>           \
+   : K <= 256 ? (const void*)&cis_distill_row_kernel<E, B, 256, N>       \
+              : (const void*)&cis_distill_row_kernel<E, B, CIS_TOP_MAX_K, N>)
+#define CIS_ROW(E, B) (few ? CIS_ROW_N(E, B, 4) : CIS_ROW_N(E, B, 1))
   if (dtype == CIS_BF16) return bwd ? CIS_ROW(Bf16, true) : CIS_ROW(Bf16, false);
   return bwd ? CIS_ROW(F32, true) : CIS_ROW(F32, false);
 #undef CIS_ROW
+#undef CIS_ROW_N
 }
 const void* distill_grad_kernel(int dtype) {
   return dtype == CIS_BF16 ? (const void*)&cis_distill_grad_kernel<Bf16>

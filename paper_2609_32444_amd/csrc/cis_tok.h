@@ -139,6 +139,7 @@ struct DistillArgs {
   uint8_t* flags_ws;
   float* logk_ws;
   float* excess_ws;
+  FinalizeArgs fin;           // in parts with the gradient: where the statistics go
 };
 
 constexpr int kTokBlock = 1024;
@@ -160,7 +161,8 @@ struct DistillVariant {
 };
 // The fused pass for rows of nvec vectors, and the kernels of the pass in parts.
 DistillVariant distill_fused(int dtype, int32_t nvec, int64_t K);
-const void* distill_row_kernel(int dtype, bool bwd, int64_t K);
+// few: rows that do not fill the chip with a wave each
+const void* distill_row_kernel(int dtype, bool bwd, int64_t K, bool few);
 const void* distill_grad_kernel(int dtype);
 
 }  // namespace cis

@@ -90,6 +90,8 @@ cis::ScanLayout top_layout(int64_t T, int64_t V, int64_t K, int dtype) {
 constexpr int64_t kMaxBlocks = int64_t(1) << 23;
 // Rows of a distillation call that may go in parts with the gradient.
 constexpr int64_t kFewRows = 192;
+// Rows up to which cis_distill_row_kernel gives a row 4 waves: two such workgroups per compute unit.
+constexpr int64_t kWaveRows = 512;
 // Logits that a draw may have to look at where its parameters do not say.
 constexpr int64_t kManyLogits = 256;
 
@@ -138,14 +140,18 @@ constexpr int64_t kMaxRows = int64_t(1) << 20;
 // Temperatures of a softmax: log2(e) / temperature and a logit's exponent stay within float32.
 bool softmax_temperature(float t) { return t >= 0x1p-64f && t <= 0x1p64f; }
 
+cis::FinalizeArgs finalize_args(char* base, const cis::WsLayout& L, int64_t T, float* loss_out) {
+  auto f = [&](size_t off) { return reinterpret_cast<float*>(base + off); };
+  return cis::FinalizeArgs{f(L.terms), reinterpret_cast<uint8_t*>(base + L.flags), f(L.logk),
+                           f(L.excess), T, reinterpret_cast<cis_stats_t*>(base), loss_out, nullptr,
+                           reinterpret_cast<cis::RowStats*>(base + L.wpre), 0, 0};
+}
+
 // The call's statistics and loss, as in the loss entry points: few rows by one workgroup, more
 // by one per part and another over the parts (at wpre, which nothing else uses here).
 int launch_finalize(char* base, const cis::WsLayout& L, int64_t T, float* loss_out,
                     hipStream_t stream) {
-  auto f = [&](size_t off) { return reinterpret_cast<float*>(base + off); };
-  cis::FinalizeArgs fa{f(L.terms), reinterpret_cast<uint8_t*>(base + L.flags), f(L.logk),
-                       f(L.excess), T, reinterpret_cast<cis_stats_t*>(base), loss_out, nullptr,
-                       reinterpret_cast<cis::RowStats*>(base + L.wpre), 0, 0};
+  cis::FinalizeArgs fa = finalize_args(base, L, T, loss_out);
   if (T <= cis::kFinalizeOne) {
     const int block = T <= cis::kFinalizeSmall ? 256 : cis::kFinalizeBlock;
     return launch(cis::finalize_kernel(block, false), 1, block, &fa, stream);
@@ -219,7 +225,9 @@ int launch_distill(const DistillCall& c, const DistillLayout& D, char* base, cis
   a.grads = reinterpret_cast<uint32_t*>(base + D.grads);
   a.nseg = (a.r.nvec + cis::kDistillGradVecs - 1) / cis::kDistillGradVecs;
   if (int rc = launch_scan(a.r, a.s, c.dtype, a.c, stream)) return rc;
-  if (int rc = by_rows(cis::distill_row_kernel(c.dtype, c.bwd, c.K), 64, c.T)) return rc;
+  const bool few = c.T <= kWaveRows;
+  if (int rc = by_rows(cis::distill_row_kernel(c.dtype, c.bwd, c.K, few), few ? 256 : 64, c.T))
+    return rc;
   if (!c.bwd) return CIS_OK;
   return by_rows(cis::distill_grad_kernel(c.dtype), cis::kDistillGradBlock, c.T * a.nseg);
 }
@@ -275,7 +283,9 @@ int run_distill(const DistillCall& c, hipStream_t stream) {
     a.logk_ws = reinterpret_cast<float*>(base + L.logk);
     a.excess_ws = reinterpret_cast<float*>(base + L.excess);
     a.c = cis::scan_c(p.temperature);
+    a.fin = finalize_args(base, L, c.T, c.loss);
     if (int rc = launch_distill(c, D, base, a, cus, stream)) return rc;
+    if (c.bwd && distill_in_parts(c.T, a.r.nvec)) return CIS_OK;   // (the last kernel sums up)
   }
   return launch_finalize(base, L, c.T, c.loss, stream);
 }
