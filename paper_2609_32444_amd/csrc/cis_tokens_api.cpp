@@ -89,7 +89,7 @@ cis::ScanLayout top_layout(int64_t T, int64_t V, int64_t K, int dtype) {
 // Workgroups of 256 threads per launch of kernels that loop beyond (HIP refuses 2^32 work items).
 constexpr int64_t kMaxBlocks = int64_t(1) << 23;
 // Rows of a distillation call that may go in parts with the gradient.
-constexpr int64_t kFewRows = 192;
+constexpr int64_t kFewRows = 448;
 // Rows up to which cis_distill_row_kernel gives a row 4 waves: two such workgroups per compute unit.
 constexpr int64_t kWaveRows = 512;
 // Logits that a draw may have to look at where its parameters do not say.
@@ -200,10 +200,22 @@ DistillLayout distill_layout(int64_t T, int64_t V, int64_t K, int dtype) {
   return D;
 }
 
-// With the gradient, one workgroup per row, unless the rows are too few to fill the chip: then, and
-// without the gradient, in parts.
+// With the gradient, one workgroup per row, unless the rows are too few for that: then, and without
+// the gradient, in parts. The bounds follow the fused pass's ladder (distill_fused): rows that a wave
+// holds 10 or 18 vectors a thread of, those of 256 threads from 12 vectors and 512 threads of 10, and
+// longer ones, which take half of a compute unit and all of it. K = 64, bf16, us in parts and fused:
+//   V = 4096   448 rows 17, 20      V = 20000  320 rows 19, 21; 448 rows 22, 21
+//   V = 50264  112 rows 18, 20; 192 rows 22, 22; 256 rows 25, 21
+//   V = 151936 64 rows 20, 31; 112 rows 29, 31; 160 rows 34, 31
+//   V = 1024   64 rows 15, 14       V = 10000  64 rows 16, 15
 bool distill_in_parts(int64_t T, int32_t nvec) {
-  return T <= (nvec > 19456 ? 192 : nvec >= 12288 ? 112 : nvec >= 6144 ? 32 : 0);
+  const int64_t most = nvec <= 320    ? 0
+                       : nvec <= 1152 ? 448
+                       : nvec <= 2048 ? 0
+                       : nvec <= 5120 ? 320
+                       : nvec <= 8704 ? 144
+                                      : 112;
+  return T <= most;
 }
 
 int launch_distill(const DistillCall& c, const DistillLayout& D, char* base, cis::DistillArgs& a,
