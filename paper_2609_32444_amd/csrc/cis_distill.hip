@@ -1,5 +1,5 @@
 // Distillation kernels (gfx950): a fused pass that holds a row on the compute unit, and a pass in
-// parts (scan, one wave per row, gradient by segments) for the forward direction and for few rows.
+// parts (scan, a wave per row or four, gradient by segments) for the forward direction and for few rows.
 #include "cis_distill.h"
 #include "cis_select.h"
 #include "cis_stats.h"

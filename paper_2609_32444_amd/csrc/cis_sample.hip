@@ -16,8 +16,6 @@
 
 namespace cis {
 
-constexpr int kDrawK = 1024;
-
 struct RowParams {
   float u, temp, top_p, min_p;
   int64_t top_k;   // V: no limit

@@ -145,8 +145,10 @@ struct DistillArgs {
 constexpr int kTokBlock = 1024;
 constexpr int kTopBlock = 256;
 constexpr int kWeighBlock = 256;
+constexpr int kDrawK = 1024;      // top_k up to which a row is drawn from a list
 constexpr int kDrawListK = 128;   // top_k that the kernel for short lists takes
-const void* scan_kernel(int dtype, int32_t gv);
+// keep: the logits stay in the caches for a later kernel's read
+const void* scan_kernel(int dtype, int32_t gv, bool keep);
 // wide: any parameters; else top_k in [1, 128] for every row or nothing to cut but min_p
 const void* sample_kernel(int dtype, bool wide);
 const void* weigh_kernel(int dtype, bool step);

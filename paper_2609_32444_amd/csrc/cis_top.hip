@@ -8,11 +8,11 @@ namespace cis {
 // One wave per chunk of kScanVecs vectors, 8 of them per lane: the chunk's largest logit, the sum of
 // its exponentials relative to that, and the groups' largest logits (TokScan). Reads the logits
 // once; the workgroups are short-lived and many, which suits a read-only stream here. Bound by the
-// memory: 6000 rows of V = 151936 in 288 us (6.3 TB/s), 512 rows in 28 us (5.5 TB/s); the loads are
-// marked as not used again, which costs a draw's second read of 512 rows 2 us and saves 54 us of
-// the 6000 rows'.
+// memory: 6000 rows of V = 151936 in 288 us (6.3 TB/s), 512 rows in 24 us (6.4 TB/s). Loads of more
+// logits than the memory-side cache holds are marked as not used again (6000 rows, K = 256: 54 us
+// less); those of fewer are not (512 uncut rows, which are read again: 70 to 65 us).
 // ------------------------------------------------------------------------------------------
-template <class E, int GV>
+template <class E, int GV, int AUX>
 __global__ __launch_bounds__(kScanBlock) void cis_scan_kernel(const ScanArgs a) {
   constexpr int EPV = E::kPerVec, K = kScanSlots, NW = kScanBlock / 64;
   const int lane = threadIdx.x & 63, wid = __builtin_amdgcn_readfirstlane(threadIdx.x) >> 6;
@@ -25,7 +25,7 @@ __global__ __launch_bounds__(kScanBlock) void cis_scan_kernel(const ScanArgs a) 
     const __amdgpu_buffer_rsrc_t rs = tok_rsrc(a.r, row);
     const int v0 = ch * kScanVecs + lane;
     u32x4 x[K];
-    load_chunk<E, kAuxNT>(rs, a.r, ch, lane, x);
+    load_chunk<E, AUX>(rs, a.r, ch, lane, x);
     float m8[K], m = -INFINITY;
     static_for<K>([&](auto I) {
       float f[EPV];
@@ -74,12 +74,14 @@ __global__ __launch_bounds__(kScanBlock) void cis_scan_kernel(const ScanArgs a) 
   }
 }
 
-const void* scan_kernel(int dtype, int32_t gv) {
-#define CIS_SCAN(E)                                                                      \
-  (gv == 0 ? (const void*)&cis_scan_kernel<E, 0>                                         \
-           : gv == 1 ? (const void*)&cis_scan_kernel<E, 1> : (const void*)&cis_scan_kernel<E, 8>)
+const void* scan_kernel(int dtype, int32_t gv, bool keep) {
+#define CIS_SCAN_G(E, G)                                       \
+  (keep ? (const void*)&cis_scan_kernel<E, G, 0>               \
+        : (const void*)&cis_scan_kernel<E, G, kAuxNT>)
+#define CIS_SCAN(E) (gv == 0 ? CIS_SCAN_G(E, 0) : gv == 1 ? CIS_SCAN_G(E, 1) : CIS_SCAN_G(E, 8))
   return dtype == CIS_BF16 ? CIS_SCAN(Bf16) : CIS_SCAN(F32);
 #undef CIS_SCAN
+#undef CIS_SCAN_G
 }
 
 // ------------------------------------------------------------------------------------------
