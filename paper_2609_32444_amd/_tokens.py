@@ -152,10 +152,23 @@ def _check_top(name, t, T, K, dtype, dev):
         raise ValueError(f"{name} must have unit column stride")
 
 
+def _list_stride(ids, values, T, K):
+    """Row stride of the lists, as the library takes it: K entries of a row never share storage
+    with another row's. (That of a single row never moves an address.)"""
+    if T <= 1:
+        return K
+    if ids.stride(0) != values.stride(0):
+        raise ValueError("top_ids and top_values must have the same row stride")
+    if ids.stride(0) < K:
+        raise ValueError(f"the rows of top_ids and top_values must not share storage (expanded "
+                         f"lists need a contiguous copy): row stride {ids.stride(0)}, K {K}")
+    return ids.stride(0)
+
+
 class DistillCall(_Call):
     """KL between a teacher's lists and the student's logits (cis_distill_fwd, or with bwd=True
     cis_distill_bwd). top_ids [T, K] int32 and top_values [T, K] float32 as TopLogitsCall leaves
-    them; tail [T] its tail, or None: the teacher is its list alone (KL_FORWARD only); row_weight [T]
+    them, or the first columns of longer ones (of one row stride, K at least); tail [T] its tail, or None: the teacher is its list alone (KL_FORWARD only); row_weight [T]
     float32 or None. run() returns "terms" [T], "loss" [1] (their sum) and with bwd "dlogits"; the
     workspace holds the statistics (read_stats)."""
 
@@ -170,9 +183,7 @@ class DistillCall(_Call):
         K = top_ids.shape[1]
         _check_top("top_ids", top_ids, T, K, torch.int32, dev)
         _check_top("top_values", top_values, T, K, torch.float32, dev)
-        ld_top = max(top_ids.stride(0), K)
-        if T > 1 and top_ids.stride(0) != top_values.stride(0):
-            raise ValueError("top_ids and top_values must have the same row stride")
+        ld_top = _list_stride(top_ids, top_values, T, K)
         _check_vec("tail", tail, T, torch.float32, dev, optional=True)
         _check_vec("row_weight", row_weight, T, torch.float32, dev, optional=True)
         mask = _check_vec("mask", _mask_u8(mask), T, torch.uint8, dev, optional=True)

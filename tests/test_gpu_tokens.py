@@ -677,3 +677,18 @@ def test_rows_beyond_4_gib():
     _check_distill(logits[-3:], ids, values, tail, sub)
     assert (out["dlogits"][-3:].float() - sub["dlogits"].float()).abs().max() < 1e-2
     assert (out["terms"][-3:] - sub["terms"]).abs().max() < TOL
+
+
+def test_shared_lists_are_refused():
+    """Lists that all rows share have the storage of one row."""
+    T, V, K = 5, 64, 4
+    z = torch.zeros(T, V, device=DEV)
+    ids = torch.arange(K, dtype=torch.int32, device=DEV).expand(T, K)
+    values = torch.zeros(K, device=DEV).expand(T, K)
+    for call in (cis.distill_fwd, cis.distill_bwd):
+        with pytest.raises(ValueError, match="share storage"):
+            call(z, ids, values)
+    out = cis.distill_fwd(z, ids.contiguous(), values.contiguous())
+    _check_distill(z, ids, values, None, out)
+    out = cis.distill_fwd(z[:1], ids[:1], values[:1])
+    _check_distill(z[:1], ids[:1], values[:1], None, out)

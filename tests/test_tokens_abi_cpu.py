@@ -158,3 +158,26 @@ def test_binding_rejects_wrong_tensors():
         cis.top_logits(z, 4)
     with pytest.raises(ValueError):
         cis.distill_fwd(z, torch.zeros(2, 3, dtype=torch.int32), torch.zeros(2, 3))
+
+
+def test_lists_whose_rows_share_storage_are_refused():
+    """The kernels read entry t * ld_top + k: no list passes whose storage ends before that."""
+    T, K = 5, 4
+    base = torch.zeros(T * 8, dtype=torch.int32)
+
+    def lists(step, rows=T):
+        return (base.as_strided((rows, K), (step, 1)),
+                base.float().as_strided((rows, K), (step, 1)))
+
+    for step in (K, K + 1, 8):
+        ld = _tokens._list_stride(*lists(step), T, K)
+        assert ld == step and (T - 1) * ld + K <= base.numel()
+    for step in (0, 1, K - 1):
+        with pytest.raises(ValueError, match="share storage"):
+            _tokens._list_stride(*lists(step), T, K)
+    with pytest.raises(ValueError, match="same row stride"):
+        _tokens._list_stride(lists(8)[0], lists(K)[1], T, K)
+    # one row, or none: its stride never moves an address
+    for rows in (0, 1):
+        for step in (0, 1, 8):
+            assert _tokens._list_stride(*lists(step, rows), rows, K) == K
