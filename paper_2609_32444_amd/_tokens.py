@@ -90,6 +90,14 @@ def _per_row(name, x, T, dtype, dev):
     return x, None
 
 
+def _top_k(k):
+    """top_k as the library's int32 (a ctypes field takes the low bits of a larger one)."""
+    k = int(k)
+    if not -2 ** 31 <= k < 2 ** 31:
+        raise ValueError(f"top_k must be an int32, got {k}")
+    return k
+
+
 class SampleCall(_Call):
     """One token per row of logits, drawn with the random numbers u [T] float32 (cis_sample).
 
@@ -109,7 +117,7 @@ class SampleCall(_Call):
         top_p, ps = _per_row("top_p", top_p, T, torch.float32, dev)
         min_p, ms = _per_row("min_p", min_p, T, torch.float32, dev)
         self._prm = _SampleParams(1.0 if temperature is None else float(temperature),
-                                  0 if top_k is None else int(top_k),
+                                  0 if top_k is None else _top_k(top_k),
                                   1.0 if top_p is None else float(top_p),
                                   0.0 if min_p is None else float(min_p))
         self._keep = (logits, u, mask, temps, ks, ps, ms)

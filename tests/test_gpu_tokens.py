@@ -692,3 +692,8 @@ def test_shared_lists_are_refused():
     _check_distill(z, ids, values, None, out)
     out = cis.distill_fwd(z[:1], ids[:1], values[:1])
     _check_distill(z[:1], ids[:1], values[:1], None, out)
+
+
+def test_top_k_beyond_int32_is_refused():
+    with pytest.raises(ValueError, match="int32"):
+        cis.sample(torch.zeros(2, 64, device=DEV), torch.zeros(2, device=DEV), top_k=2 ** 32 + 5)
