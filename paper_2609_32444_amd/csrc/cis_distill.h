@@ -1,17 +1,16 @@
 // What the distillation kernels share: a row's list as a table that the sweeps look its tokens up
 // in, and the arithmetic of the loss on the classes {listed tokens, everything else}.
 //
-// The sums are kept in units of log2: with c = log2(e) / temperature a logit z has the exponent
-// z c, a reference R is itself a rounded exponent, and exp2(fma(z, c, -R)) rounds once; what R
-// rounds off cancels, because total = 2^R sum is formed with the same R.
+// Every exponent is that of a difference of logits, (z - m) c with c = log2(e) / temperature and m the
+// largest logit of the sum: as large as the difference is, wherever the logits lie, and finite sums for
+// every temperature. (fma(z, c, -m c) is an instruction less, but m c rounds at its own size: 3e-6 of
+// every value for logits near 100, and sums of 0 or inf once it is off by 128, at temperatures of 1e-8.)
 #pragma once
 
 #include "cis_tok_row.h"
 
 namespace cis {
 
-// Lowest reference of a row's sum: finite where there is nothing but -inf.
-constexpr float kMinExp = -0x1p126f;
 constexpr float kLn2 = 0.693147180559945309417f;
 // expm1(d) - d for |d| <= kNearLog by its series (which does not cancel): nine terms, the first left
 // out below 2^-24 of the sum.
@@ -35,6 +34,14 @@ __device__ __forceinline__ float log_rest(float list, float rest) {
   return rest > 0.5f * total ? log1pf(-list / total) : logf(rest / total);
 }
 
+// Log of the share of a token x below the largest, of a total of 2^L. (In units of log2, that of the
+// type's lowest logit would be past float32.) Teacher and student round alike here: shares of the same
+// logits are the same bits.
+__device__ __forceinline__ float log_share(float x, float inv_t, float L) {
+#pragma clang fp contract(off)
+  return x * inv_t - L * kLn2;
+}
+
 // A class's part of sum a log(a/b) for log a - log b = d: a log(a/b) - a + b >= 0, where a and b are
 // near each other from the series, since the terms cancel there; b at a = 0.
 __device__ __forceinline__ float kl_part(float a, float d, float b) {
@@ -42,9 +49,13 @@ __device__ __forceinline__ float kl_part(float a, float d, float b) {
   return fabsf(d) <= kNearLog ? a * expm1_less(-d) : __builtin_fmaf(a, d, b - a);
 }
 
-__device__ __forceinline__ RestGrad rest_grad(float coef, float R, float total) {
-  const float b2 = coef != 0.f ? (R + log2f(total)) - log2f(fabsf(coef)) : INFINITY;
-  return RestGrad{b2, coef < 0.f ? 1u : 0u};
+// The gradient of a class as a factor for its tokens, whose exponentials relative to m sum up to s. A
+// factor above 1 leaves its power of two to the exponent: only a gradient below 2^-126 is flushed.
+__device__ __forceinline__ RestGrad rest_grad(float grad, float m, float s) {
+  const float g = grad == 0.f || s == 0.f ? 0.f : grad / s;
+  int up = __builtin_amdgcn_frexp_expf(g);   // (0 for inf and NaN)
+  up = up > 0 ? up : 0;
+  return RestGrad{m, (float)up, __builtin_amdgcn_ldexpf(g, -up)};
 }
 
 // Gradient coefficients (before scale * weight / temperature) of a listed token and, of p_j, of the
@@ -104,49 +115,52 @@ __device__ __forceinline__ float row_weight(const DistillArgs& a, int64_t row) {
 template <int KMAX>
 __device__ __forceinline__ Teacher teacher_list(const DistillArgs& a, float tail,
                                                 ListShared<KMAX>& sh, int lane) {
-  const float c = a.c;
-  tail *= kLog2e;
   float m = -INFINITY;
   each_entry(sh.id, a.K, lane, [&](int k) { m = fmaxf(m, sh.lq[k]); });
-  const float R = fmaxf(fmaxf(wave_max(m) * c, tail), kMinExp);
+  m = wave_max(m);
+  // the tail beside the list's largest: their difference in double, since each is rounded at its own
+  // size. Where the tail is the larger one, all are relative to it.
+  float t = tail < INFINITY ? m > -INFINITY ? (float)((double)tail - (double)m * a.inv_t64)
+                              : tail > -INFINITY ? 0.f : -INFINITY
+                            : NAN;
+  const float above = t > 0.f ? t : 0.f;
+  if (t > 0.f) t = 0.f;
+  m = sum_ref(m);
   float s = 0.f;
-  each_entry(sh.id, a.K, lane, [&](int k) {
-    const float x = __builtin_fmaf(sh.lq[k], c, -R);
-    s += fast_exp2(x);
-    sh.lq[k] = x;
-  });
+  const float c = a.c, up = above * kLog2e;
+  each_entry(sh.id, a.K, lane, [&](int k) { s += fast_exp2((sh.lq[k] - m) * c - up); });
   s = wave_sum(s);
-  const float rest = fast_exp2(tail - R), total = s + rest, L = log2f(total);
+  const float rest = fast_exp2(t * kLog2e), total = s + rest, L = log2f(total);
   each_entry(sh.id, a.K, lane, [&](int k) {
-    const float x = sh.lq[k] - L;
-    sh.lq[k] = x * kLn2;
-    sh.q[k] = fast_exp2(x);
+    const float x = sh.lq[k] - m;
+    sh.q[k] = fast_exp2((x * c - up) - L);
+    sh.lq[k] = log_share(x, a.inv_t, L) - above;
   });
   return Teacher{rest / total, log_rest(s, rest), total > 0.f && total < INFINITY};
 }
 
-// The loss of a row whose listed logits are at sh.z and whose other tokens sum up to rest 2^R, and with
-// BWD its gradient: of the listed tokens at sh.grad.
+// The loss of a row whose listed logits are at sh.z and whose other tokens' exponentials relative to
+// m_rest sum up to s_rest, and with BWD its gradient: of the listed tokens at sh.grad.
 template <class E, bool BWD, int KMAX>
 __device__ __forceinline__ Student student_list(const DistillArgs& a, float weight,
                                                 ListShared<KMAX>& sh, int lane, const Teacher& t,
-                                                float R, float rest) {
+                                                float m_rest, float s_rest) {
   const float c = a.c;
   const bool reverse = a.reverse != 0;
   float m = -INFINITY;
   each_entry(sh.id, a.K, lane, [&](int k) { m = fmaxf(m, sh.z[k]); });
-  const float Rs = fmaxf(R, wave_max(m) * c);
-  rest *= fast_exp2(R - Rs);
+  m = fmaxf(m_rest, wave_max(m));
   float s = 0.f;
-  each_entry(sh.id, a.K, lane, [&](int k) { s += fast_exp2(__builtin_fmaf(sh.z[k], c, -Rs)); });
+  each_entry(sh.id, a.K, lane, [&](int k) { s += fast_exp2((sh.z[k] - m) * c); });
   s = wave_sum(s);
+  const float rest = s_rest * fast_exp2((m_rest - m) * c);
   const float total = s + rest, L = log2f(total);
   const float p_rest = rest / total, d_rest = log_rest(s, rest) - t.log_rest;
   // (the logits' exponents are formed once more for the gradient: nothing else of the entry is kept)
   auto share = [&](int k, float& p) {
-    const float x = __builtin_fmaf(sh.z[k], c, -Rs) - L;
-    p = fast_exp2(x);
-    return x * kLn2 - sh.lq[k];   // log p - log q
+    const float x = sh.z[k] - m;
+    p = fast_exp2(x * c - L);
+    return log_share(x, a.inv_t, L) - sh.lq[k];   // log p - log q
   };
   float kl = 0.f;
   each_entry(sh.id, a.K, lane, [&](int k) {
@@ -162,7 +176,7 @@ __device__ __forceinline__ Student student_list(const DistillArgs& a, float weig
   Student out;
   out.term = w == 0.f ? 0.f : w * kl;
   out.finite = isfinite(kl) && isfinite(out.term);
-  out.rest = RestGrad{INFINITY, 0u};
+  out.rest = RestGrad{0.f, 0.f, 0.f};
   if (BWD) {
     const float cf = w / a.temperature;
     each_entry(sh.id, a.K, lane, [&](int k) {
@@ -170,8 +184,9 @@ __device__ __forceinline__ Student student_list(const DistillArgs& a, float weig
       const float d = share(k, p);
       sh.grad[k] = E::bits_of(cf == 0.f ? 0.f : cf * listed_grad(reverse, p, sh.q[k], d, kl));
     });
-    out.rest = rest_grad(cf == 0.f ? 0.f : cf * others_grad(reverse, p_rest, t.q_rest, d_rest, kl),
-                         Rs, total);
+    out.rest = rest_grad(
+        cf == 0.f ? 0.f : cf * p_rest * others_grad(reverse, p_rest, t.q_rest, d_rest, kl), m_rest,
+        s_rest);
   }
   return out;
 }
@@ -193,9 +208,8 @@ __device__ __forceinline__ u32x4 rest_vec(u32x4 z, float c, const RestGrad& g) {
   float f[E::kPerVec];
   E::unpack(z, f);
 #pragma unroll
-  for (int e = 0; e < E::kPerVec; ++e) f[e] = fast_exp2(__builtin_fmaf(f[e], c, -g.b2));
-  const uint32_t sgn = g.neg ? E::kSignMask : 0u;
-  return E::pack(f) ^ u32x4{sgn, sgn, sgn, sgn};
+  for (int e = 0; e < E::kPerVec; ++e) f[e] = fast_exp2(__builtin_fmaf(f[e] - g.m, c, g.up)) * g.g;
+  return E::pack(f);
 }
 
 }  // namespace cis

@@ -128,7 +128,7 @@ __global__ __launch_bounds__(BLOCK) __attribute__((amdgpu_waves_per_eu(4))) void
     };
     const uint32_t mine = sh.mine[tid];
     // sweep 1: the tokens that are not listed
-    float R = kMinExp, s = 0.f;
+    float R = -FLT_MAX, s = 0.f;   // the largest of them, and the sum of exponentials relative to it
     auto fold = [&](int v, u32x4 x, bool listed, bool last) {
       float f[EPV];
       E::unpack(x, f);
@@ -145,11 +145,11 @@ __global__ __launch_bounds__(BLOCK) __attribute__((amdgpu_waves_per_eu(4))) void
       float m = f[0];
 #pragma unroll
       for (int e = 1; e < EPV; ++e) m = fmaxf(m, f[e]);
-      const float Rn = fmaxf(R, m * c);
+      const float Rn = fmaxf(R, m);
       float part = 0.f;
 #pragma unroll
-      for (int e = 0; e < EPV; ++e) part += fast_exp2(__builtin_fmaf(f[e], c, -Rn));
-      s = s * fast_exp2(R - Rn) + part;
+      for (int e = 0; e < EPV; ++e) part += fast_exp2((f[e] - Rn) * c);
+      s = s * fast_exp2((R - Rn) * c) + part;
       R = Rn;
     };
     if (valid && wid == 0) {
@@ -169,7 +169,7 @@ __global__ __launch_bounds__(BLOCK) __attribute__((amdgpu_waves_per_eu(4))) void
     if (valid) {
       for (int v = NV * BLOCK + tid; v < nvec; v += BLOCK)
         fold(v, bload_aux<kAuxStream1>(rs, (uint32_t)v * 16u), true, (v + 1) * EPV > V);
-      wave_lse(R, s);
+      wave_lse(R, s, c);
       if (lane == 0) {
         sh.f[wid] = R;
         sh.g[wid] = s;
@@ -177,11 +177,11 @@ __global__ __launch_bounds__(BLOCK) __attribute__((amdgpu_waves_per_eu(4))) void
     }
     lds_barrier();
     if (wid == 0) {
-      Student st{0.f, RestGrad{INFINITY, 0u}, true};
+      Student st{0.f, RestGrad{0.f, 0.f, 0.f}, true};
       if (valid) {
-        R = lane < NW ? sh.f[lane] : kMinExp;
+        R = lane < NW ? sh.f[lane] : -FLT_MAX;
         s = lane < NW ? sh.g[lane] : 0.f;
-        wave_lse(R, s);
+        wave_lse(R, s, c);
         st = student_list<E, true>(a, weight, sh.list, lane, sh.teacher, R, s);
       }
       if (lane == 0) {
@@ -276,7 +276,7 @@ __global__ __launch_bounds__(64 * NW) void cis_distill_row_kernel(const DistillA
     }
   seen = block_sum<NW>(seen | wrong << 16, sh.u);   // (K entries at most, in each)
   const bool bad = seen >> 16 != 0, valid = on && !bad && seen != 0;
-  Student st{0.f, RestGrad{INFINITY, 0u}, true};
+  Student st{0.f, RestGrad{0.f, 0.f, 0.f}, true};
   if (valid) {
     const __amdgpu_buffer_rsrc_t rs = tok_rsrc(a.r, row);
     float M = -INFINITY;
@@ -310,12 +310,9 @@ __global__ __launch_bounds__(64 * NW) void cis_distill_row_kernel(const DistillA
     whole = wave_sum(whole);
     double rest = whole - block_sum<NW>(less, sh.d);
     if (wid != 0) return;   // (no barrier follows)
-    float R = fmaxf(M * c, kMinExp), s;
-    // rest is relative to M; the loss takes it relative to 2^R
-    const float shift = fast_exp2(__builtin_fmaf(M, c, -R));
-    s = (float)rest * shift;
+    float R = M, s = (float)rest;
     if (!(rest > whole * 0x1p-28)) {
-      R = kMinExp;
+      R = -FLT_MAX;
       s = 0.f;
       for (int v = lane; v < nvec; v += 64) {
         float f[EPV];
@@ -332,13 +329,13 @@ __global__ __launch_bounds__(64 * NW) void cis_distill_row_kernel(const DistillA
           if (bits >> e & 1) f[e] = -INFINITY;
           m = fmaxf(m, f[e]);
         }
-        const float Rn = fmaxf(R, m * c);
+        const float Rn = fmaxf(R, m);
 #pragma unroll
-        for (int e = 0; e < EPV; ++e) part += fast_exp2(__builtin_fmaf(f[e], c, -Rn));
-        s = s * fast_exp2(R - Rn) + part;
+        for (int e = 0; e < EPV; ++e) part += fast_exp2((f[e] - Rn) * c);
+        s = s * fast_exp2((R - Rn) * c) + part;
         R = Rn;
       }
-      wave_lse(R, s);
+      wave_lse(R, s, c);
     }
     st = student_list<E, BWD>(a, row_weight(a, row), sh.list, lane, sh.teacher, R, s);
   }

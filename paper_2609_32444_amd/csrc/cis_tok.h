@@ -109,10 +109,9 @@ struct TopArgs {
   float* tail;                // nullable
 };
 
-// The gradient of a row's tokens that are not listed: exp2(fma(z, c, -b2)), negative with `neg`.
+// The gradient of a row's tokens that are not listed: exp2((z - m) c + up) g.
 struct RestGrad {
-  float b2;
-  uint32_t neg;
+  float m, up, g;
 };
 
 struct DistillArgs {
@@ -124,6 +123,8 @@ struct DistillArgs {
   int64_t row0;               // the launch's first row (cis_distill_grad_kernel: segment)
   int32_t nseg;               // segments per row
   float c;                    // scan_c(temperature)
+  float inv_t;                // 1 / temperature, and the same in double
+  double inv_t64;
   void* dlogits;              // nullable (forward)
   int64_t grow_bytes;
   const int32_t* ids;

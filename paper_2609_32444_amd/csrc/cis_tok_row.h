@@ -99,10 +99,10 @@ __device__ __forceinline__ float wave_max(float x) {
   return fmaxf(fmaxf(lane_value(m, 0), lane_value(m, 16)),
                fmaxf(lane_value(m, 32), lane_value(m, 48)));
 }
-// A wave's sum s 2^R of its lanes' sums: R the largest of their references.
-__device__ __forceinline__ void wave_lse(float& R, float& s) {
+// A wave's sum of its lanes' sums of exp2((z - R) c): R the largest of their references.
+__device__ __forceinline__ void wave_lse(float& R, float& s, float c) {
   const float m = wave_max(R);
-  s = wave_sum(s * fast_exp2(R - m));
+  s = wave_sum(s * fast_exp2((R - m) * c));
   R = m;
 }
 // Sum over the lanes up to this one.

@@ -297,6 +297,8 @@ int run_distill(const DistillCall& c, hipStream_t stream) {
     a.logk_ws = reinterpret_cast<float*>(base + L.logk);
     a.excess_ws = reinterpret_cast<float*>(base + L.excess);
     a.c = cis::scan_c(p.temperature);
+    a.inv_t = 1.f / p.temperature;
+    a.inv_t64 = 1.0 / (double)p.temperature;
     a.fin = finalize_args(base, L, c.T, c.loss);
     if (int rc = launch_distill(c, D, base, a, cus, stream)) return rc;
     if (c.bwd && distill_in_parts(c.T, a.r.nvec)) return CIS_OK;   // (the last kernel sums up)

@@ -1,0 +1,240 @@
+"""The distillation loss on the GPU against its formulas in 64 bits, in log space: classes of any size
+beside each other, logits and temperatures anywhere in their ranges.
+
+Tolerances, u = 2^-24. A class's log-probability comes from the exponent of a difference of logits,
+x = (z - M) / temperature, which takes four roundings (the difference, the factor's two, the product:
+8 u |x| leaves room), minus the log of a sum, of which
+  * the terms have their own exponents' errors, weighed by their shares (8 u E|x|),
+  * the sum has 4 roundings for every vector that a thread adds and 40 u for the rest of the tree,
+  * the log and the conversion to natural units round at its own size (4 u of either);
+64 u cover the hardware's exp2, log and the last roundings. What follows from the log-probabilities
+has these errors times its derivatives, and 32 u of its own for its arithmetic."""
+
+import math
+
+import pytest
+import torch
+
+import paper_2609_32444_amd as cis
+
+pytestmark = pytest.mark.gpu
+DEV = "cuda"
+U = 2.0 ** -24
+INF = math.inf
+DTYPES = [torch.bfloat16, torch.float32]
+
+
+def _gen(seed):
+    return torch.Generator(device=DEV).manual_seed(seed)
+
+
+def _store(z, dtype, pad=0, fill=float("nan")):
+    """[T, V] logits in rows of whole 16-byte vectors, the padding holding NaNs."""
+    T, V = z.shape
+    epv = 16 // dtype.itemsize
+    ld = (V + epv - 1) // epv * epv + pad * epv
+    s = torch.full((max(T, 1), ld), fill, dtype=dtype, device=DEV)
+    s[:T, :V] = z.to(dtype)
+    return s[:T, :V]
+
+
+def _lists(zt, K, temp, seed=0, tail=True, holes=0.0):
+    """The K largest logits of a teacher [T, V] in a shuffled order, some entries empty, and the
+    log-sum-exp of what the lists leave."""
+    T, V = zt.shape
+    K = min(K, V)
+    v, i = zt.topk(K, dim=1)
+    perm = torch.rand(T, K, generator=_gen(seed), device=DEV).argsort(1)
+    v, i = v.gather(1, perm).contiguous(), i.gather(1, perm).to(torch.int32)
+    i[torch.rand(T, K, generator=_gen(seed + 1), device=DEV) < holes] = -1
+    if not tail:
+        return i, v, None
+    out = torch.zeros(T, V + 1, dtype=torch.bool, device=DEV)
+    out.scatter_(1, torch.where(i < 0, V, i).long(), True)
+    y = (zt.double() / temp).masked_fill(out[:, :V], -INF)
+    return i, v, torch.logsumexp(y, 1).float()
+
+
+def _f32(x):
+    return float(torch.tensor(x, dtype=torch.float32))
+
+
+def _classes(x, rest):
+    """log shares of the classes (x [T, K], rest [T]; -inf: nothing) and the log of the whole."""
+    lse = torch.logaddexp(torch.logsumexp(x, 1), rest)
+    share = torch.cat([x, rest[:, None]], 1) - lse[:, None]
+    near = -torch.log1p(torch.exp(torch.logsumexp(x, 1) - rest))
+    share[:, -1] = torch.where(rest > torch.logsumexp(x, 1), near, share[:, -1])
+    return share, lse
+
+
+def _kl_parts(la, lb):
+    """a log(a / b) - a + b of each class."""
+    a, b, d = la.exp(), lb.exp(), la - lb
+    part = torch.where(d.abs() < 0.5, a * (torch.expm1(-d) + d), a * d - a + b)
+    return torch.where(la == -INF, b, part)
+
+
+def _minus(la, lb):
+    """a - b."""
+    d = la - lb
+    return torch.where(d.abs() < 0.5, lb.exp() * torch.expm1(d), la.exp() - lb.exp())
+
+
+def _zero(x, where):
+    return torch.where(where, torch.zeros_like(x), x)
+
+
+def _check(logits, ids, values, tail, out, *, reverse=False, temp=1.0, scale=1.0, weight=None,
+           mask=None, rows=slice(None), n_nonfinite=0, stats=True):
+    """All rows of a call, or `rows` of them (stats=False: their outputs alone)."""
+    pick = lambda t: None if t is None else t[rows]  # noqa: E731
+    z, ids, values, tail, weight, mask = map(pick, (logits, ids, values, tail, weight, mask))
+    bf16, z = z.dtype == torch.bfloat16, z.double()
+    T, V = z.shape
+    temp, scale = _f32(temp), _f32(scale)
+    on = torch.ones(T, dtype=torch.bool, device=DEV) if mask is None else mask != 0
+    ids = ids.long()
+    inside = (ids >= 0) & (ids < V)
+    at = torch.where(inside, ids, V)
+    count = torch.zeros(T, V + 1, device=DEV).scatter_add_(1, at, torch.ones_like(at).float())
+    bad = on & (((ids != -1) & ~inside).any(1) | (count[:, :V] > 1).any(1))
+    valid = on & ~bad & inside.any(1)
+    listed = count[:, :V] > 0
+    # the student's and the teacher's exponents, relative to their largest; log shares
+    y = z / temp
+    x = y - y.amax(1, keepdim=True)
+    xk = x.gather(1, torch.where(inside, ids, 0)).masked_fill(~inside, -INF)
+    xr = x.masked_fill(listed, -INF)
+    lr = torch.logsumexp(xr, 1)
+    lp, p_lse = _classes(xk, lr)
+    t = (values.double() / temp).masked_fill(~inside, -INF)
+    tt = torch.full_like(lr, -INF) if tail is None else tail.double()
+    top = torch.maximum(t.amax(1), tt)[:, None]
+    t, tt = t - top, tt - top[:, 0]
+    lq, q_lse = _classes(t, tt)
+    p, q = lp.exp(), lq.exp()
+    none = (lp == -INF) & (lq == -INF)   # empty entries, and a rest that neither has
+    d = _zero(lp - lq, none)
+    kl = _zero(_kl_parts(lp, lq) if reverse else _kl_parts(lq, lp), none).sum(1)
+    factor = p * (d - kl[:, None]) if reverse else _minus(lp, lq)
+    factor = _zero(factor, lp == -INF if reverse else none)
+    part = torch.exp(xr - lr[:, None]).masked_fill((lr == -INF)[:, None], 0.0)
+    w = scale * (1.0 if weight is None else weight.double()) * torch.ones(T, device=DEV).double()
+    w = torch.where(valid, w, 0.0)
+    cf = (w / temp)[:, None]
+    # errors of the log-probabilities
+    vecs = min(20, -(-V * logits.element_size() // 16) // 64 + 1)
+    own = 64 + 40 + 4 * vecs
+
+    def size(x):
+        return torch.where(x == -INF, 0.0, x).abs()
+
+    spread = (x.exp() * size(x)).sum(1) / p_lse.exp()
+    ep = U * (8 * size(torch.cat([xk, lr[:, None]], 1)) + 4 * size(lp)
+              + (8 * spread + 4 * p_lse.abs() + own)[:, None])
+    spread = (t.exp() * size(t)).sum(1) / q_lse.exp()
+    eq = U * (8 * size(torch.cat([t, tt[:, None]], 1)) + 4 * size(lq)
+              + (8 * spread + 4 * q_lse.abs() + own)[:, None])
+    first, second, ef, es = (p, q, ep, eq) if reverse else (q, p, eq, ep)
+    moved = _zero(first * d, first == 0).abs() * (ef + 32 * U) + (q - p).abs() * (es + 32 * U)
+    e_kl = _zero(moved, none).sum(1) + 32 * U * kl + 2.0 ** -120
+    terms, tol_t = _zero(w * kl, w == 0), w.abs() * e_kl
+    assert not out["terms"][rows][~valid].any()
+    got = out["terms"][rows].double()
+    fine = (got - terms).abs() <= tol_t
+    assert fine.all(), (int((~fine).sum()), got[~fine][:4], terms[~fine][:4], tol_t[~fine][:4])
+    if stats:
+        loss = float(out["loss"])
+        assert abs(loss - float(terms.sum())) <= float(tol_t.sum()) + 64 * U * float(terms.abs().sum())
+        st = cis.read_stats(out["workspace"])
+        assert (st["n_valid"], st["n_bad_id"], st["n_nonfinite"]) == (int(valid.sum()),
+                                                                      int(bad.sum()), n_nonfinite)
+    if "dlogits" not in out:
+        return
+    if reverse:
+        e_factor = size(factor) * ep + p * (ep + eq + e_kl[:, None])
+    else:
+        e_factor = p * ep + q * eq
+    e_factor = _zero(e_factor + 32 * U * size(factor), none)
+    grad = part * factor[:, -1:]
+    tol = part * e_factor[:, -1:] + grad.abs() * U * (8 * size(x) + own
+                                                      + (8 * spread.abs() + 32)[:, None])
+
+    def put(a, b):   # (empty entries go to a column of their own)
+        return torch.cat([a, a[:, :1]], 1).scatter_(1, at, b)[:, :V]
+
+    grad, tol = put(grad, factor[:, :-1]) * cf, put(tol, e_factor[:, :-1]) * cf.abs()
+    grad, tol = _zero(grad, cf == 0), tol + 2.0 ** -126
+    if bf16:
+        tol = tol + grad.abs() * 2.0 ** -8
+    got = out["dlogits"][rows].double()
+    off = (got - grad).abs()
+    fine = off <= tol
+    assert fine.all(), (int((~fine).sum()), (~fine).nonzero()[:4].tolist(), got[~fine][:4],
+                        grad[~fine][:4], tol[~fine][:4])
+
+
+def _both(logits, ids, values, tail, **kw):
+    """The loss alone and with its gradient."""
+    args = dict(kind=cis.KL_REVERSE if kw.get("reverse") else cis.KL_FORWARD,
+                temperature=kw.get("temp", 1.0), scale=kw.get("scale", 1.0))
+    w, m = kw.get("weight"), kw.get("mask")
+    for call in (cis.distill_fwd, cis.distill_bwd):
+        _check(logits, ids, values, tail, call(logits, ids, values, tail, w, m, **args), **kw)
+
+
+# Rows of the fused pass (a wave's, and 256 threads'), and of the pass in parts.
+WIDTHS = [(1000, 0), (3000, 1), (10000, 0), (20000, 0)]
+
+
+@pytest.mark.parametrize("dtype", DTYPES)
+@pytest.mark.parametrize("temp", [1.0, 0.1, 0.01, 0.001, 50.0])
+@pytest.mark.parametrize("V,pad", WIDTHS)
+def test_logits_far_from_zero(V, pad, temp, dtype):
+    """What is common to a row's logits is of no account, however large beside the temperature."""
+    T, K = 6, 40
+    g = _gen(V)
+    zt = torch.randn(T, V, generator=g, device=DEV) * (2.0 * temp)
+    noise = torch.randn(T, V, generator=g, device=DEV) * temp
+    for offset in (0.0, 100.0, -1000.0, 30000.0):
+        # (rounded as stored first: the teacher has lists of the same numbers)
+        teacher = _store(zt + offset, dtype).float()
+        logits = _store(teacher + noise, dtype, pad=pad)
+        for tail, reverse in ((False, False), (True, False), (True, True)):
+            lists = _lists(teacher, K, temp, tail=tail)
+            _both(logits, *lists, temp=temp, reverse=reverse, scale=0.25)
+
+
+@pytest.mark.parametrize("dtype", DTYPES)
+@pytest.mark.parametrize("temp", [1e-6, 1e-9, 2.0 ** -64, 1e9, 2.0 ** 64])
+@pytest.mark.parametrize("V,pad", WIDTHS)
+def test_temperatures_at_the_ends_of_their_range(V, pad, temp, dtype):
+    T, K = 6, 40
+    g = _gen(V + 1)
+    zt = torch.randn(T, V, generator=g, device=DEV) * 2
+    logits = _store(zt + 0.1 * torch.randn(T, V, generator=g, device=DEV) + 7.0, dtype, pad=pad)
+    lists = _lists(_store(zt, dtype).float(), K, temp, tail=False)
+    _both(logits, *lists, temp=temp)
+
+
+@pytest.mark.parametrize("dtype", DTYPES)
+@pytest.mark.parametrize("V,pad", WIDTHS)
+def test_rows_of_the_lowest_value(V, pad, dtype):
+    """Logits set to the type's lowest value: the whole row, the listed ones, all others."""
+    T, K = 4, 12
+    g = _gen(V + 2)
+    lowest = torch.finfo(dtype).min
+    zt = torch.randn(T, V, generator=g, device=DEV) * 2
+    ids, values, tail = _lists(zt, K, 1.0)
+    z = zt + torch.randn(T, V, generator=g, device=DEV)
+    z[0] = lowest
+    z[1].index_fill_(0, ids[1].long(), lowest)
+    z[2, torch.rand(V, generator=g, device=DEV) < 0.7] = lowest
+    z[3] = z[3].index_copy(0, ids[3].long(), torch.full((K,), 1.0, device=DEV))
+    logits = _store(z, dtype, pad=pad)
+    # (a listed token of the lowest value makes a forward KL of some 1e38)
+    _both(logits, ids, values, tail, scale=1e-6)
+    alone = z.index_fill(0, torch.tensor([0, 1], device=DEV), lowest)
+    alone = torch.full_like(alone, lowest).scatter(1, ids.long(), values)
+    _both(_store(alone, dtype, pad=pad), ids, values, None)
