@@ -28,18 +28,20 @@ __device__ __forceinline__ float expm1_less(float d) {
   return s * d * d;
 }
 
-// log(rest / (list + rest)), accurate at both ends.
-__device__ __forceinline__ float log_rest(float list, float rest) {
-  const float total = list + rest;
-  return rest > 0.5f * total ? log1pf(-list / total) : logf(rest / total);
-}
-
 // Log of the share of a token x below the largest, of a total of 2^L. (In units of log2, that of the
 // type's lowest logit would be past float32.) Teacher and student round alike here: shares of the same
 // logits are the same bits.
 __device__ __forceinline__ float log_share(float x, float inv_t, float L) {
 #pragma clang fp contract(off)
   return x * inv_t - L * kLn2;
+}
+
+// log(rest / (list + rest)), accurate at both ends; x = log rest (which may be far below what rest can be),
+// 2^L = list + rest.
+__device__ __forceinline__ float log_rest(float list, float rest, float x, float L) {
+  const float total = list + rest;
+  if (rest > 0.5f * total) return log1pf(-list / total);
+  return rest > 0x1p-64f * total ? logf(rest / total) : x - L * kLn2;
 }
 
 // A class's part of sum a log(a/b) for log a - log b = d: a log(a/b) - a + b >= 0, where a and b are
@@ -58,17 +60,21 @@ __device__ __forceinline__ RestGrad rest_grad(float grad, float m, float s) {
   return RestGrad{m, (float)up, __builtin_amdgcn_ldexpf(g, -up)};
 }
 
-// Gradient coefficients (before scale * weight / temperature) of a listed token and, of p_j, of the
-// others.
-__device__ __forceinline__ float listed_grad(bool reverse, float p, float q, float d, float kl) {
-  if (reverse) return p > 0.f ? p * (d - kl) : 0.f;
-  return fabsf(d) <= kNearLog ? q * (d + expm1_less(d)) : p - q;   // (p - q cancels near 0)
+// cf exp(l) f for the log l of a share, which may lie far below float32 where the product does not:
+// the factors' powers of two join the exponent. cf = mant 2^up.
+__device__ __forceinline__ float share_grad(float l, float f, float mant, int up) {
+  up += __builtin_amdgcn_frexp_expf(f);
+  return fast_exp2(__builtin_fmaf(l, kLog2e, (float)up)) * (mant * __builtin_amdgcn_frexp_mantf(f));
 }
-__device__ __forceinline__ float others_grad(bool reverse, float p_rest, float q_rest, float d,
-                                             float kl) {
-  if (!(p_rest > 0.f)) return 0.f;
-  if (reverse) return d - kl;
-  return q_rest > 0.f ? -expm1f(-d) : 1.f;
+// Gradient of a class, by cf = mant 2^up = scale * weight / temperature: a listed token's, or that of
+// all others, each of which has it in proportion to its exponential. (lp, lq: logs of its shares)
+__device__ __forceinline__ float class_grad(bool reverse, float lp, float lq, float kl, float mant,
+                                            int up) {
+  const float d = lp - lq;
+  if (reverse) return lp > -INFINITY ? share_grad(lp, d - kl, mant, up) : 0.f;
+  if (fabsf(d) <= kNearLog)   // (p - q cancels near 0)
+    return share_grad(lq, d + expm1_less(d), mant, up);
+  return share_grad(lp, 1.f, mant, up) - share_grad(lq, 1.f, mant, up);
 }
 
 // ------------------------------------------------------------------------------------------
@@ -136,7 +142,7 @@ __device__ __forceinline__ Teacher teacher_list(const DistillArgs& a, float tail
     sh.q[k] = fast_exp2((x * c - up) - L);
     sh.lq[k] = log_share(x, a.inv_t, L) - above;
   });
-  return Teacher{rest / total, log_rest(s, rest), total > 0.f && total < INFINITY};
+  return Teacher{rest / total, log_rest(s, rest, t, L), total > 0.f && total < INFINITY};
 }
 
 // The loss of a row whose listed logits are at sh.z and whose other tokens' exponentials relative to
@@ -155,17 +161,14 @@ __device__ __forceinline__ Student student_list(const DistillArgs& a, float weig
   s = wave_sum(s);
   const float rest = s_rest * fast_exp2((m_rest - m) * c);
   const float total = s + rest, L = log2f(total);
-  const float p_rest = rest / total, d_rest = log_rest(s, rest) - t.log_rest;
-  // (the logits' exponents are formed once more for the gradient: nothing else of the entry is kept)
-  auto share = [&](int k, float& p) {
-    const float x = sh.z[k] - m;
-    p = fast_exp2(x * c - L);
-    return log_share(x, a.inv_t, L) - sh.lq[k];   // log p - log q
-  };
+  const float p_rest = rest / total,
+              lp_rest = log_rest(s, rest, (m_rest - m) * a.inv_t + logf(s_rest), L),
+              d_rest = lp_rest - t.log_rest;
+  // (the logits' logs are formed once more for the gradient: nothing of an entry is kept)
   float kl = 0.f;
   each_entry(sh.id, a.K, lane, [&](int k) {
-    float p;
-    const float d = share(k, p), q = sh.q[k];
+    const float x = sh.z[k] - m, d = log_share(x, a.inv_t, L) - sh.lq[k], q = sh.q[k],
+                p = fast_exp2(x * c - L);
     kl += reverse ? kl_part(p, d, q) : kl_part(q, -d, p);
   });
   kl = wave_sum(kl);
@@ -178,15 +181,15 @@ __device__ __forceinline__ Student student_list(const DistillArgs& a, float weig
   out.finite = isfinite(kl) && isfinite(out.term);
   out.rest = RestGrad{0.f, 0.f, 0.f};
   if (BWD) {
-    const float cf = w / a.temperature;
+    const float cf = w / a.temperature, mant = __builtin_amdgcn_frexp_mantf(cf);
+    const int up = __builtin_amdgcn_frexp_expf(cf);
     each_entry(sh.id, a.K, lane, [&](int k) {
-      float p;
-      const float d = share(k, p);
-      sh.grad[k] = E::bits_of(cf == 0.f ? 0.f : cf * listed_grad(reverse, p, sh.q[k], d, kl));
+      const float lp = log_share(sh.z[k] - m, a.inv_t, L);
+      sh.grad[k] =
+          E::bits_of(cf == 0.f ? 0.f : class_grad(reverse, lp, sh.lq[k], kl, mant, up));
     });
     out.rest = rest_grad(
-        cf == 0.f ? 0.f : cf * p_rest * others_grad(reverse, p_rest, t.q_rest, d_rest, kl), m_rest,
-        s_rest);
+        cf == 0.f ? 0.f : class_grad(reverse, lp_rest, t.log_rest, kl, mant, up), m_rest, s_rest);
   }
   return out;
 }

@@ -238,3 +238,34 @@ def test_rows_of_the_lowest_value(V, pad, dtype):
     alone = z.index_fill(0, torch.tensor([0, 1], device=DEV), lowest)
     alone = torch.full_like(alone, lowest).scatter(1, ids.long(), values)
     _both(_store(alone, dtype, pad=pad), ids, values, None)
+
+
+@pytest.mark.parametrize("dtype", DTYPES)
+@pytest.mark.parametrize("gap", [20.0, 60.0, 90.0, 140.0, 500.0])
+@pytest.mark.parametrize("V,pad", WIDTHS)
+def test_classes_far_below_each_other(V, pad, gap, dtype):
+    """Listed tokens, or all others, with probabilities far below what 32 bits hold: their logarithms
+    are ordinary numbers, and so are the loss and its gradient."""
+    T, K = 6, 10
+    g = _gen(V + 3)
+    zt = torch.randn(T, V, generator=g, device=DEV)
+    ids, values, tail = _lists(zt, K, 1.0, holes=0.1)
+    listed = torch.zeros(T, V, dtype=torch.bool, device=DEV)
+    listed.scatter_(1, torch.where(ids < 0, ids.max(1, keepdim=True).values, ids).long(), True)
+    z = zt + torch.randn(T, V, generator=g, device=DEV)
+    z[0] += listed[0] * gap             # the student has next to nothing outside the list
+    z[1] -= listed[1] * gap             # ... or within it
+    z[2, ids[2].max()] += gap           # ... or all of it in one token
+    far = tail.clone()
+    far[3] -= gap                       # the teacher has next to nothing outside the list
+    far[4] += gap                       # ... or within it
+    z[5] += listed[5] * gap             # both of them
+    far[5] -= gap
+    weight = torch.rand(T, generator=g, device=DEV) + 0.5
+    for scale in (1.0, 65536.0):
+        for reverse in (False, True):
+            _both(_store(z, dtype, pad=pad), ids, values, far, weight=weight, reverse=reverse,
+                  scale=scale)
+    # by the temperature alone
+    for reverse in (False, True):
+        _both(_store(z, dtype, pad=pad), ids, values, tail / 0.05, temp=0.05, reverse=reverse)
