@@ -192,6 +192,7 @@ __global__ __launch_bounds__(BLOCK) __attribute__((amdgpu_waves_per_eu(4))) void
     lds_barrier();
     // sweep 2
     const RestGrad g = sh.rest;
+    const bool others = valid && g.g != 0.f;   // (else 0, whatever the logits are)
     opaque(r);
     fetch(next, tid);
     void* grow = (char*)a.dlogits + row * a.grow_bytes;
@@ -199,10 +200,9 @@ __global__ __launch_bounds__(BLOCK) __attribute__((amdgpu_waves_per_eu(4))) void
     const __amdgpu_buffer_rsrc_t ws = make_rsrc(grow, (uint32_t)(nvec - (ragged ? 1 : 0)) * 16u);
     auto put = [&](int v, u32x4 x, bool listed, bool last) {
       u32x4 out{0u, 0u, 0u, 0u};
-      if (valid) {
-        out = rest_vec<E>(x, c, g);
-        if (listed) each_listed(v, [&](uint32_t k, int e) { out = E::set(out, e, sh.list.grad[k]); });
-      }
+      if (others) out = rest_vec<E>(x, c, g);
+      if (valid && listed)
+        each_listed(v, [&](uint32_t k, int e) { out = E::set(out, e, sh.list.grad[k]); });
       bstore(out, ws, (uint32_t)v * 16u, 0u);
       if (last && ragged && v == nvec - 1)
         for (int e = 0; e < V - v * EPV; ++e) E::store_elem(grow, v * EPV + e, E::elem_bits(out, e));
@@ -364,9 +364,10 @@ __global__ __launch_bounds__(kDistillGradBlock) void cis_distill_grad_kernel(con
   const int seg = (int)(b - row * a.nseg);
   const bool valid = a.valid[row] != 0;
   const RestGrad g = a.rest[row];
+  const bool others = valid && g.g != 0.f;   // (else 0, whatever the logits are)
   const bool ragged = a.r.V % EPV != 0;
   const __amdgpu_buffer_rsrc_t rs =
-      make_rsrc((const char*)a.r.logits + row * a.r.row_bytes, valid ? (uint32_t)a.r.nvec * 16u : 0u);
+      make_rsrc((const char*)a.r.logits + row * a.r.row_bytes, others ? (uint32_t)a.r.nvec * 16u : 0u);
   void* grow = (char*)a.dlogits + row * a.grow_bytes;
   const __amdgpu_buffer_rsrc_t ws =
       make_rsrc(grow, (uint32_t)(a.r.nvec - (ragged ? 1 : 0)) * 16u);
@@ -375,7 +376,7 @@ __global__ __launch_bounds__(kDistillGradBlock) void cis_distill_grad_kernel(con
   static_for<K>([&](auto I) { r[I] = bload(rs, (uint32_t)(v0 + I * BLOCK) * 16u, 0u); });
   static_for<K>([&](auto I) {
     const int v = v0 + I * BLOCK;
-    const u32x4 out = valid ? rest_vec<E>(r[I], a.c, g) : u32x4{0u, 0u, 0u, 0u};
+    const u32x4 out = others ? rest_vec<E>(r[I], a.c, g) : u32x4{0u, 0u, 0u, 0u};
     bstore(out, ws, (uint32_t)v * 16u, 0u);
     if (ragged && v == a.r.nvec - 1)
       for (int e = 0; e < a.r.V - v * EPV; ++e)

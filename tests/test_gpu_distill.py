@@ -269,3 +269,29 @@ def test_classes_far_below_each_other(V, pad, gap, dtype):
     # by the temperature alone
     for reverse in (False, True):
         _both(_store(z, dtype, pad=pad), ids, values, tail / 0.05, temp=0.05, reverse=reverse)
+
+
+@pytest.mark.parametrize("dtype", DTYPES)
+@pytest.mark.parametrize("V,pad", WIDTHS)
+def test_weight_of_zero_in_rows_that_are_not_finite(V, pad, dtype):
+    """A row of weight 0 has term 0 and a zero gradient, whatever its logits and its list hold."""
+    T, K = 8, 10
+    g = _gen(V + 4)
+    zt = torch.randn(T, V, generator=g, device=DEV)
+    ids, values, tail = _lists(zt, K, 1.0)
+    other = [int(next(j for j in range(V) if j not in set(i))) for i in ids.tolist()]
+    z = zt + torch.randn(T, V, generator=g, device=DEV)
+    z[0, other[0]] = math.nan
+    z[1, other[1]] = INF
+    z[2, ids[2, 0]] = math.nan
+    z[3, ids[3, 0]] = INF
+    z[4] = -INF
+    values[5, 3] = math.nan
+    tail[6] = math.nan
+    weight = torch.zeros(T, device=DEV)
+    weight[7] = 1.0
+    logits = _store(z, dtype, pad=pad)
+    for kind in (cis.KL_FORWARD, cis.KL_REVERSE):
+        out = cis.distill_bwd(logits, ids, values, tail, weight, kind=kind)
+        assert not out["terms"][:7].any() and not out["dlogits"][:7].any()
+        assert out["dlogits"][7].any() and float(out["loss"]) == float(out["terms"][7]) > 0
