@@ -295,3 +295,161 @@ def test_weight_of_zero_in_rows_that_are_not_finite(V, pad, dtype):
         out = cis.distill_bwd(logits, ids, values, tail, weight, kind=kind)
         assert not out["terms"][:7].any() and not out["dlogits"][:7].any()
         assert out["dlogits"][7].any() and float(out["loss"]) == float(out["terms"][7]) > 0
+
+
+@pytest.mark.parametrize("dtype", DTYPES)
+@pytest.mark.parametrize("V", [1, 2, 7, 64, 1000, 1024])
+def test_reverse_with_every_token_listed(V, dtype):
+    """Nothing is left outside the lists, of the teacher or of the student."""
+    T = 7
+    g = _gen(V + 5)
+    zt = torch.randn(T, V, generator=g, device=DEV) * 2
+    z = zt + torch.randn(T, V, generator=g, device=DEV)
+    for temp in (1.0, 0.25):
+        ids, values, tail = _lists(zt, V, temp)
+        assert (tail == -INF).all()
+        for reverse in (True, False):
+            _both(_store(z, dtype, pad=1), ids, values, tail, reverse=reverse, temp=temp)
+        _both(_store(z, dtype), ids, values, None, temp=temp)
+
+
+# ------------------------------------------------------------------------------------------
+# Every width of the fused pass, and the pass in parts beside it
+# ------------------------------------------------------------------------------------------
+
+def _mixed(T, V, K, dtype, seed, *, pad=0, extra=0):
+    """Rows of which some are masked, some have weight 0, an empty list, empty entries, ids out of range or
+    repeated ids, in no order; lists as the first K columns of longer ones."""
+    g = _gen(seed)
+
+    def some(share):
+        return torch.rand(T, generator=g, device=DEV) < share
+
+    zt = torch.randn(T, V, generator=g, device=DEV) * 2.5
+    ids, values, tail = _lists(zt, K, 1.0, seed=seed)
+    logits = _store(zt.add_(torch.randn(T, V, generator=g, device=DEV)), dtype, pad=pad, fill=3.0)
+    holes = some(0.3)[:, None] & (torch.rand(ids.shape, generator=g, device=DEV) < 0.3)
+    ids = torch.where(holes, -1, ids)
+    ids[some(0.1)] = -1
+    ids[some(0.05), 1] = V
+    ids[some(0.05), 2] = -7
+    twice = some(0.1)
+    ids[twice, 3] = ids[twice, 0]
+    weight = torch.rand(T, generator=g, device=DEV) + 0.1
+    weight[some(0.1)] = 0.0
+    mask = (~some(0.2)).to(torch.uint8)
+    wide_i = torch.zeros(T, K + extra, dtype=torch.int32, device=DEV)
+    wide_v = torch.zeros(T, K + extra, device=DEV)
+    wide_i[:, :K], wide_v[:, :K] = ids, values
+    return logits, wide_i[:, :K], wide_v[:, :K], tail, weight, mask
+
+
+def _check_mixed(case, kind, rows, scale=0.5):
+    """A call with the gradient beside its logits and in their place, and the loss alone: the chosen rows
+    against the formulas, and what all rows have to be."""
+    logits, ids, values, tail, weight, mask = case
+    T, V = logits.shape
+    kw = dict(kind=kind, scale=scale)
+    out = cis.distill_bwd(*case, **kw)
+    ref = dict(reverse=kind == cis.KL_REVERSE, scale=scale, weight=weight, mask=mask, rows=rows,
+               stats=False)
+    _check(logits, ids, values, tail, out, **ref)
+    fwd = cis.distill_fwd(*case, **kw)
+    _check(logits, ids, values, tail, fwd, **ref)
+    # what counts
+    on = mask != 0
+    order = torch.where((ids < 0) | (ids >= V), -1 - torch.arange(ids.shape[1], device=DEV),
+                        ids).sort(1).values
+    bad = (((ids != -1) & ((ids < 0) | (ids >= V))).any(1) | (order[:, 1:] == order[:, :-1]).any(1))
+    valid = on & ~bad & (ids >= 0).any(1)
+    live = valid & (weight != 0)
+    for o in (out, fwd):
+        assert not o["terms"][~live].any() and (o["terms"][live] != 0).all()
+        total = o["terms"].double()
+        assert abs(float(o["loss"]) - float(total.sum())) <= 64 * U * float(total.abs().sum())
+        st = cis.read_stats(o["workspace"])
+        assert (st["n_valid"], st["n_bad_id"], st["n_nonfinite"]) == (int(valid.sum()),
+                                                                      int((on & bad).sum()), 0)
+    assert not out["dlogits"][~live].any() and out["dlogits"][live].any(1).all()
+    # in place, whatever the rows hold besides; the columns past V stay
+    base = logits._base if logits._base is not None else logits
+    place = base.clone()[:T, :V]
+    res = cis.distill_bwd(place, ids, values, tail, weight, mask, dlogits=place, **kw)
+    assert torch.equal(place, out["dlogits"]) and torch.equal(res["terms"], out["terms"])
+    if base.shape[1] > V:
+        assert (place._base[:, V:] == 3.0).all()
+
+
+def _some_rows(T, n, seed=0):
+    rows = torch.randperm(T, generator=torch.Generator().manual_seed(seed))[:n].tolist()
+    return sorted(set(rows) | {0, T - 1})
+
+
+# Vectors of 16 bytes per row, one in each step of the fused pass (and beyond what it holds), and the
+# largest number of rows that go in parts there.
+STEPS = [(37, 0), (300, 0), (620, 448), (1100, 448), (2001, 0), (3000, 320), (4050, 320),
+         (5101, 320), (6600, 144), (8650, 144), (12200, 112), (15300, 112), (19456, 112),
+         (19457, 112), (26000, 112)]
+
+
+@pytest.mark.parametrize("dtype", DTYPES)
+@pytest.mark.parametrize("K", [40, 300])
+@pytest.mark.parametrize("nvec,most", STEPS)
+def test_every_step_and_the_rows_beside_it(nvec, most, K, dtype):
+    V = nvec * (16 // dtype.itemsize) - nvec % 3
+    K = min(K, V // 2)
+    for T in ([20] if most == 0 else [most, most + 1]):
+        case = _mixed(T, V, K, dtype, nvec + T, pad=nvec % 2, extra=nvec % 5)
+        for kind in (cis.KL_FORWARD, cis.KL_REVERSE):
+            _check_mixed(case, kind, _some_rows(T, 10, nvec))
+
+
+@pytest.mark.parametrize("dtype", DTYPES)
+@pytest.mark.parametrize("nvec,T", [(90, 9000), (1000, 9000), (2000, 2600), (6000, 1300),
+                                    (13000, 700), (20500, 530)])
+def test_rows_of_several_rounds(nvec, T, dtype):
+    """More rows than workgroups at once: what one row leaves in shared memory is gone for the next."""
+    V = nvec * (16 // dtype.itemsize) - 1
+    case = _mixed(T, V, 50, dtype, nvec)
+    _check_mixed(case, cis.KL_FORWARD, _some_rows(T, 30, nvec))
+    _check_mixed(case, cis.KL_REVERSE, _some_rows(T, 30, nvec + 1))
+
+
+@pytest.mark.parametrize("dtype", DTYPES)
+@pytest.mark.parametrize("V,T", [(2500, 30), (70000, 150), (300000, 113)])
+def test_lists_that_share_places_of_the_table(V, T, dtype):
+    """Ids that fill whole vectors, run along the row, or fall into one place of the fused pass's table,
+    with rows enough for that pass."""
+    g = _gen(V)
+    zt = torch.randn(T, V, generator=g, device=DEV) * 2
+    logits = _store(zt + torch.randn(T, V, generator=g, device=DEV), dtype, pad=1)
+    rows = [0, 1, 2, T // 2, T - 1]
+    for stride, K in ((1, 1024), (8, 280), (4, 37), (16384, 9), (32768, 9), (293, 230), (65536, 4)):
+        K = min(K, (V - 1) // stride + 1)
+        ids = (torch.arange(K, device=DEV) * stride).to(torch.int32).expand(T, K).contiguous()
+        ids[1::2] = V - 1 - ids[1::2]
+        values = zt.gather(1, ids.long())
+        tail = torch.logsumexp(zt.scatter(1, ids.long(), -INF), dim=1)
+        for reverse in (False, True):
+            out = cis.distill_bwd(logits, ids, values, tail,
+                                  kind=cis.KL_REVERSE if reverse else cis.KL_FORWARD)
+            _check(logits, ids, values, tail, out, reverse=reverse, rows=rows, stats=False)
+
+
+@pytest.mark.parametrize("dtype", DTYPES)
+@pytest.mark.parametrize("K", [1, 40, 64, 200, 1000])
+@pytest.mark.parametrize("T,V", [(513, 2000), (900, 33001), (2000, 5000)])
+def test_loss_alone_over_many_rows(T, V, K, dtype):
+    """The loss without its gradient by one wave per row, on either side of 512 rows."""
+    g = _gen(T + K)
+    case = list(_mixed(T, V, max(K, 8), dtype, T, pad=1))
+    case[1], case[2] = case[1][:, :K].contiguous(), case[2][:, :K].contiguous()
+    case[3] = torch.randn(T, generator=g, device=DEV)
+    for kind in (cis.KL_FORWARD, cis.KL_REVERSE):
+        rows = _some_rows(T, 25, K)
+        out = cis.distill_fwd(*case, kind=kind)
+        ref = dict(reverse=kind == cis.KL_REVERSE, weight=case[4], mask=case[5])
+        _check(*case[:4], out, rows=rows, stats=False, **ref)
+        few = [x[:500] for x in case]
+        _check(*few[:4], cis.distill_fwd(*few, kind=kind), rows=[r for r in rows if r < 500],
+               stats=False, reverse=ref["reverse"], weight=few[4], mask=few[5])
