@@ -425,15 +425,16 @@ DistillVariant distill_fused(int dtype, int32_t nvec, int64_t K) {
   return DistillVariant{t[i].block, K <= 256 ? t[i].few : t[i].many};
 }
 
-// (96 rows of V = 151936, K = 256: 8.5 us by 4 waves a row, 11.5 by one)
+// (96 rows of V = 151936, K = 256: 8.5 us by 4 waves a row, 11.5 by one. With the gradient, rows that go
+// in parts are always few.)
 const void* distill_row_kernel(int dtype, bool bwd, int64_t K, bool few) {
 #define CIS_ROW_N(E, B, N)                                               \
   (K <= 64 ? (const void*)&cis_distill_row_kernel<E, B, 64, N>           \
    : K <= 256 ? (const void*)&cis_distill_row_kernel<E, B, 256, N>       \
               : (const void*)&cis_distill_row_kernel<E, B, CIS_TOP_MAX_K, N>)
-#define CIS_ROW(E, B) (few ? CIS_ROW_N(E, B, 4) : CIS_ROW_N(E, B, 1))
-  if (dtype == CIS_BF16) return bwd ? CIS_ROW(Bf16, true) : CIS_ROW(Bf16, false);
-  return bwd ? CIS_ROW(F32, true) : CIS_ROW(F32, false);
+#define CIS_ROW(E) \
+  (bwd ? CIS_ROW_N(E, true, 4) : few ? CIS_ROW_N(E, false, 4) : CIS_ROW_N(E, false, 1))
+  return dtype == CIS_BF16 ? CIS_ROW(Bf16) : CIS_ROW(F32);
 #undef CIS_ROW
 #undef CIS_ROW_N
 }

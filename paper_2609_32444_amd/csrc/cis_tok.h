@@ -164,7 +164,7 @@ struct DistillVariant {
 };
 // The fused pass for rows of nvec vectors, and the kernels of the pass in parts.
 DistillVariant distill_fused(int dtype, int32_t nvec, int64_t K);
-// few: rows that do not fill the chip with a wave each
+// few: rows that do not fill the chip with a wave each (with bwd all calls are)
 const void* distill_row_kernel(int dtype, bool bwd, int64_t K, bool few);
 const void* distill_grad_kernel(int dtype);
 

@@ -92,6 +92,7 @@ constexpr int64_t kMaxBlocks = int64_t(1) << 23;
 constexpr int64_t kFewRows = 448;
 // Rows up to which cis_distill_row_kernel gives a row 4 waves: two such workgroups per compute unit.
 constexpr int64_t kWaveRows = 512;
+static_assert(kFewRows <= kWaveRows, "with the gradient, a row has 4 waves");
 // Logits that a draw may have to look at where its parameters do not say.
 constexpr int64_t kManyLogits = 256;
 
