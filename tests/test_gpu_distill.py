@@ -453,3 +453,12 @@ def test_loss_alone_over_many_rows(T, V, K, dtype):
         few = [x[:500] for x in case]
         _check(*few[:4], cis.distill_fwd(*few, kind=kind), rows=[r for r in rows if r < 500],
                stats=False, reverse=ref["reverse"], weight=few[4], mask=few[5])
+
+
+@pytest.mark.parametrize("dtype,T", [(torch.bfloat16, 2100), (torch.float32, 1050)])
+def test_loss_alone_of_logits_beyond_the_caches(dtype, T):
+    """More than 192 MiB of logits, which the scan does not keep for a later read."""
+    case = _mixed(T, 50003, 40, dtype, 3)
+    assert case[0].stride(0) * T * dtype.itemsize > 192 << 20
+    rows = _some_rows(T, 25)
+    _check(*case[:4], cis.distill_fwd(*case), rows=rows, stats=False, weight=case[4], mask=case[5])

@@ -697,3 +697,22 @@ def test_shared_lists_are_refused():
 def test_top_k_beyond_int32_is_refused():
     with pytest.raises(ValueError, match="int32"):
         cis.sample(torch.zeros(2, 64, device=DEV), torch.zeros(2, device=DEV), top_k=2 ** 32 + 5)
+
+
+@pytest.mark.parametrize("dtype,T", [(torch.bfloat16, 2100), (torch.float32, 1050)])
+def test_lists_and_draws_of_logits_beyond_the_caches(dtype, T):
+    """More than 192 MiB of logits, which the scan does not keep for a later read."""
+    V = 50003
+    logits = _store(_logits(T, V, 13, "peaked"), dtype)
+    assert logits.stride(0) * T * dtype.itemsize > 192 << 20
+    u = torch.rand(T, generator=_gen(14), device=DEV)
+    rows = torch.randperm(T, generator=torch.Generator().manual_seed(1))[:40].to(DEV)
+
+    def some(out):
+        return {k: v[rows] for k, v in out.items() if k != "workspace"}
+
+    for K in (8, 256, 1024):
+        _check_top(logits[rows], K, some(cis.top_logits(logits, K)))
+    for s in (dict(), dict(top_k=20), dict(top_k=2000), dict(top_p=0.9),
+              dict(top_k=900, top_p=0.8, min_p=0.001)):
+        _check_sample(logits[rows], u[rows], some(cis.sample(logits, u, **s)), **s)
