@@ -26,8 +26,9 @@ extern "C" {
  * number u in [0, 1):
  *
  *   M    = max_j z_j
- *   q_j  = floor(2^28 * 2^((z_j - M) * c)),  c = log2(e) / temperature, the difference, c and the
- *          product each rounded to float32
+ *   q_j  = floor(2^28 * exp2((z_j - M) * c)),  c = log2(e) / temperature; the difference, c and the
+ *          product are rounded to float32, and exp2 is the device's own in float32 (within a unit in
+ *          the last place: 16 of 2^28 for a token near the largest)
  *   cuts, each a first part of the tokens in order of (z_j descending, j ascending):
  *     top_k   the first top_k tokens                                         (0: all)
  *     top_p   of those, the fewest whose sum of q reaches top_p times the sum over those (1: all)
@@ -35,8 +36,8 @@ extern "C" {
  *   kept = the tokens in every cut, N = sum of q over kept
  *   y    = the lowest id whose running sum of q over the kept ids <= y exceeds floor(u * N)
  *
- * The weights q are whole numbers, so the sums and the draw are exact and do not depend on an order
- * of summation; a token of probability below 2^-28 of the row's largest has weight 0. (top_p * sum,
+ * The weights q are whole numbers, so with them the sums and the draw are exact and do not depend on an
+ * order of summation; a token of probability below 2^-28 of the row's largest has weight 0. (top_p * sum,
  * min_p * 2^28 and u * N are formed in double.)
  * temperature = 0, or one so small that c is not finite, keeps the first token alone (greedy).
  *
