@@ -90,7 +90,11 @@ cis::ScanLayout top_layout(int64_t T, int64_t V, int64_t K, int dtype) {
 constexpr int64_t kMaxBlocks = int64_t(1) << 23;
 // Rows of a distillation call that may go in parts with the gradient.
 constexpr int64_t kFewRows = 448;
-// Rows up to which cis_distill_row_kernel gives a row 4 waves: two such workgroups per compute unit.
+// Rows up to which cis_distill_row_kernel gives a row 4 waves: two such workgroups per compute unit. The
+// loss alone, us by one wave and by four, 4096 rows of 8192 bytes, bf16 (float32 within 10% of it):
+//   K = 8 21.6, 25.7; K = 64 23.7, 26.9; K = 200 40.9, 34.3; K = 500 179, 108; K = 1000 290, 169
+// The bound suits lists of up to 64. Beyond them four waves are the faster at every count of rows, since a
+// workgroup's table and list (14 KB up to K = 256, then 55 KB of LDS) leave room for few: it does not look at K.
 constexpr int64_t kWaveRows = 512;
 static_assert(kFewRows <= kWaveRows, "with the gradient, a row has 4 waves");
 // Logits that a draw may have to look at where its parameters do not say.
@@ -211,6 +215,12 @@ DistillLayout distill_layout(int64_t T, int64_t V, int64_t K, int dtype) {
 //   V = 50264  112 rows 18, 20; 192 rows 22, 22; 256 rows 25, 21
 //   V = 151936 64 rows 20, 31; 112 rows 29, 31; 160 rows 34, 31
 //   V = 1024   64 rows 15, 14       V = 10000  64 rows 16, 15
+// K = 8 and 500 and float32 take the same bounds. Over 594 points (both types, K = 8, 64, 500, rows of
+// 128 to 30000 vectors, 64 to 448 rows) the side that the rule takes is 12% the faster one on average, and at
+// 101 of them the slower one by more than 3%. The largest of those, us in parts and fused:
+//   4500 vectors, 320 rows: K = 500 float32 37, 28; K = 64 float32 22, 18, bf16 25, 22; K = 8 bf16 24, 19
+//   18992 vectors, 112 rows, float32: K = 500 40, 31; K = 8 26, 22
+//   128 vectors, 112 rows, K = 500, bf16 25, 29; 30000 vectors, 320 rows, K = 64, bf16 82, 94
 bool distill_in_parts(int64_t T, int32_t nvec) {
   const int64_t most = nvec <= 320    ? 0
                        : nvec <= 1152 ? 448
