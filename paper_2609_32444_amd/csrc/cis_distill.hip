@@ -12,7 +12,7 @@ namespace cis {
 // table in LDS, hashed by the vector that a token lies in, with chains, and every thread has a bit for
 // each of its vectors that holds one: the first sweep leaves the listed tokens out of its sum and notes
 // their logits, the second puts their gradients in. Bound by the memory: 16384 rows of V = 151936 in
-// 1.83 ms (5.4 TB/s of reads and writes); the list's table and the loss by one wave lie between the
+// 1.88 ms (5.3 TB/s of reads and writes); the list's table and the loss by one wave lie between the
 // sweeps of a row, where the compute unit has no other row's loads to turn to.
 // ------------------------------------------------------------------------------------------
 template <int BLOCK, int KMAX>
@@ -38,7 +38,7 @@ __global__ __launch_bounds__(BLOCK) __attribute__((amdgpu_waves_per_eu(4))) void
     const DistillArgs a) {
   constexpr int NW = BLOCK / 64, EPV = E::kPerVec;
   // vectors that are asked for before the list, and stay in flight ahead of sweep 1 (16384 rows of
-  // V = 151936: 4 1981 us, 8 1902, 12 2056; 3001 of V = 50257: 142, 146, 153)
+  // V = 151936: 4 1903 us, 8 1867, 12 2081; 3001 of V = 50257: 144, 148, 154)
   constexpr int MOST = BLOCK == 1024 ? 8 : 4, FIRST = NV > MOST ? MOST : NV;
   typedef FusedShared<BLOCK, KMAX> Shared;
   __shared__ Shared sh;
@@ -223,7 +223,7 @@ __global__ __launch_bounds__(BLOCK) __attribute__((amdgpu_waves_per_eu(4))) void
 // are in double, and a vector's sum is the same bits wherever it is formed). Where less than 2^-28
 // of the row remains, the row is summed again without the listed tokens. The vectors are found
 // in a table in LDS: open addressing, a key and the listed tokens of the vector as bits. Bound by the
-// latency of a row's steps: 8192 rows, K = 64, in 14 us.
+// latency of a row's steps: 8192 rows, K = 64, in 15 us.
 // ------------------------------------------------------------------------------------------
 template <int KMAX>
 struct RowShared {
@@ -354,7 +354,7 @@ __global__ __launch_bounds__(64 * NW) void cis_distill_row_kernel(const DistillA
 // ------------------------------------------------------------------------------------------
 // In parts, 3: the gradient by segments of kGradVecs vectors; listed tokens are put in by the segment
 // that they lie in, once its own stores are done. The first workgroup sums up the call's statistics
-// too: there are few rows, and they were done before the launch. 96 rows of V = 151936 in 12 us (4.7 TB/s).
+// too: there are few rows, and they were done before the launch. 96 rows of V = 151936 in 14 us (4.3 TB/s).
 // ------------------------------------------------------------------------------------------
 template <class E>
 __global__ __launch_bounds__(kDistillGradBlock) void cis_distill_grad_kernel(const DistillArgs a) {
@@ -400,7 +400,8 @@ __global__ __launch_bounds__(kDistillGradBlock) void cis_distill_grad_kernel(con
 }
 
 // Variants of the fused pass: the first that holds a row. 1024 x 19 vectors take 76 of a thread's
-// 128 registers; longer rows read the rest twice.
+// 128 registers (10 others lie in scratch in bf16 and 6 in float32; no other variant has any); longer rows
+// read the rest twice.
 struct FusedVariant {
   int block, nv;
   const void *few, *many;   // lists of up to 256 and 1024 entries
@@ -425,8 +426,8 @@ DistillVariant distill_fused(int dtype, int32_t nvec, int64_t K) {
   return DistillVariant{t[i].block, K <= 256 ? t[i].few : t[i].many};
 }
 
-// (96 rows of V = 151936, K = 256: 8.5 us by 4 waves a row, 11.5 by one. With the gradient, rows that go
-// in parts are always few.)
+// (A forward call of 96 rows of V = 151936, K = 256: 17.7 us by 4 waves a row, 22.0 by one. With the
+// gradient, rows that go in parts are always few.)
 const void* distill_row_kernel(int dtype, bool bwd, int64_t K, bool few) {
 #define CIS_ROW_N(E, B, N)                                               \
   (K <= 64 ? (const void*)&cis_distill_row_kernel<E, B, 64, N>           \

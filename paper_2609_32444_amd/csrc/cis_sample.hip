@@ -177,8 +177,8 @@ __global__ __launch_bounds__(kHistBlock) void cis_step_kernel(const SampleArgs a
 // A wave's chunks one after the other, of one row in a workgroup: the sum of their weights, of a row
 // that top_p cuts those above the step of the cut, whose tokens are listed. A chunk whose largest logit
 // does not reach that far is not read. Without STEP, no row is cut by top_p. Bound by some 10
-// instructions a logit (24 us) and the second read of the row: 512 rows of V = 151936 in 31 us; with
-// STEP 256 rows of V = 262144, half of them peaked, in 19.
+// instructions a logit (24 us) and the second read of the row: 512 rows of V = 151936 in 32 us; with
+// STEP 256 rows of V = 262144, half of them peaked, in 21.
 // ------------------------------------------------------------------------------------------
 template <class E, bool STEP>
 __global__ __launch_bounds__(kWeighBlock) void cis_weigh_kernel(const SampleArgs a) {
@@ -246,7 +246,8 @@ __global__ __launch_bounds__(kWeighBlock) void cis_weigh_kernel(const SampleArgs
 
 // ------------------------------------------------------------------------------------------
 // The draw, by one workgroup per row. Bound by the latency of its steps, each of which waits for the
-// one before: a top-k list of one row 15 us, uncut rows 6 us, a step of top_p 11 us.
+// one before: a top-k list of one row 16 us (26 barriers), 512 uncut rows 9 us, 256 rows with a step of
+// top_p 14 us.
 // ------------------------------------------------------------------------------------------
 struct WideShared {
   u64 mass[kFineSteps];

@@ -211,10 +211,10 @@ DistillLayout distill_layout(int64_t T, int64_t V, int64_t K, int dtype) {
 // the gradient, in parts. The bounds follow the fused pass's ladder (distill_fused): rows that a wave
 // holds 10 or 18 vectors a thread of, those of 256 threads from 12 vectors and 512 threads of 10, and
 // longer ones, which take half of a compute unit and all of it. K = 64, bf16, us in parts and fused:
-//   V = 4096   448 rows 17, 20      V = 20000  320 rows 19, 21; 448 rows 22, 21
-//   V = 50264  112 rows 18, 20; 192 rows 22, 22; 256 rows 25, 21
-//   V = 151936 64 rows 20, 31; 112 rows 29, 31; 160 rows 34, 31
-//   V = 1024   64 rows 15, 14       V = 10000  64 rows 16, 15
+//   V = 1024   64 rows 15, 13       V = 4096   448 rows 17, 21     V = 12800  320 rows 18, 18
+//   V = 20000  320 rows 19, 23; 448 rows 22, 22
+//   V = 50400  112 rows 18, 20; 144 rows 19, 21; 240 rows 25, 21
+//   V = 151936 64 rows 21, 29; 112 rows 30, 30; 144 rows 35, 30
 // K = 8 and 500 and float32 take the same bounds. Over 594 points (both types, K = 8, 64, 500, rows of
 // 128 to 30000 vectors, 64 to 448 rows) the side that the rule takes is 12% the faster one on average, and at
 // 101 of them the slower one by more than 3%. The largest of those, us in parts and fused:

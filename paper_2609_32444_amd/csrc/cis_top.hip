@@ -8,7 +8,7 @@ namespace cis {
 // One wave per chunk of kScanVecs vectors, 8 of them per lane: the chunk's largest logit, the sum of
 // its exponentials relative to that, and the groups' largest logits (TokScan). Reads the logits
 // once; the workgroups are short-lived and many, which suits a read-only stream here. Bound by the
-// memory: 6000 rows of V = 151936 in 288 us (6.3 TB/s), 512 rows in 24 us (6.4 TB/s). Loads of more
+// memory: 6000 rows of V = 151936 in 299 us (6.1 TB/s), 512 rows in 25 us (6.2 TB/s). Loads of more
 // logits than the memory-side cache holds are marked as not used again (6000 rows, K = 256: 54 us
 // less); those of fewer are not (512 uncut rows, which are read again: 70 to 65 us).
 // ------------------------------------------------------------------------------------------
@@ -96,8 +96,8 @@ const void* scan_kernel(int dtype, int32_t gv, bool keep) {
 //      the same bits wherever it is formed, so that nothing of the listed tokens is left over;
 //      where less than 2^-28 of the row remains, the row is summed again without them.
 // Where the list overflows (a row of many equal logits) the cut is found in passes over the row.
-// Bound by the groups' lines, which lie apart: 6000 rows, K = 256, in 130 us (some 600 lines of 128
-// bytes a row); and for few rows by the steps' latency: 96 rows, K = 8, in 13 us.
+// Bound by the groups' lines, which lie apart: 6000 rows, K = 256, in 136 us (some 600 lines of 128
+// bytes a row); and for few rows by the steps' latency: 96 rows, K = 8, in 14 us.
 // ------------------------------------------------------------------------------------------
 template <class E, int BLOCK, int LIST>
 __global__ __launch_bounds__(BLOCK) __attribute__((amdgpu_waves_per_eu(4))) void cis_top_kernel(
