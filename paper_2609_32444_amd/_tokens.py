@@ -91,11 +91,9 @@ def _per_row(name, x, T, dtype, dev):
 
 
 def _top_k(k):
-    """top_k as the library's int32 (a ctypes field takes the low bits of a larger one)."""
-    k = int(k)
-    if not -2 ** 31 <= k < 2 ** 31:
-        raise ValueError(f"top_k must be an int32, got {k}")
-    return k
+    """top_k as the library's int32: more than that is more than any row has, and a negative one stays
+    one (a ctypes field takes the low bits of what does not fit)."""
+    return max(-1, min(int(k), 2 ** 31 - 1))
 
 
 class SampleCall(_Call):

@@ -694,9 +694,13 @@ def test_shared_lists_are_refused():
     _check_distill(z[:1], ids[:1], values[:1], None, out)
 
 
-def test_top_k_beyond_int32_is_refused():
-    with pytest.raises(ValueError, match="int32"):
-        cis.sample(torch.zeros(2, 64, device=DEV), torch.zeros(2, device=DEV), top_k=2 ** 32 + 5)
+def test_top_k_beyond_int32_keeps_every_token():
+    logits = _store(_logits(40, 500, 3), torch.float32)
+    u = torch.rand(40, generator=_gen(5), device=DEV)
+    for k in (2 ** 31, 2 ** 32 + 5):
+        _check_sample(logits, u, cis.sample(logits, u, top_k=k), top_k=0)
+    with pytest.raises(cis.CisError):
+        cis.sample(logits, u, top_k=-2 ** 32)
 
 
 @pytest.mark.parametrize("dtype,T", [(torch.bfloat16, 2100), (torch.float32, 1050)])

@@ -183,10 +183,14 @@ def test_lists_whose_rows_share_storage_are_refused():
             assert _tokens._list_stride(*lists(step, rows), rows, K) == K
 
 
-def test_top_k_beyond_int32_is_refused():
-    """The library's field holds 32 bits: 2^32 + 5 would be 5 there."""
-    for k in (0, 5, 2 ** 31 - 1, -3):
-        assert _tokens._SampleParams(1.0, _tokens._top_k(k), 1.0, 0.0).top_k == k
-    for k in (2 ** 31, 2 ** 32, 2 ** 32 + 5, -2 ** 31 - 1):
-        with pytest.raises(ValueError, match="int32"):
-            _tokens._top_k(k)
+def test_top_k_beyond_int32_stays_beyond_every_row():
+    """The library's field holds 32 bits: 2^32 + 5 would be 5 there, 2^31 negative."""
+    def field(k):
+        return _tokens._SampleParams(1.0, _tokens._top_k(k), 1.0, 0.0).top_k
+
+    for k in (0, 5, 2 ** 31 - 1):
+        assert field(k) == k
+    for k in (2 ** 31, 2 ** 32, 2 ** 32 + 5, 2 ** 80):
+        assert field(k) == 2 ** 31 - 1   # V is 2^28 at most
+    for k in (-1, -3, -2 ** 31 - 1, -2 ** 32):
+        assert field(k) < 0
