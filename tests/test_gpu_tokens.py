@@ -720,3 +720,17 @@ def test_lists_and_draws_of_logits_beyond_the_caches(dtype, T):
     for s in (dict(), dict(top_k=20), dict(top_k=2000), dict(top_p=0.9),
               dict(top_k=900, top_p=0.8, min_p=0.001)):
         _check_sample(logits[rows], u[rows], some(cis.sample(logits, u, **s)), **s)
+
+
+@pytest.mark.parametrize("dtype", DTYPES)
+@pytest.mark.parametrize("temp", [2.0 ** -64, 1e-9, 1e-3, 30.0, 2.0 ** 64])
+@pytest.mark.parametrize("V", [40, 3000, 60000])
+def test_top_tail_at_the_ends_of_the_temperatures(V, temp, dtype):
+    """The tail far from 0, where all but one of its terms vanish, and where all are alike."""
+    z = _logits(5, V, 17)
+    z[1] += 100.0
+    z[2] -= 3000.0
+    z[3, :V // 2] = torch.finfo(torch.bfloat16).min * 1e-20
+    logits = _store(z, dtype)
+    for K in (1, 30, 300):
+        _check_top(logits, K, cis.top_logits(logits, K, temperature=temp), temp)
