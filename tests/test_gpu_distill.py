@@ -462,3 +462,13 @@ def test_loss_alone_of_logits_beyond_the_caches(dtype, T):
     assert case[0].stride(0) * T * dtype.itemsize > 192 << 20
     rows = _some_rows(T, 25)
     _check(*case[:4], cis.distill_fwd(*case), rows=rows, stats=False, weight=case[4], mask=case[5])
+
+
+@pytest.mark.parametrize("dtype", DTYPES)
+def test_more_rows_than_a_launch_takes(dtype):
+    """2^20 rows are one launch of a wave each; the fused pass takes any number in rounds."""
+    T, V = (1 << 20) + 77, 24
+    case = _mixed(T, V, 6, dtype, 9)
+    rows = [0, 5, (1 << 20) - 1, 1 << 20, (1 << 20) + 1, T - 1]
+    for kind in (cis.KL_FORWARD, cis.KL_REVERSE):
+        _check_mixed(case, kind, rows)

@@ -734,3 +734,22 @@ def test_top_tail_at_the_ends_of_the_temperatures(V, temp, dtype):
     logits = _store(z, dtype)
     for K in (1, 30, 300):
         _check_top(logits, K, cis.top_logits(logits, K, temperature=temp), temp)
+
+
+@pytest.mark.parametrize("dtype", DTYPES)
+def test_more_rows_than_a_launch_takes(dtype):
+    """2^20 rows are one launch of a workgroup each."""
+    T, V = (1 << 20) + 77, 24
+    logits = _store(_logits(T, V, 19), dtype)
+    u = torch.rand(T, generator=_gen(20), device=DEV)
+    rows = torch.tensor([0, 5, (1 << 20) - 1, 1 << 20, (1 << 20) + 1, T - 1], device=DEV)
+
+    def some(out):
+        return {k: v[rows] for k, v in out.items() if k != "workspace"}
+
+    for s in (dict(), dict(top_k=3), dict(top_p=0.7, min_p=0.1), dict(temperature=0.0)):
+        kw = {{"temperature": "temp"}.get(k, k): v for k, v in s.items()}
+        out = cis.sample(logits, u, **s)
+        assert (out["ids"] >= 0).all()
+        _check_sample(logits[rows], u[rows], some(out), **kw)
+    _check_top(logits[rows], 5, some(cis.top_logits(logits, 5)))
