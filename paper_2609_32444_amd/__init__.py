@@ -44,6 +44,15 @@ from ._binding import (  # noqa: F401
     workspace_bytes,
     workspace_bytes_ex,
 )
+from ._norm import (  # noqa: F401
+    NORM_GROUPS,
+    NORM_MAX_H,
+    RmsNormCall,
+    RmsNormGradCall,
+    rms_norm,
+    rms_norm_bwd,
+    rms_norm_workspace_bytes,
+)
 from ._tokens import (  # noqa: F401
     KL_FORWARD,
     KL_REVERSE,
@@ -70,4 +79,6 @@ __all__ = [
     "KL_FORWARD", "KL_REVERSE", "TOP_MAX_K", "DistillCall", "SampleCall", "TopLogitsCall",
     "distill_bwd", "distill_fwd", "distill_workspace_bytes", "sample", "sample_workspace_bytes",
     "top_logits", "top_logits_workspace_bytes",
+    "NORM_GROUPS", "NORM_MAX_H", "RmsNormCall", "RmsNormGradCall", "rms_norm", "rms_norm_bwd",
+    "rms_norm_workspace_bytes",
 ]

@@ -7,29 +7,14 @@
 
 #include <mutex>
 
+#include "cis_host.h"
 #include "cis_tok.h"
 
 namespace {
 
+using namespace cis::host;
+
 constexpr int64_t kMaxV = int64_t(1) << 28;
-constexpr int kMaxDevices = 64;
-
-// Compute units of the current device, or CIS_ERR_DEVICE.
-int device_cus() {
-  static std::mutex mu;
-  static int cus[kMaxDevices] = {};   // 0: not looked at yet
-  int dev = -1;
-  if (hipGetDevice(&dev) != hipSuccess || dev < 0 || dev >= kMaxDevices) return CIS_ERR_DEVICE;
-  std::lock_guard<std::mutex> lk(mu);
-  if (cus[dev] == 0) {
-    hipDeviceProp_t prop;
-    if (hipGetDeviceProperties(&prop, dev) != hipSuccess) return CIS_ERR_DEVICE;
-    cus[dev] = strncmp(prop.gcnArchName, "gfx950", 6) == 0 ? prop.multiProcessorCount
-                                                           : CIS_ERR_DEVICE;
-  }
-  return cus[dev];
-}
-
 // Workgroups of a kernel that a compute unit holds at once. (The devices are all gfx950.)
 int blocks_per_cu(const void* fn, int block) {
   static std::mutex mu;
@@ -47,17 +32,6 @@ int blocks_per_cu(const void* fn, int block) {
   return n;
 }
 
-bool aligned(const void* p, size_t a) { return ((uintptr_t)p % a) == 0; }
-bool known(int dtype) { return dtype == CIS_BF16 || dtype == CIS_F32; }
-int elem_bytes(int dtype) { return dtype == CIS_BF16 ? 2 : 4; }
-
-int launch(const void* fn, int64_t grid, int block, void* arg, hipStream_t stream) {
-  void* args[] = {arg};
-  return hipLaunchKernel(fn, dim3((unsigned)grid), dim3(block), args, 0, stream) == hipSuccess
-             ? CIS_OK
-             : CIS_ERR_LAUNCH;
-}
-
 // The rows' shape; pointers and alignment follow once every size has been found right.
 int check_shape(int dtype, int64_t T, int64_t V, int64_t ld) {
   if (!known(dtype)) return CIS_ERR_DTYPE;
@@ -68,11 +42,6 @@ int check_shape(int dtype, int64_t T, int64_t V, int64_t ld) {
 bool aligned_rows(const void* p, int dtype, int64_t ld) {
   return aligned(p, 16) && (ld * elem_bytes(dtype)) % 16 == 0;
 }
-int check_workspace(const void* workspace, size_t have, size_t need) {
-  if (!aligned(workspace, 256)) return CIS_ERR_ALIGN;
-  return have < need ? CIS_ERR_WORKSPACE : CIS_OK;
-}
-
 int32_t row_vecs(int64_t V, int dtype) {
   const int epv = 16 / elem_bytes(dtype);
   return (int32_t)((V + epv - 1) / epv);
