@@ -39,14 +39,22 @@ struct NormGradArgs {
   float* dw;
 };
 
-constexpr int kNormBlock = 1024;
+constexpr int kNormBlock = 1024;              // threads to a row that goes in passes
 constexpr int kNormColumns = 256;             // threads of 8 columns each in a part of dweight's sums
-constexpr uint32_t kNormParts = 256;
-constexpr int kNormReduce = 1024, kNormReduceCols = 64;
+constexpr int kNormReduce = 1024, kNormReduceCols = 16;
+constexpr int32_t kNormGradResident = 16384;  // elements of a row up to which the gradients take one pass
 
+// The kernel for rows of H elements, with `lanes` lanes to a row, or in passes over it (0: one workgroup of
+// kNormBlock threads per row).
+struct NormVariant {
+  int lanes;
+  const void* fn;
+};
+inline int norm_block(int lanes) { return lanes == 0 ? kNormBlock : lanes > 256 ? lanes : 256; }
+inline int norm_block_rows(int lanes) { return lanes == 0 ? 1 : norm_block(lanes) / lanes; }
 // x and stream in float32 or bf16; res: a residual is added
-const void* norm_kernel(bool x_f32, bool stream_f32, bool res);
-const void* norm_grad_kernel(bool dy_f32, bool x_f32);
+NormVariant norm_kernel(int32_t H, bool x_f32, bool stream_f32, bool res);
+NormVariant norm_grad_kernel(int32_t H, bool dy_f32, bool x_f32);
 const void* norm_rstd_kernel(bool x_f32);
 const void* norm_part_kernel(bool dy_f32, bool x_f32);
 const void* norm_reduce_kernel();

@@ -1,8 +1,9 @@
 // RMS norm kernels (gfx950): forward with the residual's addition, in 16, 32 or 8 bits, and backward.
 //
-// A row is taken in groups of 8 elements. Sums of squares and of products are in double: squares of
-// float32 values neither overflow nor vanish there, and the extra cost, a conversion an element, is
-// hidden behind the memory.
+// A row is taken in groups of 8 elements, which LANES lanes hold in registers (a part of a wave, a wave
+// or a workgroup to a row); rows beyond that go in passes. Sums of squares and of products are in
+// double: squares of float32 values neither overflow nor vanish there, and the extra cost, a conversion
+// an element, is hidden behind the memory.
 #include <type_traits>
 
 #include "cis_norm.h"
@@ -17,21 +18,55 @@ struct Raw {
   u32x4 v[kVecs<E>];
 };
 
+// Unpacked again from here on, rather than kept unpacked (see opaque()).
+template <class E, int NV>
+__device__ __forceinline__ void hold(Raw<E> (&x)[NV]) {
+  static_for<NV>([&](auto I) __attribute__((always_inline)) { opaque(x[I].v); });
+}
+
 __device__ __forceinline__ char* row_at(const NormRows& m, uint32_t row, uint32_t N) {
   if (N == 1) return m.p + (int64_t)row * m.st;
   const uint32_t t = row / N;
   return m.p + (int64_t)t * m.st + (int64_t)(row - t * N) * m.sn;
 }
 
-// Group g of a row of nvec vectors; beyond the row its last vector again.
-template <class E>
-__device__ __forceinline__ Raw<E> load_raw(const char* row, int g, int nvec) {
+// A row: an address, or where it is the whole wave's a descriptor of its vectors, beyond which loads give
+// zeros and stores are dropped.
+struct RowPtr {
+  char* p;
+  int nvec;
+  __device__ __forceinline__ u32x4 load(int v) const {   // beyond the row its last vector again
+    return *(const u32x4*)(p + 16 * (int64_t)(v < nvec ? v : nvec - 1));
+  }
+  __device__ __forceinline__ void store(int v, u32x4 x) const { *(u32x4*)(p + 16 * (int64_t)v) = x; }
+  __device__ __forceinline__ void store2(int v, u32x2 x) const { *(u32x2*)(p + 8 * (int64_t)v) = x; }
+};
+struct RowBuf {
+  char* p;
+  __amdgpu_buffer_rsrc_t r;
+  __device__ __forceinline__ u32x4 load(int v) const { return bload_aux<0>(r, (uint32_t)v * 16u); }
+  __device__ __forceinline__ void store(int v, u32x4 x) const {
+    __builtin_amdgcn_raw_buffer_store_b128(x, r, (uint32_t)v * 16u, 0, 0);
+  }
+  __device__ __forceinline__ void store2(int v, u32x2 x) const {
+    __builtin_amdgcn_raw_buffer_store_b64(x, r, (uint32_t)v * 8u, 0, 0);
+  }
+};
+template <bool WAVE>
+__device__ __forceinline__ auto row_of(const NormRows& m, uint32_t row, uint32_t N, int nvec) {
+  char* p = row_at(m, row, N);
+  if constexpr (WAVE)
+    return RowBuf{p, make_rsrc(p, (uint32_t)nvec * 16u)};
+  else
+    return RowPtr{p, nvec};
+}
+
+// Group g of a row.
+template <class E, class R>
+__device__ __forceinline__ Raw<E> load_raw(const R& row, int g) {
   Raw<E> x;
 #pragma unroll
-  for (int k = 0; k < kVecs<E>; ++k) {
-    const int v = g * kVecs<E> + k;
-    x.v[k] = *(const u32x4*)(row + 16 * (int64_t)(v < nvec ? v : nvec - 1));
-  }
+  for (int k = 0; k < kVecs<E>; ++k) x.v[k] = row.load(g * kVecs<E> + k);
   return x;
 }
 // Its elements; 0 past the row's end.
@@ -56,20 +91,20 @@ __device__ __forceinline__ void round_to(float (&f)[8]) {
     E::unpack(b, f);
   }
 }
-template <class E>
-__device__ __forceinline__ void store8(char* row, int g, int H, const float (&f)[8]) {
+template <class E, class R>
+__device__ __forceinline__ void store8(const R& row, int g, int H, const float (&f)[8]) {
   if ((g + 1) * 8 <= H) {
 #pragma unroll
     for (int k = 0; k < kVecs<E>; ++k) {
       float t[E::kPerVec];
 #pragma unroll
       for (int e = 0; e < E::kPerVec; ++e) t[e] = f[k * E::kPerVec + e];
-      *(u32x4*)(row + 16 * (int64_t)(g * kVecs<E> + k)) = E::pack(t);
+      row.store(g * kVecs<E> + k, E::pack(t));
     }
   } else {
 #pragma unroll
     for (int e = 0; e < 8; ++e)
-      if (g * 8 + e < H) E::store_elem(row, g * 8 + e, E::bits_of(f[e]));
+      if (g * 8 + e < H) E::store_elem(row.p, g * 8 + e, E::bits_of(f[e]));
   }
 }
 // The weight's group, which is not read past its end.
@@ -79,9 +114,9 @@ __device__ __forceinline__ void load_weight(const void* w, bool f32, int g, int 
     for (int e = 0; e < 8; ++e) f[e] = 1.f;
   } else if ((g + 1) * 8 <= H) {
     if (f32)
-      unpack8<F32>(load_raw<F32>((const char*)w, g, INT32_MAX), g, H, f);
+      unpack8<F32>(load_raw<F32>(RowPtr{(char*)w, INT32_MAX}, g), g, H, f);
     else
-      unpack8<Bf16>(load_raw<Bf16>((const char*)w, g, INT32_MAX), g, H, f);
+      unpack8<Bf16>(load_raw<Bf16>(RowPtr{(char*)w, INT32_MAX}, g), g, H, f);
   } else {
 #pragma unroll
     for (int e = 0; e < 8; ++e) {
@@ -121,7 +156,8 @@ __device__ __forceinline__ float e4m3_scale(uint32_t size) {
   const float s = __uint_as_float(size) / 448.f;
   return s < 0x1p-126f ? 0x1p-126f : s;
 }
-__device__ __forceinline__ void store_e4m3(char* row, int g, int H, const float (&f)[8], float inv) {
+template <class R>
+__device__ __forceinline__ void store_e4m3(const R& row, int g, int H, const float (&f)[8], float inv) {
   uint32_t b[2];
 #pragma unroll
   for (int k = 0; k < 2; ++k) {
@@ -129,15 +165,315 @@ __device__ __forceinline__ void store_e4m3(char* row, int g, int H, const float 
     b[k] = __builtin_amdgcn_cvt_pk_fp8_f32(f[4 * k + 2] * inv, f[4 * k + 3] * inv, b[k], true);
   }
   if ((g + 1) * 8 <= H) {
-    *(u32x2*)(row + 8 * (int64_t)g) = u32x2{b[0], b[1]};
+    row.store2(g, u32x2{b[0], b[1]});
   } else {
 #pragma unroll
     for (int e = 0; e < 8; ++e)
-      if (g * 8 + e < H) row[g * 8 + e] = (char)(b[e / 4] >> (8 * (e % 4)));
+      if (g * 8 + e < H) row.p[g * 8 + e] = (char)(b[e / 4] >> (8 * (e % 4)));
   }
+}
+__device__ __forceinline__ int vecs_of(int dtype, int H) {
+  return dtype == CIS_E4M3 ? (H + 15) / 16 : dtype == CIS_F32 ? (H + 3) / 4 : (H + 7) / 8;
 }
 __device__ __forceinline__ float rstd_of(double ss, int H, float eps) {
   return (float)(1.0 / sqrt(ss / (double)H + (double)eps));
+}
+
+// The weight's groups as they are stored, asked for without waiting: ones where there is no weight, zeros
+// past its end, beyond which it is not read.
+// (Values are chosen, not stores: else the arrays end up in scratch memory.)
+template <int LANES, int NV>
+struct WeightRow {
+  u32x4 lo[NV], hi[NV];
+  __device__ __forceinline__ void load(const void* w, bool f32, int l, int H) {
+    const int nvec = f32 ? H / 4 : H / 8;   // whole ones
+    const uint32_t one = w ? 0u : f32 ? 0x3F800000u : 0x3F803F80u;
+    const u32x4 none{one, one, one, one};
+    const bool any = w && nvec > 0;
+    auto at = [&](int i) {
+      u32x4 x = none;
+      if (any) x = *(const u32x4*)((const char*)w + 16 * (int64_t)(i < nvec ? i : nvec - 1));
+      return i < nvec ? x : none;
+    };
+    static_for<NV>([&](auto I) __attribute__((always_inline)) {
+      const int g = l + I * LANES;
+      lo[I] = at(f32 ? 2 * g : g);
+      hi[I] = none;
+      if (f32) hi[I] = at(2 * g + 1);
+    });
+    const int h0 = nvec * (f32 ? 4 : 8);
+    if (w && h0 < H) {   // the vector that it ends in
+      uint32_t x[4] = {0, 0, 0, 0};
+#pragma unroll
+      for (int e = 0; e < 4; ++e)
+        if (f32) {
+          if (h0 + e < H) x[e] = ((const uint32_t*)w)[h0 + e];
+        } else {
+          if (h0 + 2 * e < H) x[e] = ((const uint16_t*)w)[h0 + 2 * e];
+          if (h0 + 2 * e + 1 < H) x[e] |= (uint32_t)((const uint16_t*)w)[h0 + 2 * e + 1] << 16;
+        }
+      const u32x4 last{x[0], x[1], x[2], x[3]};
+      static_for<NV>([&](auto I) __attribute__((always_inline)) {
+        const int g = l + I * LANES;
+        lo[I] = (f32 ? 2 * g : g) == nvec ? last : lo[I];
+        hi[I] = f32 && 2 * g + 1 == nvec ? last : hi[I];
+      });
+    }
+  }
+  template <int I>
+  __device__ __forceinline__ void get(bool f32, float (&f)[8]) const {
+    if (f32) {
+#pragma unroll
+      for (int e = 0; e < 4; ++e) {
+        f[e] = __uint_as_float(lo[I][e]);
+        f[e + 4] = __uint_as_float(hi[I][e]);
+      }
+    } else {
+      Bf16::unpack(lo[I], f);
+    }
+  }
+};
+
+// Sums and maxima over the LANES lanes of a row, in each of them. `sh` may be used again after the next
+// barrier.
+template <int LANES>
+__device__ __forceinline__ double lanes_sum(double x, double* sh) {
+  if constexpr (LANES > 64) {
+    return block_sum<LANES / 64>(x, sh);
+  } else if constexpr (LANES == 64) {
+    return wave_sum(x);
+  } else {
+    auto step = [](double y, auto ctrl) {
+      constexpr int C = ctrl;
+      const u64 b = __builtin_bit_cast(u64, y);
+      return __builtin_bit_cast(double, ((u64)dpp_word<C>((uint32_t)(b >> 32)) << 32) |
+                                            dpp_word<C>((uint32_t)b));
+    };
+    x = wave_reduce(x, step);
+    return LANES == 16 ? x : x + __shfl_xor(x, 16, 64);
+  }
+}
+template <int LANES>
+__device__ __forceinline__ uint32_t row_max(uint32_t m, uint32_t* sh) {
+  m = lanes_max(m, 16);
+#pragma unroll
+  for (int l = 16; l < 64 && l < LANES; l += l) {
+    const uint32_t o = __shfl_xor(m, l, 64);
+    m = o > m ? o : m;
+  }
+  if constexpr (LANES > 64) {
+    if ((threadIdx.x & 63) == 0) sh[threadIdx.x >> 6] = m;
+    __syncthreads();
+    for (int w = 0; w < LANES / 64; ++w) m = sh[w] > m ? sh[w] : m;
+  }
+  return m;
+}
+
+// ------------------------------------------------------------------------------------------
+// LANES lanes to a row, which holds at most 8 * NV * LANES elements.
+// ------------------------------------------------------------------------------------------
+template <int LANES>
+constexpr int kRowBlock = LANES > 256 ? LANES : 256;   // threads of a workgroup
+template <class X, class S, bool RES, int LANES, int NV>
+__global__ __launch_bounds__(kRowBlock<LANES>) void cis_norm_row_kernel(const NormArgs a) {
+  constexpr int NW = LANES > 64 ? LANES / 64 : 1, R = kRowBlock<LANES> / LANES;
+  __shared__ double sh[NW];
+  __shared__ uint32_t shm[NW];
+  const int H = a.H, n8 = (H + 7) / 8;
+  const int xv = (H + X::kPerVec - 1) / X::kPerVec, sv = (H + S::kPerVec - 1) / S::kPerVec;
+  const int l = threadIdx.x % LANES;
+  uint32_t at = threadIdx.x / LANES;
+  if (LANES >= 64) at = __builtin_amdgcn_readfirstlane(at);
+  uint32_t row = a.row0 + blockIdx.x * R + at;
+  const bool on = row < a.rows;
+  if (!on) row = a.rows - 1;
+  constexpr bool WAVE = LANES >= 64;
+  const auto x = row_of<WAVE>(a.x, row, a.N, xv), r = row_of<WAVE>(RES ? a.r : a.x, row, a.N, sv);
+  const auto y = row_of<WAVE>(a.y, row, a.N, vecs_of(a.ydt, H));
+  Raw<X> rx[NV];
+  Raw<S> rr[RES ? NV : 1];
+  static_for<NV>([&](auto I) __attribute__((always_inline)) {
+    rx[I] = load_raw<X>(x, l + I * LANES);
+    if constexpr (RES) rr[I] = load_raw<S>(r, l + I * LANES);
+  });
+  WeightRow<LANES, NV> w;
+  w.load(a.w, a.w_f32, l, H);
+  float f[NV][8];
+  double ss = 0.0;
+  static_for<NV>([&](auto I) __attribute__((always_inline)) {
+    const int g = l + I * LANES;
+    unpack8<X>(rx[I], g, H, f[I]);
+    if constexpr (RES) {
+      float t[8];
+      unpack8<S>(rr[I], g, H, t);
+#pragma unroll
+      for (int e = 0; e < 8; ++e) f[I][e] += t[e];
+      round_to<S>(f[I]);
+    }
+#pragma unroll
+    for (int e = 0; e < 8; ++e) ss = fma((double)f[I][e], (double)f[I][e], ss);
+  });
+  const float rstd = rstd_of(lanes_sum<LANES>(ss, sh), H, a.eps);
+  if (RES && a.s.p && on) {   // (all of the row has been read)
+    const auto s = row_of<WAVE>(a.s, row, a.N, sv);
+    static_for<NV>([&](auto I) __attribute__((always_inline)) {
+      if (l + I * LANES < n8) store8<S>(s, l + I * LANES, H, f[I]);
+    });
+  }
+  static_for<NV>([&](auto I) __attribute__((always_inline)) {
+    float t[8];
+    w.template get<I>(a.w_f32, t);
+#pragma unroll
+    for (int e = 0; e < 8; ++e) f[I][e] = f[I][e] * rstd * t[e];
+  });
+  if (a.ydt == CIS_E4M3) {
+    float inv = 0.f;
+    if (a.group == 0) {
+      uint32_t m = 0;
+      static_for<NV>([&](auto I) __attribute__((always_inline)) {
+        const uint32_t b = l + I * LANES < n8 ? size_of8(f[I]) : 0;
+        m = b > m ? b : m;
+      });
+      const float scale = e4m3_scale(row_max<LANES>(m, shm));
+      if (l == 0 && on) a.scale[row] = scale;
+      inv = 1.f / scale;
+    }
+    const int lanes = a.group / 8;
+    static_for<NV>([&](auto I) __attribute__((always_inline)) {
+      const int g = l + I * LANES;
+      if (a.group) {
+        const float scale = e4m3_scale(lanes_max(g < n8 ? size_of8(f[I]) : 0, lanes));
+        if (g < n8 && (g & (lanes - 1)) == 0 && on) a.scale[(int64_t)row * a.blocks + g / lanes] = scale;
+        inv = 1.f / scale;
+      }
+      if (g < n8 && on) store_e4m3(y, g, H, f[I], inv);
+    });
+  } else if (on) {
+    static_for<NV>([&](auto I) __attribute__((always_inline)) {
+      const int g = l + I * LANES;
+      if (g < n8) {
+        if (a.ydt == CIS_F32)
+          store8<F32>(y, g, H, f[I]);
+        else
+          store8<Bf16>(y, g, H, f[I]);
+      }
+    });
+  }
+}
+
+// The gradients, with rows that a workgroup's lanes take in turn and dweight's sums in registers; a
+// workgroup's are a part.
+template <class D, class X, int LANES, int NV>
+__global__ __launch_bounds__(kRowBlock<LANES>) void cis_norm_grad_row_kernel(const NormGradArgs a) {
+  constexpr int NW = LANES > 64 ? LANES / 64 : 1, BLOCK = kRowBlock<LANES>, R = BLOCK / LANES;
+  __shared__ double sh[2][2][NW];
+  __shared__ float sum[R > 1 ? BLOCK : 1][9];
+  const int H = a.H, n8 = (H + 7) / 8;
+  const int dv = (H + D::kPerVec - 1) / D::kPerVec, xv = (H + X::kPerVec - 1) / X::kPerVec;
+  const int rv = a.dx_f32 ? (H + 3) / 4 : n8;
+  constexpr bool WAVE = LANES >= 64;
+  const int l0 = threadIdx.x % LANES;
+  uint32_t at = threadIdx.x / LANES;
+  if (LANES >= 64) at = __builtin_amdgcn_readfirstlane(at);
+  WeightRow<LANES, NV> w;
+  w.load(a.w, a.w_f32, l0, H);
+  float acc[NV][8] = {};
+  int turn = 0;
+  for (uint64_t row0 = (uint64_t)blockIdx.x * R; row0 < a.rows; row0 += (uint64_t)gridDim.x * R) {
+    int l = l0;
+    asm volatile("" : "+v"(l));   // (else what follows from it, and the weight unpacked, is kept for all rows)
+    opaque(w.lo);
+    opaque(w.hi);
+    const bool on = row0 + at < a.rows;
+    const uint32_t row = on ? (uint32_t)row0 + at : a.rows - 1;
+    const auto x = row_of<WAVE>(a.x, row, a.N, xv), dy = row_of<WAVE>(a.dy, row, a.N, dv);
+    Raw<X> rx[NV];
+    Raw<D> rd[NV];
+    static_for<NV>([&](auto I) __attribute__((always_inline)) {
+      rx[I] = load_raw<X>(x, l + I * LANES);
+      rd[I] = load_raw<D>(dy, l + I * LANES);
+    });
+    u32x4 lo[NV], hi[NV];   // dr
+    static_for<NV>([&](auto I) __attribute__((always_inline)) { lo[I] = hi[I] = u32x4{0, 0, 0, 0}; });
+    if (a.dr.p) {
+      const auto dr = row_of<WAVE>(a.dr, row, a.N, rv);
+      static_for<NV>([&](auto I) __attribute__((always_inline)) {
+        const int g = l + I * LANES;
+        lo[I] = dr.load(a.dx_f32 ? 2 * g : g);
+        if (a.dx_f32) hi[I] = dr.load(2 * g + 1);
+      });
+    }
+    double ss = 0.0, dot = 0.0;
+    static_for<NV>([&](auto I) __attribute__((always_inline)) {
+      const int g = l + I * LANES;
+      float f[8], d[8], t[8];
+      unpack8<X>(rx[I], g, H, f);
+      unpack8<D>(rd[I], g, H, d);
+      w.template get<I>(a.w_f32, t);
+#pragma unroll
+      for (int e = 0; e < 8; ++e) {
+        ss = fma((double)f[e], (double)f[e], ss);
+        dot = fma((double)f[e], (double)(d[e] * t[e]), dot);
+      }
+      slot_fence();
+    });
+    hold(rx);
+    hold(rd);
+    ss = lanes_sum<LANES>(ss, sh[turn][0]);
+    dot = lanes_sum<LANES>(dot, sh[turn][1]);
+    turn ^= 1;   // (a wave may be a row ahead of another's reading)
+    const float rstd = rstd_of(ss, H, a.eps), mean = (float)(dot * (double)rstd / (double)H);
+    if (!on) continue;
+    const auto dx = row_of<WAVE>(a.dx, row, a.N, rv);
+    static_for<NV>([&](auto I) __attribute__((always_inline)) {
+      const int g = l + I * LANES;
+      if (g < n8) {
+        float f[8], d[8], t[8];
+        unpack8<X>(rx[I], g, H, f);
+        unpack8<D>(rd[I], g, H, d);
+        w.template get<I>(a.w_f32, t);
+#pragma unroll
+        for (int e = 0; e < 8; ++e) {
+          const float xh = f[e] * rstd;
+          acc[I][e] = fmaf(d[e], xh, acc[I][e]);
+          t[e] = rstd * (d[e] * t[e] - xh * mean);
+        }
+        if (a.dr.p) {
+          if (a.dx_f32)
+            unpack8<F32>(Raw<F32>{{lo[I], hi[I]}}, g, H, f);
+          else
+            unpack8<Bf16>(Raw<Bf16>{{lo[I]}}, g, H, f);
+#pragma unroll
+          for (int e = 0; e < 8; ++e) t[e] += f[e];
+        }
+        if (a.dx_f32)
+          store8<F32>(dx, g, H, t);
+        else
+          store8<Bf16>(dx, g, H, t);
+      }
+      slot_fence();
+    });
+  }
+  if (!a.dw) return;
+  float* out = a.part + (int64_t)blockIdx.x * H;
+  static_for<NV>([&](auto I) __attribute__((always_inline)) {
+    const int g = l0 + I * LANES;
+    if constexpr (R > 1) {   // the rows' lanes, in order
+      __syncthreads();
+#pragma unroll
+      for (int e = 0; e < 8; ++e) sum[threadIdx.x][e] = acc[I][e];
+      __syncthreads();
+      if (threadIdx.x < LANES)
+        for (int k = 1; k < R; ++k)
+#pragma unroll
+          for (int e = 0; e < 8; ++e) acc[I][e] += sum[k * LANES + l0][e];
+    }
+    if (threadIdx.x < LANES) {
+#pragma unroll
+      for (int e = 0; e < 8; ++e)
+        if (g * 8 + e < H) out[g * 8 + e] = acc[I][e];
+    }
+  });
 }
 
 // ------------------------------------------------------------------------------------------
@@ -150,17 +486,17 @@ __global__ __launch_bounds__(kNormBlock) void cis_norm_kernel(const NormArgs a) 
   __shared__ uint32_t shm[NW];
   const int H = a.H, n8 = (H + 7) / 8;
   const int xv = (H + X::kPerVec - 1) / X::kPerVec, sv = (H + S::kPerVec - 1) / S::kPerVec;
-  const int tid = threadIdx.x, lane = tid & 63, wid = tid >> 6;
+  const int tid = threadIdx.x;
   const uint32_t row = a.row0 + blockIdx.x;
-  const char* x = row_at(a.x, row, a.N);
-  const char* r = RES ? row_at(a.r, row, a.N) : nullptr;
-  char* s = RES && a.s.p ? row_at(a.s, row, a.N) : nullptr;
-  char* y = row_at(a.y, row, a.N);
+  const RowPtr x = row_of<false>(a.x, row, a.N, xv), y = row_of<false>(a.y, row, a.N, 0);
+  RowPtr r{}, s{};
+  if (RES) r = row_of<false>(a.r, row, a.N, sv);
+  if (RES && a.s.p) s = row_of<false>(a.s, row, a.N, sv);
   auto sum8 = [&](int g, float (&f)[8]) {
-    unpack8<X>(load_raw<X>(x, g, xv), g, H, f);
+    unpack8<X>(load_raw<X>(x, g), g, H, f);
     if constexpr (RES) {
       float t[8];
-      unpack8<S>(load_raw<S>(r, g, sv), g, H, t);
+      unpack8<S>(load_raw<S>(r, g), g, H, t);
 #pragma unroll
       for (int e = 0; e < 8; ++e) f[e] += t[e];
       round_to<S>(f);
@@ -170,7 +506,7 @@ __global__ __launch_bounds__(kNormBlock) void cis_norm_kernel(const NormArgs a) 
   for (int g = tid; g < n8; g += kNormBlock) {
     float f[8];
     sum8(g, f);
-    if (s) store8<S>(s, g, H, f);
+    if (s.p) store8<S>(s, g, H, f);
 #pragma unroll
     for (int e = 0; e < 8; ++e) ss = fma((double)f[e], (double)f[e], ss);
   }
@@ -182,8 +518,8 @@ __global__ __launch_bounds__(kNormBlock) void cis_norm_kernel(const NormArgs a) 
 #pragma unroll
     for (int e = 0; e < 8; ++e) f[e] = 0.f;
     if (g >= n8) return;
-    if (s)
-      unpack8<S>(load_raw<S>(s, g, sv), g, H, f);
+    if (s.p)
+      unpack8<S>(load_raw<S>(s, g), g, H, f);
     else
       sum8(g, f);
     load_weight(a.w, a.w_f32, g, H, w);
@@ -199,16 +535,7 @@ __global__ __launch_bounds__(kNormBlock) void cis_norm_kernel(const NormArgs a) 
       const uint32_t b = size_of8(f);
       m = b > m ? b : m;
     }
-    m = lanes_max(m, 16);
-#pragma unroll
-    for (int l = 16; l < 64; l += 16) {
-      const uint32_t o = __shfl_xor(m, l, 64);
-      m = o > m ? o : m;
-    }
-    if (lane == 0) shm[wid] = m;
-    __syncthreads();
-    for (int w = 0; w < NW; ++w) m = shm[w] > m ? shm[w] : m;
-    const float scale = e4m3_scale(m);
+    const float scale = e4m3_scale(row_max<kNormBlock>(m, shm));
     if (tid == 0) a.scale[row] = scale;
     inv = 1.f / scale;
   }
@@ -241,14 +568,14 @@ __global__ __launch_bounds__(kNormBlock) void cis_norm_grad_kernel(const NormGra
   const int H = a.H, n8 = (H + 7) / 8;
   const int dv = (H + D::kPerVec - 1) / D::kPerVec, xv = (H + X::kPerVec - 1) / X::kPerVec;
   const uint32_t row = a.row0 + blockIdx.x;
-  const char* dy = row_at(a.dy, row, a.N);
-  const char* x = row_at(a.x, row, a.N);
-  const char* dr = a.dr.p ? row_at(a.dr, row, a.N) : nullptr;
-  char* dx = row_at(a.dx, row, a.N);
+  const RowPtr dy = row_of<false>(a.dy, row, a.N, dv), x = row_of<false>(a.x, row, a.N, xv);
+  const RowPtr dx = row_of<false>(a.dx, row, a.N, 0);
+  RowPtr dr{};
+  if (a.dr.p) dr = row_of<false>(a.dr, row, a.N, a.dx_f32 ? (H + 3) / 4 : n8);
   auto load = [&](int g, float (&f)[8], float (&d)[8]) {
     float w[8];
-    unpack8<X>(load_raw<X>(x, g, xv), g, H, f);
-    unpack8<D>(load_raw<D>(dy, g, dv), g, H, d);
+    unpack8<X>(load_raw<X>(x, g), g, H, f);
+    unpack8<D>(load_raw<D>(dy, g), g, H, d);
     load_weight(a.w, a.w_f32, g, H, w);
 #pragma unroll
     for (int e = 0; e < 8; ++e) d[e] *= w[e];
@@ -271,12 +598,12 @@ __global__ __launch_bounds__(kNormBlock) void cis_norm_grad_kernel(const NormGra
     load(g, f, d);
 #pragma unroll
     for (int e = 0; e < 8; ++e) d[e] = rstd * (d[e] - f[e] * rstd * mean);
-    if (dr) {
+    if (dr.p) {
       float t[8];
       if (a.dx_f32)
-        unpack8<F32>(load_raw<F32>(dr, g, (H + 3) / 4), g, H, t);
+        unpack8<F32>(load_raw<F32>(dr, g), g, H, t);
       else
-        unpack8<Bf16>(load_raw<Bf16>(dr, g, n8), g, H, t);
+        unpack8<Bf16>(load_raw<Bf16>(dr, g), g, H, t);
 #pragma unroll
       for (int e = 0; e < 8; ++e) d[e] += t[e];
     }
@@ -293,11 +620,11 @@ __global__ __launch_bounds__(kNormBlock) void cis_norm_rstd_kernel(const NormGra
   __shared__ double sh[NW];
   const int H = a.H, n8 = (H + 7) / 8, xv = (H + X::kPerVec - 1) / X::kPerVec;
   const uint32_t row = a.row0 + blockIdx.x;
-  const char* x = row_at(a.x, row, a.N);
+  const RowPtr x = row_of<false>(a.x, row, a.N, xv);
   double ss = 0.0;
   for (int g = threadIdx.x; g < n8; g += kNormBlock) {
     float f[8];
-    unpack8<X>(load_raw<X>(x, g, xv), g, H, f);
+    unpack8<X>(load_raw<X>(x, g), g, H, f);
 #pragma unroll
     for (int e = 0; e < 8; ++e) ss = fma((double)f[e], (double)f[e], ss);
   }
@@ -316,8 +643,8 @@ __global__ __launch_bounds__(kNormColumns) void cis_norm_part_kernel(const NormG
   float acc[8] = {};
   for (uint64_t row = part; row < a.rows; row += a.parts) {
     float f[8], d[8];
-    unpack8<X>(load_raw<X>(row_at(a.x, (uint32_t)row, a.N), g, xv), g, H, f);
-    unpack8<D>(load_raw<D>(row_at(a.dy, (uint32_t)row, a.N), g, dv), g, H, d);
+    unpack8<X>(load_raw<X>(row_of<false>(a.x, (uint32_t)row, a.N, xv), g), g, H, f);
+    unpack8<D>(load_raw<D>(row_of<false>(a.dy, (uint32_t)row, a.N, dv), g), g, H, d);
     const float rstd = a.rstd[row];
 #pragma unroll
     for (int e = 0; e < 8; ++e) acc[e] = fmaf(d[e], f[e] * rstd, acc[e]);
@@ -328,37 +655,88 @@ __global__ __launch_bounds__(kNormColumns) void cis_norm_part_kernel(const NormG
     if (g * 8 + e < H) out[g * 8 + e] = acc[e];
 }
 
-// dweight from the parts, in double: a column per lane, the parts in turn over the waves.
+// dweight from the parts, in double: kNormReduceCols columns to a workgroup, the parts in turn over its
+// threads.
 __global__ __launch_bounds__(kNormReduce) void cis_norm_reduce_kernel(const NormGradArgs a) {
-  constexpr int NW = kNormReduce / kNormReduceCols;
-  __shared__ double sh[NW][kNormReduceCols];
-  const int lane = threadIdx.x % kNormReduceCols, wid = threadIdx.x / kNormReduceCols;
-  const int h = blockIdx.x * kNormReduceCols + lane;
+  constexpr int C = kNormReduceCols, P = kNormReduce / C;
+  __shared__ double sh[P][C + 1];
+  const int col = threadIdx.x % C, at = threadIdx.x / C;
+  const int h = blockIdx.x * C + col;
   double s = 0.0;
-  if (h < a.H)
-    for (uint32_t p = wid; p < a.parts; p += NW) s += (double)a.part[(int64_t)p * a.H + h];
-  sh[wid][lane] = s;
-  __syncthreads();
-  if (wid == 0 && h < a.H) {
-    for (int w = 1; w < NW; ++w) s += sh[w][lane];
-    a.dw[h] = (float)s;
+  if (h < a.H) {
+#pragma unroll 8
+    for (uint32_t p = at; p < a.parts; p += P) s += (double)a.part[(int64_t)p * a.H + h];
   }
+  sh[at][col] = s;
+#pragma unroll
+  for (int half = P / 2; half > 0; half /= 2) {
+    __syncthreads();
+    if (at < half) sh[at][col] += sh[at + half][col];
+  }
+  if (at == 0 && h < a.H) a.dw[h] = (float)sh[0][col];
 }
 
-const void* norm_kernel(bool x_f32, bool stream_f32, bool res) {
-  if (!res)
-    return x_f32 ? (const void*)&cis_norm_kernel<F32, F32, false>
-                 : (const void*)&cis_norm_kernel<Bf16, Bf16, false>;
-  if (x_f32) return (const void*)&cis_norm_kernel<F32, F32, true>;
-  return stream_f32 ? (const void*)&cis_norm_kernel<Bf16, F32, true>
-                    : (const void*)&cis_norm_kernel<Bf16, Bf16, true>;
+namespace {
+template <int LANES, int NV>
+NormVariant row_variant(bool x_f32, bool stream_f32, bool res) {
+#define CIS_NORM(X, S, RES) {LANES, (const void*)&cis_norm_row_kernel<X, S, RES, LANES, NV>}
+  if (!res) return x_f32 ? NormVariant CIS_NORM(F32, F32, false) : NormVariant CIS_NORM(Bf16, Bf16, false);
+  if (x_f32) return CIS_NORM(F32, F32, true);
+  return stream_f32 ? NormVariant CIS_NORM(Bf16, F32, true) : NormVariant CIS_NORM(Bf16, Bf16, true);
+#undef CIS_NORM
 }
-const void* norm_grad_kernel(bool dy_f32, bool x_f32) {
+template <int LANES, int NV>
+NormVariant grad_variant(bool dy_f32, bool x_f32) {
+#define CIS_NORM(D, X) NormVariant{LANES, (const void*)&cis_norm_grad_row_kernel<D, X, LANES, NV>}
+  if (dy_f32) return x_f32 ? CIS_NORM(F32, F32) : CIS_NORM(F32, Bf16);
+  return x_f32 ? CIS_NORM(Bf16, F32) : CIS_NORM(Bf16, Bf16);
+#undef CIS_NORM
+}
+}  // namespace
+
+// Rows of few elements share a wave; one wave to a row up to 2048 elements, then a workgroup. us for 16384
+// rows of 2048, 64 lanes of 4 groups 47.9, 256 of 1 48.6; for 8192 rows of 8192 with a float32 stream, to
+// e4m3, 256 lanes of 4 groups 129, 512 of 2 130, 1024 of 1 132. In passes they take 125 and 175.
+NormVariant norm_kernel(int32_t H, bool x_f32, bool stream_f32, bool res) {
+  const int n8 = (H + 7) / 8;
+#define CIS_NORM(L, V) return row_variant<L, V>(x_f32, stream_f32, res)
+  if (n8 <= 16) CIS_NORM(16, 1);
+  if (n8 <= 32) CIS_NORM(32, 1);
+  if (n8 <= 64) CIS_NORM(64, 1);
+  if (n8 <= 128) CIS_NORM(64, 2);
+  if (n8 <= 256) CIS_NORM(64, 4);
+  if (n8 <= 512) CIS_NORM(256, 2);
+  if (n8 <= 1024) CIS_NORM(256, 4);
+  if (n8 <= 2048) CIS_NORM(512, 4);
+  if (n8 <= 4096) CIS_NORM(1024, 4);
+#undef CIS_NORM
+  if (!res)
+    return {0, x_f32 ? (const void*)&cis_norm_kernel<F32, F32, false>
+                     : (const void*)&cis_norm_kernel<Bf16, Bf16, false>};
+  if (x_f32) return {0, (const void*)&cis_norm_kernel<F32, F32, true>};
+  return {0, stream_f32 ? (const void*)&cis_norm_kernel<Bf16, F32, true>
+                        : (const void*)&cis_norm_kernel<Bf16, Bf16, true>};
+}
+// More lanes of fewer groups, since each group takes another 70 registers: 16384 rows of 2048, dy in
+// float32, 64 lanes of 4 groups 77.7 us, 256 of 1 61.4.
+NormVariant norm_grad_kernel(int32_t H, bool dy_f32, bool x_f32) {
+  const int n8 = (H + 7) / 8;
+#define CIS_NORM(L, V) return grad_variant<L, V>(dy_f32, x_f32)
+  if (n8 <= 16) CIS_NORM(16, 1);
+  if (n8 <= 32) CIS_NORM(32, 1);
+  if (n8 <= 64) CIS_NORM(64, 1);
+  if (n8 <= 128) CIS_NORM(64, 2);
+  if (n8 <= 256) CIS_NORM(256, 1);
+  if (n8 <= 512) CIS_NORM(512, 1);
+  if (n8 <= 1024) CIS_NORM(512, 2);
+  if (n8 <= 2048) CIS_NORM(1024, 2);
+  static_assert(kNormGradResident == 2048 * 8, "the rows' sums need no room up to here");
+#undef CIS_NORM
   if (dy_f32)
-    return x_f32 ? (const void*)&cis_norm_grad_kernel<F32, F32>
-                 : (const void*)&cis_norm_grad_kernel<F32, Bf16>;
-  return x_f32 ? (const void*)&cis_norm_grad_kernel<Bf16, F32>
-               : (const void*)&cis_norm_grad_kernel<Bf16, Bf16>;
+    return {0, x_f32 ? (const void*)&cis_norm_grad_kernel<F32, F32>
+                     : (const void*)&cis_norm_grad_kernel<F32, Bf16>};
+  return {0, x_f32 ? (const void*)&cis_norm_grad_kernel<Bf16, F32>
+                   : (const void*)&cis_norm_grad_kernel<Bf16, Bf16>};
 }
 const void* norm_rstd_kernel(bool x_f32) {
   return x_f32 ? (const void*)&cis_norm_rstd_kernel<F32> : (const void*)&cis_norm_rstd_kernel<Bf16>;

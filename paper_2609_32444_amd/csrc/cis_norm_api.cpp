@@ -10,8 +10,10 @@ namespace {
 
 using namespace cis::host;
 
-// Rows per launch (HIP refuses 2^32 work items).
-constexpr int64_t kMaxRows = int64_t(1) << 21;
+// Workgroups per launch (HIP refuses 2^32 work items).
+constexpr int64_t kMaxBlocks = int64_t(1) << 21;
+// Parts of dweight's sums: workgroups that take rows in turn.
+constexpr int64_t kGradParts = 1024;
 
 int bytes_of(int dtype) { return dtype == CIS_E4M3 ? 1 : elem_bytes(dtype); }
 
@@ -76,9 +78,7 @@ int check_weight(const void* w, int dtype) {
   return w && !known(dtype) ? CIS_ERR_DTYPE : CIS_OK;
 }
 
-uint32_t grad_parts(int64_t rows) {
-  return (uint32_t)(rows < cis::kNormParts ? rows : cis::kNormParts);
-}
+uint32_t grad_parts(int64_t rows) { return (uint32_t)(rows < kGradParts ? rows : kGradParts); }
 struct GradLayout {
   size_t rstd, part, total;
 };
@@ -86,7 +86,7 @@ GradLayout grad_layout(const Shape& s) {
   GradLayout L{};
   const int64_t rows = s.T * s.N;
   L.rstd = 0;
-  L.part = cis::align_up((size_t)rows * 4, 256);
+  L.part = s.H > cis::kNormGradResident ? cis::align_up((size_t)rows * 4, 256) : 0;
   L.total = L.part + cis::align_up((size_t)grad_parts(rows) * s.H * 4, 256);
   return L;
 }
@@ -155,13 +155,14 @@ int cis_rms_norm_fwd(int64_t T, int64_t N, int64_t H, const cis_rows_t* x,
   a.group = (int32_t)group;
   a.blocks = (int32_t)blocks;
   a.scale = e4m3 ? scale_out : nullptr;
-  const void* fn = cis::norm_kernel(x->dtype == CIS_F32, residual && residual->dtype == CIS_F32,
-                                    residual != nullptr);
-  for (int64_t row0 = 0; row0 < rows; row0 += kMaxRows) {
+  const cis::NormVariant v = cis::norm_kernel((int32_t)H, x->dtype == CIS_F32,
+                                              residual && residual->dtype == CIS_F32,
+                                              residual != nullptr);
+  const int64_t per = cis::norm_block_rows(v.lanes), most = kMaxBlocks * per;
+  for (int64_t row0 = 0; row0 < rows; row0 += most) {
     a.row0 = (uint32_t)row0;
-    if (int rc = launch(fn, rows - row0 < kMaxRows ? rows - row0 : kMaxRows, cis::kNormBlock, &a,
-                        stream))
-      return rc;
+    const int64_t n = rows - row0 < most ? rows - row0 : most;
+    if (int rc = launch(v.fn, (n + per - 1) / per, cis::norm_block(v.lanes), &a, stream)) return rc;
   }
   return CIS_OK;
 }
@@ -228,30 +229,40 @@ int cis_rms_norm_bwd(int64_t T, int64_t N, int64_t H, const cis_rows_t* dy, cons
   a.dx_f32 = dx->dtype == CIS_F32;
   a.dw = dweight;
   const bool df = dy->dtype == CIS_F32, xf = x->dtype == CIS_F32;
+  const GradLayout L = grad_layout(s);
+  if (dweight) {
+    a.rstd = reinterpret_cast<float*>((char*)workspace + L.rstd);
+    a.part = reinterpret_cast<float*>((char*)workspace + L.part);
+  }
+  auto sum_parts = [&] {
+    const int64_t grid = (H + cis::kNormReduceCols - 1) / cis::kNormReduceCols;
+    return launch(cis::norm_reduce_kernel(), grid, cis::kNormReduce, &a, stream);
+  };
+  if (a.rows == 0) return dweight ? sum_parts() : CIS_OK;
+  const cis::NormVariant v = cis::norm_grad_kernel((int32_t)H, df, xf);
+  if (v.lanes) {
+    const int64_t per = cis::norm_block_rows(v.lanes), need = (a.rows + per - 1) / per;
+    a.parts = grad_parts(need);
+    if (int rc = launch(v.fn, a.parts, cis::norm_block(v.lanes), &a, stream)) return rc;
+    return dweight ? sum_parts() : CIS_OK;
+  }
   auto by_rows = [&](const void* fn) {
-    for (int64_t row0 = 0; row0 < (int64_t)a.rows; row0 += kMaxRows) {
+    for (int64_t row0 = 0; row0 < (int64_t)a.rows; row0 += kMaxBlocks) {
       a.row0 = (uint32_t)row0;
-      const int64_t n = a.rows - row0 < kMaxRows ? a.rows - row0 : kMaxRows;
+      const int64_t n = a.rows - row0 < kMaxBlocks ? a.rows - row0 : kMaxBlocks;
       if (int rc = launch(fn, n, cis::kNormBlock, &a, stream)) return rc;
     }
     return (int)CIS_OK;
   };
   if (dweight) {   // ahead of dx, which may replace what it is made from
-    const GradLayout L = grad_layout(s);
-    a.rstd = reinterpret_cast<float*>((char*)workspace + L.rstd);
-    a.part = reinterpret_cast<float*>((char*)workspace + L.part);
     a.parts = grad_parts(a.rows);
-    if (a.rows) {
-      if (int rc = by_rows(cis::norm_rstd_kernel(xf))) return rc;
-      const int64_t cols = (H + 8 * cis::kNormColumns - 1) / (8 * cis::kNormColumns);
-      if (int rc = launch(cis::norm_part_kernel(df, xf), cols * a.parts, cis::kNormColumns, &a,
-                          stream))
-        return rc;
-    }
-    const int64_t grid = (H + cis::kNormReduceCols - 1) / cis::kNormReduceCols;
-    if (int rc = launch(cis::norm_reduce_kernel(), grid, cis::kNormReduce, &a, stream)) return rc;
+    if (int rc = by_rows(cis::norm_rstd_kernel(xf))) return rc;
+    const int64_t cols = (H + 8 * cis::kNormColumns - 1) / (8 * cis::kNormColumns);
+    if (int rc = launch(cis::norm_part_kernel(df, xf), cols * a.parts, cis::kNormColumns, &a, stream))
+      return rc;
+    if (int rc = sum_parts()) return rc;
   }
-  return by_rows(cis::norm_grad_kernel(df, xf));
+  return by_rows(v.fn);
 }
 
 }  // extern "C"
