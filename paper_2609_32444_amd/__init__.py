@@ -68,6 +68,7 @@ from ._tokens import (  # noqa: F401
     top_logits,
     top_logits_workspace_bytes,
 )
+from ._verify import VerifyCall, verify, verify_workspace_bytes  # noqa: F401
 
 __all__ = [
     "CisError", "CIS_BF16", "CIS_F32", "LMHEAD_CHUNK", "LossCall", "NOALLOC_MAX_T", "OP_CIS", "OP_EXACT", "OP_ICEPOP", "OP_KPOP",
@@ -80,5 +81,5 @@ __all__ = [
     "distill_bwd", "distill_fwd", "distill_workspace_bytes", "sample", "sample_workspace_bytes",
     "top_logits", "top_logits_workspace_bytes",
     "NORM_GROUPS", "NORM_MAX_H", "RmsNormCall", "RmsNormGradCall", "rms_norm", "rms_norm_bwd",
-    "rms_norm_workspace_bytes",
+    "rms_norm_workspace_bytes", "VerifyCall", "verify", "verify_workspace_bytes",
 ]

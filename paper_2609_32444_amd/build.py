@@ -16,7 +16,7 @@ LIB_PATH = os.path.join(HERE, "libcis.so")
 SOURCES = [os.path.join(HERE, "csrc", f) for f in
            ("cis_kernels.hip", "cis_kernels_ext.hip", "cis_gemm.hip", "cis_api.cpp",
             "cis_top.hip", "cis_sample.hip", "cis_distill.hip", "cis_tokens_api.cpp",
-            "cis_norm.hip", "cis_norm_api.cpp")]
+            "cis_verify.hip", "cis_norm.hip", "cis_norm_api.cpp")]
 # bandwidth probes for the roofline (a separate library; not part of the loss)
 PROBE_PATH = os.path.join(HERE, "libcis_probe.so")
 PROBE_SOURCES = [os.path.join(HERE, "csrc", "bw_probe.hip")]
@@ -27,7 +27,7 @@ HEADERS = [os.path.join(ROOT, "include", "cis.h"), os.path.join(HERE, "csrc", "c
            os.path.join(ROOT, "include", "cis_tokens.h"), os.path.join(HERE, "csrc", "cis_tok.h"),
            os.path.join(HERE, "csrc", "cis_tok_row.h"),
            os.path.join(HERE, "csrc", "cis_select.h"), os.path.join(HERE, "csrc", "cis_distill.h"),
-           os.path.join(ROOT, "include", "cis_norm.h"), os.path.join(HERE, "csrc", "cis_norm.h"),
+           os.path.join(ROOT, "include", "cis_verify.h"), os.path.join(ROOT, "include", "cis_norm.h"), os.path.join(HERE, "csrc", "cis_norm.h"),
            os.path.join(HERE, "csrc", "cis_host.h")]
 
 # -packed-fp32-ops: no v_pk_{add,mul,fma}_f32 in device code (the compiler's host pass warns

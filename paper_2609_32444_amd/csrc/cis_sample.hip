@@ -26,11 +26,14 @@ struct RowParams {
 };
 __device__ __forceinline__ RowParams row_params(const SampleArgs& a, int64_t row) {
   RowParams p;
-  p.u = sload(a.u + row);
-  p.temp = a.temperature ? sload(a.temperature + row) : a.prm.temperature;
-  const int k = a.top_k ? sload(a.top_k + row) : a.prm.top_k;
-  p.top_p = a.top_p ? sload(a.top_p + row) : a.prm.top_p;
-  p.min_p = a.min_p ? sload(a.min_p + row) : a.prm.min_p;
+  // (verification: a draft's row needs no number, and parameters are the sequences')
+  p.u = row < a.r.T1 ? sload(a.u + row) : 0.f;
+  const bool arrays = a.temperature || a.top_k || a.top_p || a.min_p;
+  const int64_t at = a.r.offsets && arrays ? tok_seq(a.r, row) : row;
+  p.temp = a.temperature ? sload(a.temperature + at) : a.prm.temperature;
+  const int k = a.top_k ? sload(a.top_k + at) : a.prm.top_k;
+  p.top_p = a.top_p ? sload(a.top_p + at) : a.prm.top_p;
+  p.min_p = a.min_p ? sload(a.min_p + at) : a.prm.min_p;
   p.ok = tok_on(a.r, row) && p.u >= 0.f && p.u < 1.f && p.temp >= 0.f && p.temp < INFINITY &&
          k >= 0 && p.top_p > 0.f && p.top_p <= 1.f && p.min_p >= 0.f && p.min_p <= 1.f;
   p.c = kLog2e / p.temp;
@@ -40,6 +43,14 @@ __device__ __forceinline__ RowParams row_params(const SampleArgs& a, int64_t row
   p.counted = greedy || (p.top_k <= kDrawK && (p.top_k < a.r.V || p.top_p < 1.f));
   p.least_w = (uint32_t)ceil((double)p.min_p * kDrawOne);
   return p;
+}
+// The outputs of a row without a token. (Verification: of all rows of the target, until it is done; the
+// drafts' have none.)
+__device__ __forceinline__ void no_row(const SampleArgs& a, int64_t row) {
+  if (row >= a.r.T1) return;
+  a.ids[row] = -1;
+  if (a.logp) a.logp[row] = 0.f;
+  if (a.logp_kept) a.logp_kept[row] = 0.f;
 }
 // Rows that cis_weigh_kernel sums up: those that no count cuts. (The draw adds up the kept part of
 // a step by chunks at WideShared::mass.)
@@ -266,13 +277,20 @@ struct RowDraw {
   int64_t row;
   float rest;   // sum of exp(z - M) over the row but one of its largest logits
   u64 mass0;    // the sum of chunk `lane`, asked for ahead of what comes before its use
+  u64 last_kept;   // verification: the last token that the cuts keep (RowKept::last)
 
   __device__ __forceinline__ uint32_t weight(float f) const { return draw_weight(f, sel.M, p.c); }
 
   __device__ __forceinline__ void put_row(int id, float f, u64 w, u64 N) const {
+    const float logp = (f - sel.M) - log1pf(rest), logp_kept = (float)log((double)w / (double)N);
+    if (a.kept) {
+      a.kept[row] = RowKept{last_kept, N, sel.M, p.c, p.least_w, rest, id, logp, logp_kept};
+      no_row(a, row);
+      return;
+    }
     a.ids[row] = id;
-    if (a.logp) a.logp[row] = (f - sel.M) - log1pf(rest);
-    if (a.logp_kept) a.logp_kept[row] = (float)log((double)w / (double)N);
+    if (a.logp) a.logp[row] = logp;
+    if (a.logp_kept) a.logp_kept[row] = logp_kept;
   }
 
   // f(logits of vector v, v) for a thread's vectors of chunk ch, which follow each other.
@@ -376,6 +394,7 @@ struct RowDraw {
     const int np = (int)(uint32_t)keep, nm = (int)(keep >> 32);
     n = n < np ? n : np;
     n = n < nm ? n : nm;
+    last_kept = sh.list[n - 1];   // (the list changes after the next barrier)
     s = 0;
     static_for<PT>([&](auto J) {
       if (tid * PT + J >= n) q[J] = 0;
@@ -493,6 +512,51 @@ struct RowDraw {
       in_chunk<true>(above, cut, wt);
     else
       in_chunk<false>(above, cut, 0);
+  }
+
+  // The last token that a cut keeps, from the counts of its key's tokens by chunks.
+  __device__ __forceinline__ u64 last_of(const Cut& cut, const uint32_t* ties) {
+    const int tid = threadIdx.x, lane = tid & 63;
+    if (cut.key == kNoToken) return 0;
+    if (cut.ties == 0) return ((u64)cut.key + 1) << 32;
+    __syncthreads();
+    if (tid < 64) {
+      u64 before = 0;
+      int ch = sel.nch;
+      for (int i0 = 0; i0 < sel.nch; i0 += 64) {
+        const u64 n = i0 + lane < sel.nch ? ties[i0 + lane] : 0, upto = before + wave_scan(n, lane);
+        const u64 hit = __ballot(upto >= cut.ties);
+        if (hit) {
+          const int who = __ffsll(hit) - 1;
+          ch = i0 + who;
+          before = __shfl(upto - n, who, 64);
+          break;
+        }
+        before = __shfl(upto, 63, 64);
+      }
+      if (lane == 0) {
+        sh.u[0] = (u64)ch;
+        sh.u[1] = before;
+      }
+    }
+    __syncthreads();
+    const int ch = (int)sh.u[0];
+    u64 before = sh.u[1], n = 0;
+    if (ch >= sel.nch) return (u64)cut.key << 32;   // every one of them
+    each_in_chunk(ch, [&](const float (&f)[EPV], int) {
+#pragma unroll
+      for (int e = 0; e < EPV; ++e) n += order_key(f[e]) == cut.key ? 1 : 0;
+    });
+    __syncthreads();
+    before += ahead(n, sh.u);
+    if (before < cut.ties && cut.ties <= before + n)
+      each_in_chunk(ch, [&](const float (&f)[EPV], int v) {
+#pragma unroll
+        for (int e = 0; e < EPV; ++e)
+          if (order_key(f[e]) == cut.key && ++before == cut.ties) sh.bin = (uint32_t)(v * EPV + e);
+      });
+    __syncthreads();
+    return ((u64)cut.key << 32) | (uint32_t)~sh.bin;
   }
 
   // What the first wave found: the chunk, the sum ahead of it, the draw, the whole sum, and the ties
@@ -795,6 +859,7 @@ struct RowDraw {
           t = 0;
         });
     __syncthreads();
+    if (a.kept) last_kept = last_of(cut, ties);
     from_chunks(cut, ties, p.least_w);
   }
 
@@ -836,6 +901,7 @@ struct RowDraw {
     __syncthreads();
     keep = block_sum<NW>(keep, sh.u);
     const u64 last = keep > 0 ? sh.list[keep - 1] : ~u64(0);
+    last_kept = keep > 0 ? last : sh.list[0] + 1;
     __syncthreads();
     if (tid < 64) {
       Place at{0, 0, 0, 0, 0};
@@ -932,13 +998,12 @@ __global__ __launch_bounds__(BLOCK) __attribute__((amdgpu_waves_per_eu(4))) void
   RowSelect<E, BLOCK, LIST> sel(sh, a.r, a.s, row, p.ok, p.counted);
   if (!p.ok || !sel.tokens()) {
     if (threadIdx.x == 0) {
-      a.ids[row] = -1;
-      if (a.logp) a.logp[row] = 0.f;
-      if (a.logp_kept) a.logp_kept[row] = 0.f;
+      if (a.kept) a.kept[row].id = -1;
+      no_row(a, row);
     }
     return;
   }
-  RowDraw<E, BLOCK, LIST, WIDE> draw{a, p, sel, sh, row, 0.f, mass0};
+  RowDraw<E, BLOCK, LIST, WIDE> draw{a, p, sel, sh, row, 0.f, mass0, 0};
   if constexpr (WIDE)
     draw.run(&ws);
   else

@@ -2,7 +2,7 @@
 // what their kernels share.
 #pragma once
 
-#include "../../include/cis_tokens.h"
+#include "../../include/cis_verify.h"
 #include "cis_internal.h"
 
 namespace cis {
@@ -14,6 +14,12 @@ struct TokRows {
   const uint8_t* mask;   // nullable
   int64_t T;
   int32_t V, nvec;       // nvec = ceil(V / elements per 16-byte vector)
+  // verification: rows [0, T1) are the target's, those behind them the drafts' (else T1 = T)
+  int64_t T1;
+  const void* draft;
+  int64_t draft_bytes;
+  const int64_t* offsets;   // nullable (no verification); the sequences' first rows, and the last one's end
+  int64_t n_seq;
 };
 
 // Weights of a draw are whole multiples of 1 / kDrawOne of the row's largest. 8 weights of a vector
@@ -76,6 +82,17 @@ constexpr int kFineSteps = 29 * kFine;     // (a weight's exponent is at least -
 constexpr int kHistBlock = 1024;
 constexpr int kStepTokens = 8192;          // tokens of its step that a row's list holds
 
+// What verification keeps of a row's draw: the tokens of its distribution are those from `last` on (in the
+// order of token_of()) with weights of least_w at least, relative to M and c, and N is their sum.
+struct RowKept {
+  unsigned long long last, N;
+  float M, c;
+  uint32_t least_w;
+  float rest;            // sum of exp(z - M) over the row but one of its largest logits
+  int32_t id;            // drawn with the row's own random number; -1: the row cannot be drawn from
+  float logp, logp_kept;
+};
+
 struct SampleArgs {
   TokRows r;
   TokScan s;                  // of the rows at temperature 1
@@ -94,6 +111,29 @@ struct SampleArgs {
   const float* top_p;
   const float* min_p;
   int64_t* ids;
+  float* logp;                // nullable
+  float* logp_kept;           // nullable
+  RowKept* kept;              // verification: [T]; else null
+};
+
+// Where a sequence's token is drawn in place of a draft.
+struct VerifyStop {
+  int64_t row;                // -1: nothing is left to draw
+  int32_t draft;              // the token that was turned down
+};
+struct VerifyArgs {
+  TokRows r;
+  const float* cmax;          // [T, nch] of the scan
+  int32_t nch, parts;         // parts: workgroups of a sequence in cis_verify_kernel
+  const RowKept* kept;        // [T]
+  const int64_t* draft_ids;
+  int64_t D;
+  const float* u;
+  int64_t seq0;               // the launch's first sequence
+  VerifyStop* stops;          // [n_seq]
+  unsigned long long* left;   // [n_seq, nch] the chunks' weights of the draw
+  int64_t* ids;
+  int32_t* accepted;
   float* logp;                // nullable
   float* logp_kept;           // nullable
 };
@@ -155,6 +195,9 @@ const void* sample_kernel(int dtype, bool wide);
 const void* weigh_kernel(int dtype, bool step);
 const void* hist_kernel(int dtype);
 const void* step_kernel();
+constexpr int kVerifyBlock = 256;
+const void* verify_kernel(int dtype);
+const void* verify_draw_kernel(int dtype);
 const void* top_kernel(int dtype, int64_t K);
 int top_block(int64_t K);
 constexpr int kDistillGradBlock = 128, kDistillGradVecs = 1024;   // 16 KiB of logits per workgroup

@@ -30,10 +30,30 @@ __device__ __forceinline__ uint32_t draw_weight(float f, float M, float c) {
 
 // A row's descriptor, or one of no records.
 __device__ __forceinline__ __amdgpu_buffer_rsrc_t tok_rsrc(const TokRows& r, int64_t row) {
-  return make_rsrc((const char*)r.logits + row * r.row_bytes, (uint32_t)r.nvec * 16u);
+  const char* p = row < r.T1 ? (const char*)r.logits + row * r.row_bytes
+                             : (const char*)r.draft + (row - r.T1) * r.draft_bytes;
+  return make_rsrc(p, (uint32_t)r.nvec * 16u);
 }
 __device__ __forceinline__ bool tok_on(const TokRows& r, int64_t row) {
+  if (r.offsets) {   // a sequence's row; of a draft's that it may be one
+    const int64_t end = sload(r.offsets + r.n_seq);
+    return row < r.T1 ? row < end : row - r.T1 < end - 1;
+  }
   return r.mask ? sload_byte(r.mask, row) != 0 : true;
+}
+// The sequence that a row or a draft belongs to, if any does (else one of them).
+__device__ __forceinline__ int64_t tok_seq(const TokRows& r, int64_t row) {
+  const bool draft = row >= r.T1;
+  const int64_t end = sload(r.offsets + r.n_seq), at = draft ? row - r.T1 : row;
+  int64_t lo = 0, hi = r.n_seq - 1;
+  while (lo < hi) {   // the last one that starts at the row or ahead of it
+    const int64_t mid = (lo + hi + 1) / 2, first = sload(r.offsets + mid);
+    if (draft ? first < end && first - mid <= at : first <= at)
+      lo = mid;
+    else
+      hi = mid - 1;
+  }
+  return lo;
 }
 // Vector v of a row; elements past the row's end are -inf.
 template <class E>

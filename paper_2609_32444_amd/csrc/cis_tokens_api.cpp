@@ -1,4 +1,4 @@
-// C-ABI entry points of the token operators (cis_tokens.h): argument checks, launch configuration and
+// C-ABI entry points of the token operators (cis_tokens.h, cis_verify.h): argument checks, launch configuration and
 // launches on the caller's stream. No device memory is allocated and nothing synchronises.
 #include <hip/hip_runtime.h>
 #include <math.h>
@@ -48,7 +48,8 @@ int32_t row_vecs(int64_t V, int dtype) {
 }
 cis::TokRows tok_rows(const void* logits, int dtype, int64_t T, int64_t V, int64_t ld,
                       const uint8_t* mask) {
-  return cis::TokRows{logits, ld * elem_bytes(dtype), mask, T, (int32_t)V, row_vecs(V, dtype)};
+  return cis::TokRows{logits, ld * elem_bytes(dtype), mask, T, (int32_t)V, row_vecs(V, dtype),
+                      T, nullptr, 0, nullptr, 0};
 }
 
 cis::ScanLayout top_layout(int64_t T, int64_t V, int64_t K, int dtype) {
@@ -286,67 +287,54 @@ int run_distill(const DistillCall& c, hipStream_t stream) {
   return launch_finalize(base, L, c.T, c.loss, stream);
 }
 
-}  // namespace
-
-extern "C" {
-
-size_t cis_sample_workspace_bytes(int64_t T, int64_t V, int dtype) {
-  if (T < 0 || V < 1 || V > kMaxV || !known(dtype)) return 0;
+// Rows of logits to draw from, for cis_sample and for verification (`kept`).
+struct DrawCall {
+  cis::TokRows r;
+  int dtype;
+  cis_sample_params_t p;
+  const float *u, *temperature;
+  const int32_t* top_k;
+  const float *top_p, *min_p;
+  int64_t* ids;
+  float *logp, *logp_kept;
+  cis::RowKept* kept;
+};
+size_t draw_bytes(int64_t T, int64_t V, int dtype) {
   // (the shape of the scan goes by the call's parameters: the larger of its two)
   const int32_t nvec = row_vecs(V, dtype);
   const SampleLayout a = sample_layout(T, V, nvec, elem_bytes(dtype), 1),
                      b = sample_layout(T, V, nvec, elem_bytes(dtype), 8);
-  const size_t n = a.total > b.total ? a.total : b.total;
-  return n < 256 ? 256 : n;
+  return a.total > b.total ? a.total : b.total;
 }
-
-size_t cis_top_logits_workspace_bytes(int64_t T, int64_t V, int64_t K, int dtype) {
-  if (T < 0 || V < 1 || V > kMaxV || K < 1 || K > CIS_TOP_MAX_K || !known(dtype)) return 0;
-  const size_t n = top_layout(T, V, K, dtype).total;
-  return n < 256 ? 256 : n;
+bool sample_params_ok(const cis_sample_params_t& p, const float* temperature, const int32_t* top_k,
+                      const float* top_p, const float* min_p) {
+  if (!temperature && !(p.temperature >= 0.f && isfinite(p.temperature))) return false;
+  if (!top_k && p.top_k < 0) return false;
+  if (!top_p && !(p.top_p > 0.f && p.top_p <= 1.f)) return false;
+  return min_p || (p.min_p >= 0.f && p.min_p <= 1.f);
 }
-
-size_t cis_distill_workspace_bytes(int64_t T, int64_t V, int64_t K, int dtype) {
-  if (T < 0 || V < 1 || V > kMaxV || K < 1 || K > CIS_TOP_MAX_K || !known(dtype)) return 0;
-  return distill_layout(T, V, K, dtype).total;
-}
-
-int cis_sample(const void* logits, int dtype, int64_t T, int64_t V, int64_t ld, const float* u,
-               const uint8_t* mask, const cis_sample_params_t* params, const float* temperature,
-               const int32_t* top_k, const float* top_p, const float* min_p, int64_t* ids_out,
-               float* logp_out, float* logp_kept_out, void* workspace, size_t workspace_bytes,
-               hipStream_t stream) {
-  if (!params) return CIS_ERR_NULL;
-  if (int rc = check_shape(dtype, T, V, ld)) return rc;
-  const cis_sample_params_t& p = *params;
-  if (!temperature && !(p.temperature >= 0.f && isfinite(p.temperature))) return CIS_ERR_PARAM;
-  if (!top_k && p.top_k < 0) return CIS_ERR_PARAM;
-  if (!top_p && !(p.top_p > 0.f && p.top_p <= 1.f)) return CIS_ERR_PARAM;
-  if (!min_p && !(p.min_p >= 0.f && p.min_p <= 1.f)) return CIS_ERR_PARAM;
-  if (!workspace) return CIS_ERR_NULL;
-  if (T > 0 && (!logits || !u || !ids_out)) return CIS_ERR_NULL;
-  if (int rc = check_workspace(workspace, workspace_bytes, cis_sample_workspace_bytes(T, V, dtype)))
-    return rc;
-  if (T > 0 && !aligned_rows(logits, dtype, ld)) return CIS_ERR_ALIGN;
-  if (const int cus = device_cus(); cus < 0) return cus;
-  if (T == 0) return CIS_OK;
+// cmax: where to leave the chunks' largest logits.
+int run_draws(const DrawCall& c, char* base, hipStream_t stream, const float** cmax = nullptr) {
+  const cis_sample_params_t& p = c.p;
+  const cis::TokRows& r = c.r;
+  const int64_t T = r.T, V = r.V;
   // What the call's rows can ask for. A row whose list is short takes a small workgroup; rows that no
   // count cuts need their weights summed up.
-  const bool greedy = !temperature && !(cis::scan_c(p.temperature) < INFINITY);
+  const bool greedy = !c.temperature && !(cis::scan_c(p.temperature) < INFINITY);
   const int64_t k = greedy ? 1 : p.top_k == 0 || p.top_k >= V ? V : p.top_k;
-  const bool counted = greedy || (!top_k && k <= cis::kDrawListK && k < V);   // every row
-  const bool uncut = !counted && !top_k && k == V && !top_p && p.top_p == 1.f;
+  const bool counted = greedy || (!c.top_k && k <= cis::kDrawListK && k < V);   // every row
+  const bool uncut = !counted && !c.top_k && k == V && !c.top_p && p.top_p == 1.f;
   const bool wide = !counted && !uncut;
-  const bool weighed = !counted && (top_k || k == V);
-  const bool stepped = weighed && (top_p || p.top_p < 1.f);
+  const bool weighed = !counted && (c.top_k || k == V);
+  const bool stepped = weighed && (c.top_p || p.top_p < 1.f);
   // lists start from the groups; nothing else does (512 uncut rows: the scan 28 us, 24 without)
-  const bool lists = counted || top_k || temperature || k <= cis::kDrawK;
-  const cis::TokRows r = tok_rows(logits, dtype, T, V, ld, mask);
-  char* base = static_cast<char*>(workspace);
+  const bool lists = counted || c.top_k || c.temperature || k <= cis::kDrawK;
+  const int dtype = c.dtype;
   const SampleLayout L = sample_layout(T, V, r.nvec, elem_bytes(dtype),
                                        lists ? cis::scan_group(r.nvec, counted ? k : kManyLogits)
                                              : 0);
   const cis::TokScan s = scan_at(base, L.scan);
+  if (cmax) *cmax = s.cmax;
   if (int rc = launch_scan(r, s, dtype, cis::scan_c(1.f), stream)) return rc;
   cis::SampleArgs a{};
   a.r = r;
@@ -358,15 +346,16 @@ int cis_sample(const void* logits, int dtype, int64_t T, int64_t V, int64_t ld, 
   a.hist = reinterpret_cast<unsigned long long*>(base + L.hist);
   a.step_ld = L.step_ld;
   a.parts = L.parts;
-  a.u = u;
+  a.u = c.u;
   a.prm = p;
-  a.temperature = temperature;
-  a.top_k = top_k;
-  a.top_p = top_p;
-  a.min_p = min_p;
-  a.ids = ids_out;
-  a.logp = logp_out;
-  a.logp_kept = logp_kept_out;
+  a.temperature = c.temperature;
+  a.top_k = c.top_k;
+  a.top_p = c.top_p;
+  a.min_p = c.min_p;
+  a.ids = c.ids;
+  a.logp = c.logp;
+  a.logp_kept = c.logp_kept;
+  a.kept = c.kept;
   const int block = wide ? cis::kTokBlock : cis::kTopBlock;
   const int64_t most = stepped ? kStepRows : kMaxRows;
   for (; a.row0 < T; a.row0 += most) {
@@ -389,6 +378,76 @@ int cis_sample(const void* logits, int dtype, int64_t T, int64_t V, int64_t ld, 
     if (int rc = launch(cis::sample_kernel(dtype, wide), a.rows, block, &a, stream)) return rc;
   }
   return CIS_OK;
+}
+
+// Target rows and drafts of a verification together, and its sequences.
+constexpr int64_t kMaxVerify = int64_t(1) << 31;
+// Workgroups of cis_verify_kernel beyond which a wave takes several chunks.
+constexpr int64_t kVerifyBlocks = 2048;
+struct VerifyLayout {
+  size_t kept, stops, left, total;
+};
+VerifyLayout verify_layout(int64_t T, int64_t D, int64_t n_seq, int64_t V, int dtype) {
+  VerifyLayout L{};
+  const int32_t nch = (row_vecs(V, dtype) + cis::kScanVecs - 1) / cis::kScanVecs;
+  L.kept = cis::align_up(draw_bytes(T + D, V, dtype), 256);
+  L.stops = L.kept + cis::align_up((size_t)(T + D) * sizeof(cis::RowKept), 256);
+  L.left = L.stops + cis::align_up((size_t)n_seq * sizeof(cis::VerifyStop), 256);
+  L.total = L.left + cis::align_up((size_t)n_seq * nch * 8, 256);
+  if (L.total < 256) L.total = 256;
+  return L;
+}
+
+}  // namespace
+
+extern "C" {
+
+size_t cis_sample_workspace_bytes(int64_t T, int64_t V, int dtype) {
+  if (T < 0 || V < 1 || V > kMaxV || !known(dtype)) return 0;
+  const size_t n = draw_bytes(T, V, dtype);
+  return n < 256 ? 256 : n;
+}
+
+size_t cis_top_logits_workspace_bytes(int64_t T, int64_t V, int64_t K, int dtype) {
+  if (T < 0 || V < 1 || V > kMaxV || K < 1 || K > CIS_TOP_MAX_K || !known(dtype)) return 0;
+  const size_t n = top_layout(T, V, K, dtype).total;
+  return n < 256 ? 256 : n;
+}
+
+size_t cis_distill_workspace_bytes(int64_t T, int64_t V, int64_t K, int dtype) {
+  if (T < 0 || V < 1 || V > kMaxV || K < 1 || K > CIS_TOP_MAX_K || !known(dtype)) return 0;
+  return distill_layout(T, V, K, dtype).total;
+}
+
+int cis_sample(const void* logits, int dtype, int64_t T, int64_t V, int64_t ld, const float* u,
+               const uint8_t* mask, const cis_sample_params_t* params, const float* temperature,
+               const int32_t* top_k, const float* top_p, const float* min_p, int64_t* ids_out,
+               float* logp_out, float* logp_kept_out, void* workspace, size_t workspace_bytes,
+               hipStream_t stream) {
+  if (!params) return CIS_ERR_NULL;
+  if (int rc = check_shape(dtype, T, V, ld)) return rc;
+  const cis_sample_params_t& p = *params;
+  if (!sample_params_ok(p, temperature, top_k, top_p, min_p)) return CIS_ERR_PARAM;
+  if (!workspace) return CIS_ERR_NULL;
+  if (T > 0 && (!logits || !u || !ids_out)) return CIS_ERR_NULL;
+  if (int rc = check_workspace(workspace, workspace_bytes, cis_sample_workspace_bytes(T, V, dtype)))
+    return rc;
+  if (T > 0 && !aligned_rows(logits, dtype, ld)) return CIS_ERR_ALIGN;
+  if (const int cus = device_cus(); cus < 0) return cus;
+  if (T == 0) return CIS_OK;
+  DrawCall c{};
+  c.r = tok_rows(logits, dtype, T, V, ld, mask);
+  c.dtype = dtype;
+  c.p = p;
+  c.u = u;
+  c.temperature = temperature;
+  c.top_k = top_k;
+  c.top_p = top_p;
+  c.min_p = min_p;
+  c.ids = ids_out;
+  c.logp = logp_out;
+  c.logp_kept = logp_kept_out;
+  return run_draws(c, static_cast<char*>(workspace), stream);
 }
 
 int cis_top_logits(const void* logits, int dtype, int64_t T, int64_t V, int64_t ld,
@@ -440,6 +499,89 @@ int cis_distill_bwd(const void* logits, int dtype, int64_t T, int64_t V, int64_t
                                  row_weight, mask, params, true, dlogits, ld_g, terms_out, loss_out,
                                  workspace, workspace_bytes},
                      stream);
+}
+
+size_t cis_verify_workspace_bytes(int64_t T, int64_t D, int64_t n_seq, int64_t V, int dtype) {
+  if (T < 0 || D < 0 || n_seq < 0 || T > kMaxVerify || D > kMaxVerify - T || n_seq > kMaxVerify ||
+      V < 1 || V > kMaxV || !known(dtype))
+    return 0;
+  return verify_layout(T, D, n_seq, V, dtype).total;
+}
+
+int cis_verify(const void* logits, int dtype, int64_t T, int64_t V, int64_t ld,
+               const void* draft_logits, int64_t D, int64_t ld_d, const int64_t* draft_ids,
+               const float* u, const int64_t* seq_offsets, int64_t n_seq,
+               const cis_sample_params_t* params, const float* temperature, const int32_t* top_k,
+               const float* top_p, const float* min_p, int64_t* ids_out, int32_t* accepted_out,
+               float* logp_out, float* logp_kept_out, void* workspace, size_t workspace_bytes,
+               hipStream_t stream) {
+  if (!params) return CIS_ERR_NULL;
+  if (int rc = check_shape(dtype, T, V, ld)) return rc;
+  if (D < 0 || n_seq < 0 || T > kMaxVerify || D > kMaxVerify - T || n_seq > kMaxVerify)
+    return CIS_ERR_SHAPE;
+  if (T > 0 && n_seq < 1) return CIS_ERR_SHAPE;
+  if (draft_logits)
+    if (int rc = check_shape(dtype, D, V, ld_d)) return rc;
+  if (!sample_params_ok(*params, temperature, top_k, top_p, min_p)) return CIS_ERR_PARAM;
+  if (!workspace) return CIS_ERR_NULL;
+  if (T > 0 && (!logits || !u || !ids_out)) return CIS_ERR_NULL;
+  if (n_seq > 0 && (!seq_offsets || !accepted_out)) return CIS_ERR_NULL;
+  if (D > 0 && !draft_ids) return CIS_ERR_NULL;
+  const int64_t Dl = draft_logits ? D : 0;   // rows of them
+  if (int rc = check_workspace(workspace, workspace_bytes,
+                               cis_verify_workspace_bytes(T, Dl, n_seq, V, dtype)))
+    return rc;
+  if (T > 0 && !aligned_rows(logits, dtype, ld)) return CIS_ERR_ALIGN;
+  if (Dl > 0 && !aligned_rows(draft_logits, dtype, ld_d)) return CIS_ERR_ALIGN;
+  if (const int cus = device_cus(); cus < 0) return cus;
+  if (n_seq == 0) return CIS_OK;
+
+  char* base = static_cast<char*>(workspace);
+  const VerifyLayout L = verify_layout(T, Dl, n_seq, V, dtype);
+  DrawCall c{};
+  c.r = tok_rows(logits, dtype, T, V, ld, nullptr);
+  c.r.T = T + Dl;
+  c.r.draft = draft_logits;
+  c.r.draft_bytes = draft_logits ? ld_d * elem_bytes(dtype) : 0;
+  c.r.offsets = seq_offsets;
+  c.r.n_seq = n_seq;
+  c.dtype = dtype;
+  c.p = *params;
+  c.u = u;
+  c.temperature = temperature;
+  c.top_k = top_k;
+  c.top_p = top_p;
+  c.min_p = min_p;
+  c.ids = ids_out;
+  c.logp = logp_out;
+  c.logp_kept = logp_kept_out;
+  c.kept = reinterpret_cast<cis::RowKept*>(base + L.kept);
+  cis::VerifyArgs a{};
+  if (c.r.T > 0)
+    if (int rc = run_draws(c, base, stream, &a.cmax)) return rc;
+  a.r = c.r;
+  a.nch = (c.r.nvec + cis::kScanVecs - 1) / cis::kScanVecs;
+  a.kept = c.kept;
+  a.draft_ids = draft_ids;
+  a.D = D;
+  a.u = u;
+  a.stops = reinterpret_cast<cis::VerifyStop*>(base + L.stops);
+  a.left = reinterpret_cast<unsigned long long*>(base + L.left);
+  a.ids = ids_out;
+  a.accepted = accepted_out;
+  a.logp = logp_out;
+  a.logp_kept = logp_kept_out;
+  const int64_t per = cis::kVerifyBlock / 64, most = (a.nch + per - 1) / per,
+                fill = (kVerifyBlocks + n_seq - 1) / n_seq;
+  a.parts = (int32_t)(fill < most ? fill : most);
+  const int64_t step = kMaxBlocks / a.parts > 0 ? kMaxBlocks / a.parts : 1;
+  for (; a.seq0 < n_seq; a.seq0 += step) {
+    const int64_t n = n_seq - a.seq0 < step ? n_seq - a.seq0 : step;
+    if (int rc = launch(cis::verify_kernel(dtype), n * a.parts, cis::kVerifyBlock, &a, stream))
+      return rc;
+    if (int rc = launch(cis::verify_draw_kernel(dtype), n, cis::kVerifyBlock, &a, stream)) return rc;
+  }
+  return CIS_OK;
 }
 
 }  // extern "C"
