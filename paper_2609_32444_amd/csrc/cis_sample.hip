@@ -1,7 +1,8 @@
 // Sampling kernels (gfx950).
 //
-// A row is drawn from the scan (TokScan) in one of four ways, by what its cuts keep at most:
-//   * top_k up to kDrawK (and greedy rows): the candidates that RowSelect collects, put in order; the
+// A row is drawn from the scan (TokScan) in one of five ways, by what its cuts keep at most:
+//   * greedy rows, and top_k = 1: the first of the largest logits.
+//   * top_k up to kDrawK: the candidates that RowSelect collects, put in order; the
 //     cuts and the draw run on that list.
 //   * nothing but min_p cuts: the weights' sums by chunks (cis_weigh_kernel), the chunk that the
 //     random number falls into, and the token within it.
@@ -24,17 +25,22 @@ struct RowParams {
   bool counted;    // top_k (V: all of a short row) leaves few enough for a list
   uint32_t least_w;
 };
+// KEEP: for verification, where a draft's row needs no number, and parameters are the sequences'.
+template <bool KEEP>
 __device__ __forceinline__ RowParams row_params(const SampleArgs& a, int64_t row) {
   RowParams p;
-  // (verification: a draft's row needs no number, and parameters are the sequences')
-  p.u = row < a.r.T1 ? sload(a.u + row) : 0.f;
-  const bool arrays = a.temperature || a.top_k || a.top_p || a.min_p;
-  const int64_t at = a.r.offsets && arrays ? tok_seq(a.r, row) : row;
+  int64_t at = row;
+  if constexpr (KEEP) {
+    p.u = row < a.r.T1 ? sload(a.u + row) : 0.f;
+    if (a.temperature || a.top_k || a.top_p || a.min_p) at = tok_seq(a.r, row);
+  } else {
+    p.u = sload(a.u + row);
+  }
   p.temp = a.temperature ? sload(a.temperature + at) : a.prm.temperature;
   const int k = a.top_k ? sload(a.top_k + at) : a.prm.top_k;
   p.top_p = a.top_p ? sload(a.top_p + at) : a.prm.top_p;
   p.min_p = a.min_p ? sload(a.min_p + at) : a.prm.min_p;
-  p.ok = tok_on(a.r, row) && p.u >= 0.f && p.u < 1.f && p.temp >= 0.f && p.temp < INFINITY &&
+  p.ok = (KEEP ? tok_seq_on(a.r, row) : tok_on(a.r, row)) && p.u >= 0.f && p.u < 1.f && p.temp >= 0.f && p.temp < INFINITY &&
          k >= 0 && p.top_p > 0.f && p.top_p <= 1.f && p.min_p >= 0.f && p.min_p <= 1.f;
   p.c = kLog2e / p.temp;
   const bool greedy = !(p.c < INFINITY);
@@ -44,10 +50,8 @@ __device__ __forceinline__ RowParams row_params(const SampleArgs& a, int64_t row
   p.least_w = (uint32_t)ceil((double)p.min_p * kDrawOne);
   return p;
 }
-// The outputs of a row without a token. (Verification: of all rows of the target, until it is done; the
-// drafts' have none.)
+// The outputs of a row without a token. (Verification: of all rows of the target, until it is done.)
 __device__ __forceinline__ void no_row(const SampleArgs& a, int64_t row) {
-  if (row >= a.r.T1) return;
   a.ids[row] = -1;
   if (a.logp) a.logp[row] = 0.f;
   if (a.logp_kept) a.logp_kept[row] = 0.f;
@@ -108,7 +112,7 @@ __device__ __forceinline__ DrawStep step_of_cut(const u64* mass, float top_p, in
 // times as long as the others) and the atomics: 256 rows of V = 262144 in 30 us, 37 with every
 // token in LDS.
 // ------------------------------------------------------------------------------------------
-template <class E>
+template <class E, bool KEEP>
 __global__ __launch_bounds__(kHistBlock) void cis_hist_kernel(const SampleArgs a) {
   constexpr int NW = kHistBlock / 64, EPV = E::kPerVec;
   __shared__ u64 mass[kFineSteps];
@@ -116,7 +120,7 @@ __global__ __launch_bounds__(kHistBlock) void cis_hist_kernel(const SampleArgs a
             wid = __builtin_amdgcn_readfirstlane(threadIdx.x) >> 6;
   const int64_t at = blockIdx.x / a.parts, row = a.row0 + at;
   const int part = (int)(blockIdx.x - at * a.parts), nch = a.s.nch;
-  const RowParams p = row_params(a, row);
+  const RowParams p = row_params<KEEP>(a, row);
   if (!row_stepped(p, a)) return;
   for (int i = tid; i < kFineSteps; i += kHistBlock) mass[i] = 0;
   const float* cmax = a.s.cmax + row * nch;
@@ -165,10 +169,11 @@ __global__ __launch_bounds__(kHistBlock) void cis_hist_kernel(const SampleArgs a
 }
 
 // The step of a row's cut from its parts' histograms.
+template <bool KEEP>
 __global__ __launch_bounds__(kHistBlock) void cis_step_kernel(const SampleArgs a) {
   __shared__ u64 mass[kFineSteps];
   const int64_t at = blockIdx.x, row = a.row0 + at;
-  const RowParams p = row_params(a, row);
+  const RowParams p = row_params<KEEP>(a, row);
   if (!row_stepped(p, a)) return;
   const u64* in = a.hist + at * a.parts * kFineSteps;
   for (int i = threadIdx.x; i < kFineSteps; i += kHistBlock) {
@@ -191,14 +196,14 @@ __global__ __launch_bounds__(kHistBlock) void cis_step_kernel(const SampleArgs a
 // instructions a logit (24 us) and the second read of the row: 512 rows of V = 151936 in 32 us; with
 // STEP 256 rows of V = 262144, half of them peaked, in 21.
 // ------------------------------------------------------------------------------------------
-template <class E, bool STEP>
+template <class E, bool STEP, bool KEEP>
 __global__ __launch_bounds__(kWeighBlock) void cis_weigh_kernel(const SampleArgs a) {
   constexpr int NW = kWeighBlock / 64, EPV = E::kPerVec;
   const int wid = __builtin_amdgcn_readfirstlane(threadIdx.x) >> 6, nch = a.s.nch;
   const uint32_t at = blockIdx.x / (uint32_t)a.weigh_parts;
   const int part = (int)(blockIdx.x - at * (uint32_t)a.weigh_parts);
   const int64_t row = a.row0 + at;
-  const RowParams p = row_params(a, row);
+  const RowParams p = row_params<KEEP>(a, row);
   if (!row_weighed(p, a)) return;
   const float* cmax = a.s.cmax + row * nch;
   const float M = row_max(cmax, nch, threadIdx.x & 63);
@@ -218,6 +223,8 @@ __global__ __launch_bounds__(kWeighBlock) void cis_weigh_kernel(const SampleArgs
       constexpr int kBits = 4 * EPV;
       static_assert(kScanSlots == 8, "two words");
       uint32_t in[2] = {0, 0};
+      // (without a min_p two instructions a logit less; with STEP that does not pay)
+      auto add_up = [&](auto min_p) __attribute__((always_inline)) {
       static_for<kScanSlots>([&](auto I) {
         float f[EPV];
         E::unpack(x[I], f);
@@ -227,12 +234,17 @@ __global__ __launch_bounds__(kWeighBlock) void cis_weigh_kernel(const SampleArgs
           const float t = draw_exponent(f[e], M, p.c);
           const uint32_t q = exponent_weight(t);
           if (STEP) in[I / 4] = in[I / 4] * 2 + (t > within && t <= above ? 1 : 0);
-          vs += (!STEP || t > above) && q >= p.least_w ? q : 0u;
+          vs += (!STEP || t > above) && (!min_p || q >= p.least_w) ? q : 0u;
         }
         s += vs;
         if (STEP) asm volatile("" : "+v"(in[I / 4]));   // (else all vectors are unpacked first)
         slot_fence();
       });
+      };
+      if (STEP || p.least_w > 0)
+        add_up(std::true_type{});
+      else
+        add_up(std::false_type{});
       s = wave_sum(s);
       if (STEP && step < kFineSteps && __ballot((in[0] | in[1]) != 0)) {
         const uint32_t mine = __popc(in[0]) + __popc(in[1]), upto = wave_scan(mine, lane);
@@ -267,7 +279,7 @@ struct WideShared {
   u64 left;
 };
 
-template <class E, int BLOCK, int LIST, bool WIDE>
+template <class E, int BLOCK, int LIST, bool WIDE, bool KEEP>
 struct RowDraw {
   static constexpr int NW = BLOCK / 64, EPV = E::kPerVec;
   const SampleArgs& a;
@@ -277,20 +289,21 @@ struct RowDraw {
   int64_t row;
   float rest;   // sum of exp(z - M) over the row but one of its largest logits
   u64 mass0;    // the sum of chunk `lane`, asked for ahead of what comes before its use
+  int largest;     // the lowest id of the largest logits that the thread has seen in their first chunk
   u64 last_kept;   // verification: the last token that the cuts keep (RowKept::last)
 
   __device__ __forceinline__ uint32_t weight(float f) const { return draw_weight(f, sel.M, p.c); }
 
   __device__ __forceinline__ void put_row(int id, float f, u64 w, u64 N) const {
     const float logp = (f - sel.M) - log1pf(rest), logp_kept = (float)log((double)w / (double)N);
-    if (a.kept) {
+    if constexpr (KEEP) {
       a.kept[row] = RowKept{last_kept, N, sel.M, p.c, p.least_w, rest, id, logp, logp_kept};
-      no_row(a, row);
-      return;
+      if (row < a.r.T1) no_row(a, row);
+    } else {
+      a.ids[row] = id;
+      if (a.logp) a.logp[row] = logp;
+      if (a.logp_kept) a.logp_kept[row] = logp_kept;
     }
-    a.ids[row] = id;
-    if (a.logp) a.logp[row] = logp;
-    if (a.logp_kept) a.logp_kept[row] = logp_kept;
   }
 
   // f(logits of vector v, v) for a thread's vectors of chunk ch, which follow each other.
@@ -337,8 +350,14 @@ struct RowDraw {
       if (i != first) s += sum * (double)fast_exp2((m - sel.M) * kLog2e);
     });
     u64 n = 0;   // largest ones in the chunk (counted apart: 1 would swallow what is far smaller)
-    each_in_chunk(first, [&](const float (&f)[EPV], int) {
+    largest = INT32_MAX;
+    each_in_chunk(first, [&](const float (&f)[EPV], int v) {
       float t = 0.f;
+      if (p.top_k == 1) {
+#pragma unroll
+        for (int e = EPV - 1; e >= 0; --e)
+          if (f[e] == sel.M && v * EPV + e < largest) largest = v * EPV + e;
+      }
 #pragma unroll
       for (int e = 0; e < EPV; ++e) {
         t += f[e] == sel.M ? 0.f : fast_exp2((f[e] - sel.M) * kLog2e);
@@ -350,6 +369,23 @@ struct RowDraw {
     n = block_sum<NW>(n, sh.u);
     if (tid == 0) s += (double)(n - 1);
     rest = (float)block_sum<NW>(s, sh.d);
+  }
+
+  // Takes the first of the row's largest logits.
+  __device__ __forceinline__ void from_largest() {
+    int id = largest;
+#pragma unroll
+    for (int off = 32; off >= 1; off >>= 1) {
+      const int o = __shfl_xor(id, off, 64);
+      id = id < o ? id : o;
+    }
+    if ((threadIdx.x & 63) == 0) sh.u[threadIdx.x >> 6] = (u64)id;
+    __syncthreads();
+    if (threadIdx.x == 0) {
+      for (int w = 1; w < NW; ++w) id = id < (int)sh.u[w] ? id : (int)sh.u[w];
+      last_kept = token_of(sel.M, id);
+      put_row(id, sel.M, kDrawOne, kDrawOne);
+    }
   }
 
   // Draws from the list's first logits in order: at most `n` of them; of those the fewest that
@@ -394,7 +430,7 @@ struct RowDraw {
     const int np = (int)(uint32_t)keep, nm = (int)(keep >> 32);
     n = n < np ? n : np;
     n = n < nm ? n : nm;
-    last_kept = sh.list[n - 1];   // (the list changes after the next barrier)
+    if constexpr (KEEP) last_kept = sh.list[n - 1];   // (the list changes after the next barrier)
     s = 0;
     static_for<PT>([&](auto J) {
       if (tid * PT + J >= n) q[J] = 0;
@@ -859,7 +895,7 @@ struct RowDraw {
           t = 0;
         });
     __syncthreads();
-    if (a.kept) last_kept = last_of(cut, ties);
+    if constexpr (KEEP) last_kept = last_of(cut, ties);
     from_chunks(cut, ties, p.least_w);
   }
 
@@ -938,6 +974,11 @@ struct RowDraw {
     sum_rest();
     const int64_t V = sel.V;
     const int k = (int)p.top_k;
+    if (p.counted && k == 1) {
+      __syncthreads();
+      from_largest();
+      return;
+    }
     if (p.counted) {
       if (sel.collect(k)) {
         sel.order(k);
@@ -985,48 +1026,46 @@ struct RowDraw {
 };
 
 // WIDE: any parameters; else top_k in [1, LIST / 8] for every row, or nothing to cut but min_p.
-template <class E, int BLOCK, int LIST, bool WIDE>
+template <class E, int BLOCK, int LIST, bool WIDE, bool KEEP>
 __global__ __launch_bounds__(BLOCK) __attribute__((amdgpu_waves_per_eu(4))) void cis_sample_kernel(
     const SampleArgs a) {
   __shared__ SelectShared<LIST> sh;
   __shared__ std::conditional_t<WIDE, WideShared, uint32_t> ws;
   const int64_t row = a.row0 + blockIdx.x;
-  const RowParams p = row_params(a, row);
+  const RowParams p = row_params<KEEP>(a, row);
   const int lane = threadIdx.x & 63;
   u64 mass0 = 0;
   if (row_weighed(p, a) && lane < a.s.nch) mass0 = a.draw[row * a.s.nch + lane];
-  RowSelect<E, BLOCK, LIST> sel(sh, a.r, a.s, row, p.ok, p.counted);
+  RowSelect<E, BLOCK, LIST> sel(sh, a.r, a.s, row, p.ok, p.counted && p.top_k > 1);
   if (!p.ok || !sel.tokens()) {
     if (threadIdx.x == 0) {
-      if (a.kept) a.kept[row].id = -1;
-      no_row(a, row);
+      if constexpr (KEEP) a.kept[row].id = -1;
+      if (!KEEP || row < a.r.T1) no_row(a, row);
     }
     return;
   }
-  RowDraw<E, BLOCK, LIST, WIDE> draw{a, p, sel, sh, row, 0.f, mass0, 0};
+  RowDraw<E, BLOCK, LIST, WIDE, KEEP> draw{a, p, sel, sh, row, 0.f, mass0, 0, 0};
   if constexpr (WIDE)
     draw.run(&ws);
   else
     draw.run(nullptr);
 }
 
-const void* weigh_kernel(int dtype, bool step) {
-#define CIS_WEIGH(E) \
-  (step ? (const void*)&cis_weigh_kernel<E, true> : (const void*)&cis_weigh_kernel<E, false>)
-  return dtype == CIS_BF16 ? CIS_WEIGH(Bf16) : CIS_WEIGH(F32);
-#undef CIS_WEIGH
+namespace {
+template <bool KEEP>
+DrawKernels draw_kernels_of(int dtype, bool wide, bool step) {
+#define CIS_DRAW(E)                                                                              \
+  {(const void*)&cis_hist_kernel<E, KEEP>, (const void*)&cis_step_kernel<KEEP>,                  \
+   step ? (const void*)&cis_weigh_kernel<E, true, KEEP> : (const void*)&cis_weigh_kernel<E, false, KEEP>, \
+   wide ? (const void*)&cis_sample_kernel<E, kTokBlock, 8192, true, KEEP>                        \
+        : (const void*)&cis_sample_kernel<E, kTopBlock, 1024, false, KEEP>}
+  if (dtype == CIS_BF16) return CIS_DRAW(Bf16);
+  return CIS_DRAW(F32);
+#undef CIS_DRAW
 }
-const void* hist_kernel(int dtype) {
-  return dtype == CIS_BF16 ? (const void*)&cis_hist_kernel<Bf16>
-                           : (const void*)&cis_hist_kernel<F32>;
-}
-const void* step_kernel() { return (const void*)&cis_step_kernel; }
-const void* sample_kernel(int dtype, bool wide) {
-  if (dtype == CIS_BF16)
-    return wide ? (const void*)&cis_sample_kernel<Bf16, kTokBlock, 8192, true>
-                : (const void*)&cis_sample_kernel<Bf16, kTopBlock, 1024, false>;
-  return wide ? (const void*)&cis_sample_kernel<F32, kTokBlock, 8192, true>
-              : (const void*)&cis_sample_kernel<F32, kTopBlock, 1024, false>;
+}  // namespace
+DrawKernels draw_kernels(int dtype, bool wide, bool step, bool keep) {
+  return keep ? draw_kernels_of<true>(dtype, wide, step) : draw_kernels_of<false>(dtype, wide, step);
 }
 
 }  // namespace cis

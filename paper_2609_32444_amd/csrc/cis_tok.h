@@ -124,14 +124,15 @@ struct VerifyStop {
 struct VerifyArgs {
   TokRows r;
   const float* cmax;          // [T, nch] of the scan
-  int32_t nch, parts;         // parts: workgroups of a sequence in cis_verify_kernel
+  int32_t nch;
+  int32_t nsub, parts;        // pieces of kLeftVecs vectors in a row; workgroups of a sequence
   const RowKept* kept;        // [T]
   const int64_t* draft_ids;
   int64_t D;
   const float* u;
   int64_t seq0;               // the launch's first sequence
   VerifyStop* stops;          // [n_seq]
-  unsigned long long* left;   // [n_seq, nch] the chunks' weights of the draw
+  unsigned long long* left;   // [n_seq, nsub] the pieces' weights of the draw
   int64_t* ids;
   int32_t* accepted;
   float* logp;                // nullable
@@ -190,12 +191,14 @@ constexpr int kDrawK = 1024;      // top_k up to which a row is drawn from a lis
 constexpr int kDrawListK = 128;   // top_k that the kernel for short lists takes
 // keep: the logits stay in the caches for a later kernel's read
 const void* scan_kernel(int dtype, int32_t gv, bool keep);
-// wide: any parameters; else top_k in [1, 128] for every row or nothing to cut but min_p
-const void* sample_kernel(int dtype, bool wide);
-const void* weigh_kernel(int dtype, bool step);
-const void* hist_kernel(int dtype);
-const void* step_kernel();
+// wide: any parameters; else top_k in [1, 128] for every row or nothing to cut but min_p. step: a row may be
+// cut by top_p alone. keep: for verification.
+struct DrawKernels {
+  const void *hist, *step, *weigh, *sample;
+};
+DrawKernels draw_kernels(int dtype, bool wide, bool step, bool keep);
 constexpr int kVerifyBlock = 256;
+constexpr int kLeftVecs = 128;   // vectors of a piece (a wave's)
 const void* verify_kernel(int dtype);
 const void* verify_draw_kernel(int dtype);
 const void* top_kernel(int dtype, int64_t K);

@@ -35,11 +35,12 @@ __device__ __forceinline__ __amdgpu_buffer_rsrc_t tok_rsrc(const TokRows& r, int
   return make_rsrc(p, (uint32_t)r.nvec * 16u);
 }
 __device__ __forceinline__ bool tok_on(const TokRows& r, int64_t row) {
-  if (r.offsets) {   // a sequence's row; of a draft's that it may be one
-    const int64_t end = sload(r.offsets + r.n_seq);
-    return row < r.T1 ? row < end : row - r.T1 < end - 1;
-  }
   return r.mask ? sload_byte(r.mask, row) != 0 : true;
+}
+// Verification: whether a row is a sequence's, a draft may be one.
+__device__ __forceinline__ bool tok_seq_on(const TokRows& r, int64_t row) {
+  const int64_t end = sload(r.offsets + r.n_seq);
+  return row < r.T1 ? row < end : row - r.T1 < end - 1;
 }
 // The sequence that a row or a draft belongs to, if any does (else one of them).
 __device__ __forceinline__ int64_t tok_seq(const TokRows& r, int64_t row) {

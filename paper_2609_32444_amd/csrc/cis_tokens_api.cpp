@@ -327,8 +327,9 @@ int run_draws(const DrawCall& c, char* base, hipStream_t stream, const float** c
   const bool wide = !counted && !uncut;
   const bool weighed = !counted && (c.top_k || k == V);
   const bool stepped = weighed && (c.top_p || p.top_p < 1.f);
-  // lists start from the groups; nothing else does (512 uncut rows: the scan 28 us, 24 without)
-  const bool lists = counted || c.top_k || c.temperature || k <= cis::kDrawK;
+  // lists start from the groups; nothing else does (512 uncut rows: the scan 28 us, 24 without), nor
+  // where the largest logit is all that is asked for
+  const bool lists = c.top_k || c.temperature ? true : k > 1 && (counted || k <= cis::kDrawK);
   const int dtype = c.dtype;
   const SampleLayout L = sample_layout(T, V, r.nvec, elem_bytes(dtype),
                                        lists ? cis::scan_group(r.nvec, counted ? k : kManyLogits)
@@ -356,44 +357,44 @@ int run_draws(const DrawCall& c, char* base, hipStream_t stream, const float** c
   a.logp = c.logp;
   a.logp_kept = c.logp_kept;
   a.kept = c.kept;
+  const cis::DrawKernels fn = cis::draw_kernels(dtype, wide, stepped, c.kept != nullptr);
   const int block = wide ? cis::kTokBlock : cis::kTopBlock;
   const int64_t most = stepped ? kStepRows : kMaxRows;
   for (; a.row0 < T; a.row0 += most) {
     a.rows = T - a.row0 < most ? T - a.row0 : most;
     if (stepped) {
-      if (int rc = launch(cis::hist_kernel(dtype), a.rows * L.parts, cis::kHistBlock, &a, stream))
+      if (int rc = launch(fn.hist, a.rows * L.parts, cis::kHistBlock, &a, stream))
         return rc;
       if (L.parts > 1)
-        if (int rc = launch(cis::step_kernel(), a.rows, cis::kHistBlock, &a, stream)) return rc;
+        if (int rc = launch(fn.step, a.rows, cis::kHistBlock, &a, stream)) return rc;
     }
     if (weighed) {
       // a chunk per wave, or more of them where the chip is filled all the same
       const int64_t per = cis::kWeighBlock / 64, most = (s.nch + per - 1) / per,
                     fill = (kWeighBlocks + a.rows - 1) / a.rows;
       a.weigh_parts = (int32_t)(fill < most ? fill : most);
-      if (int rc = launch(cis::weigh_kernel(dtype, stepped), a.rows * a.weigh_parts, cis::kWeighBlock, &a,
-                          stream))
+      if (int rc = launch(fn.weigh, a.rows * a.weigh_parts, cis::kWeighBlock, &a, stream))
         return rc;
     }
-    if (int rc = launch(cis::sample_kernel(dtype, wide), a.rows, block, &a, stream)) return rc;
+    if (int rc = launch(fn.sample, a.rows, block, &a, stream)) return rc;
   }
   return CIS_OK;
 }
 
 // Target rows and drafts of a verification together, and its sequences.
 constexpr int64_t kMaxVerify = int64_t(1) << 31;
-// Workgroups of cis_verify_kernel beyond which a wave takes several chunks.
-constexpr int64_t kVerifyBlocks = 2048;
+// Workgroups of cis_verify_kernel beyond which a wave takes several pieces.
+constexpr int64_t kVerifyBlocks = 8192;
 struct VerifyLayout {
   size_t kept, stops, left, total;
 };
 VerifyLayout verify_layout(int64_t T, int64_t D, int64_t n_seq, int64_t V, int dtype) {
   VerifyLayout L{};
-  const int32_t nch = (row_vecs(V, dtype) + cis::kScanVecs - 1) / cis::kScanVecs;
+  const int32_t nsub = (row_vecs(V, dtype) + cis::kLeftVecs - 1) / cis::kLeftVecs;
   L.kept = cis::align_up(draw_bytes(T + D, V, dtype), 256);
   L.stops = L.kept + cis::align_up((size_t)(T + D) * sizeof(cis::RowKept), 256);
   L.left = L.stops + cis::align_up((size_t)n_seq * sizeof(cis::VerifyStop), 256);
-  L.total = L.left + cis::align_up((size_t)n_seq * nch * 8, 256);
+  L.total = L.left + cis::align_up((size_t)n_seq * nsub * 8, 256);
   if (L.total < 256) L.total = 256;
   return L;
 }
@@ -571,14 +572,19 @@ int cis_verify(const void* logits, int dtype, int64_t T, int64_t V, int64_t ld,
   a.accepted = accepted_out;
   a.logp = logp_out;
   a.logp_kept = logp_kept_out;
-  const int64_t per = cis::kVerifyBlock / 64, most = (a.nch + per - 1) / per,
+  a.nsub = (c.r.nvec + cis::kLeftVecs - 1) / cis::kLeftVecs;
+  const int64_t per = cis::kVerifyBlock / 64, most = (a.nsub + per - 1) / per,
                 fill = (kVerifyBlocks + n_seq - 1) / n_seq;
-  a.parts = (int32_t)(fill < most ? fill : most);
+  // distributions of one token leave nothing to draw from
+  const bool one = V == 1 || (!top_k && params->top_k == 1) ||
+                   (!temperature && !(cis::scan_c(params->temperature) < INFINITY));
+  a.parts = one ? 1 : (int32_t)(fill < most ? fill : most);
   const int64_t step = kMaxBlocks / a.parts > 0 ? kMaxBlocks / a.parts : 1;
   for (; a.seq0 < n_seq; a.seq0 += step) {
     const int64_t n = n_seq - a.seq0 < step ? n_seq - a.seq0 : step;
     if (int rc = launch(cis::verify_kernel(dtype), n * a.parts, cis::kVerifyBlock, &a, stream))
       return rc;
+    if (one) continue;
     if (int rc = launch(cis::verify_draw_kernel(dtype), n, cis::kVerifyBlock, &a, stream)) return rc;
   }
   return CIS_OK;

@@ -21,7 +21,7 @@ __global__ __launch_bounds__(kScanBlock) void cis_scan_kernel(const ScanArgs a) 
   for (int64_t w = (int64_t)blockIdx.x * NW + wid; w < total; w += (int64_t)gridDim.x * NW) {
     const int64_t row = w / nch;
     const int ch = (int)(w - row * nch);
-    if (!tok_on(a.r, row)) continue;
+    if (a.r.offsets ? !tok_seq_on(a.r, row) : !tok_on(a.r, row)) continue;
     const __amdgpu_buffer_rsrc_t rs = tok_rsrc(a.r, row);
     const int v0 = ch * kScanVecs + lane;
     u32x4 x[K];

@@ -18,6 +18,21 @@ __device__ __forceinline__ uint32_t kept_weight(const RowKept& k, float f, int i
   const uint32_t q = draw_weight(f, k.M, k.c);
   return token_of(f, id) >= k.last && q >= k.least_w ? q : 0u;
 }
+// The same for many tokens of a row: those with a logit above `bound`, and of that logit the ids up to
+// `most`. CUT: there is one (else no token lies below).
+struct KeptRow {
+  float M, c, bound;
+  uint32_t least_w, most;
+  __device__ __forceinline__ explicit KeptRow(const RowKept& k)
+      : M(k.M), c(k.c), bound(k.last ? key_value((uint32_t)(k.last >> 32)) : -INFINITY),
+        least_w(k.least_w), most(~(uint32_t)k.last) {}
+  template <bool CUT>
+  __device__ __forceinline__ uint32_t weight(float f, int id) const {
+    const uint32_t q = draw_weight(f, M, c);
+    const bool in = !CUT || f > bound || (f == bound && (uint32_t)id <= most);
+    return in && q >= least_w ? q : 0u;
+  }
+};
 __device__ __forceinline__ void put_token(const VerifyArgs& a, int64_t row, int id, float logp,
                                           float logp_kept) {
   a.ids[row] = id;
@@ -54,35 +69,43 @@ struct Leftover {
     }
   }
   // Of vector v's tokens; `whole`: P itself.
+  template <bool CUT>
   __device__ __forceinline__ void weights(int v, bool whole, uint32_t (&w)[EPV], float (&f)[EPV]) const {
     float g[EPV];
     tok_vec<E>(rp, v, V, f);
     if (dist) tok_vec<E>(rq, v, V, g);
+    const KeptRow kp(p), kq(q);
 #pragma unroll
     for (int e = 0; e < EPV; ++e) {
       const int id = v * EPV + e;
-      w[e] = kept_weight(p, f[e], id);
+      w[e] = kp.weight<CUT>(f[e], id);
       if (whole) continue;
       if (dist) {
-        const double less = floor((double)kept_weight(q, g[e], id) * rho);
-        w[e] = less < (double)w[e] ? w[e] - (uint32_t)less : 0u;
+        const uint32_t less =
+            (uint32_t)fmin((double)kq.weight<CUT>(g[e], id) * rho, 0x1p32 - 1.0);   // (its floor)
+        w[e] -= less < w[e] ? less : w[e];
       } else if (id == draft) {
         w[e] = 0;
       }
     }
   }
-  // A wave's sum over a chunk.
-  __device__ __forceinline__ u64 chunk(int ch, bool whole, int lane) const {
+  __device__ __forceinline__ bool cut() const { return (p.last | q.last) != 0; }
+  // A wave's sum over a piece of the row.
+  template <bool CUT>
+  __device__ __forceinline__ u64 piece_of(int sub, bool whole, int lane) const {
     u64 s = 0;
-#pragma unroll 2
-    for (int i = 0; i < kScanSlots; ++i) {
-      uint32_t w[EPV];
+    static_for<kLeftVecs / 64>([&](auto I) __attribute__((always_inline)) {
+      uint32_t w[EPV], vs = 0;   // (8 weights stay below 2^32)
       float f[EPV];
-      weights(ch * kScanVecs + i * 64 + lane, whole, w, f);
+      weights<CUT>(sub * kLeftVecs + I * 64 + lane, whole, w, f);
 #pragma unroll
-      for (int e = 0; e < EPV; ++e) s += w[e];
-    }
+      for (int e = 0; e < EPV; ++e) vs += w[e];
+      s += vs;
+    });
     return wave_sum(s);
+  }
+  __device__ __forceinline__ u64 piece(int sub, bool whole, int lane) const {
+    return cut() ? piece_of<true>(sub, whole, lane) : piece_of<false>(sub, whole, lane);
   }
   // Whether a chunk whose largest logit is m can hold a weight.
   __device__ __forceinline__ bool reaches(float m) const {
@@ -91,24 +114,16 @@ struct Leftover {
 };
 
 // ------------------------------------------------------------------------------------------
-// A sequence's drafts, by every wave alike, a lane to a row, up to the first that is turned down; then the
-// weights of its row by chunks, a wave's in turn.
+// A sequence's drafts, a lane to a row, up to the first that is turned down, by the first wave of each of
+// its workgroups (of which one writes); then the weights that are left of its row, a piece to a wave.
 // ------------------------------------------------------------------------------------------
 template <class E>
-__global__ __launch_bounds__(kVerifyBlock) void cis_verify_kernel(const VerifyArgs a) {
-  constexpr int NW = kVerifyBlock / 64;
-  const int lane = threadIdx.x & 63, wid = __builtin_amdgcn_readfirstlane(threadIdx.x) >> 6;
-  const uint32_t at = blockIdx.x / (uint32_t)a.parts;
-  const int part = (int)(blockIdx.x - at * (uint32_t)a.parts);
-  const int64_t seq = a.seq0 + at, T = a.r.T1;
-  const int64_t o0 = sload(a.r.offsets + seq), o1 = sload(a.r.offsets + seq + 1);
-  const bool writes = part == 0 && wid == 0;
+__device__ __forceinline__ VerifyStop judge(const VerifyArgs& a, int64_t seq, bool writes) {
+  const int lane = threadIdx.x & 63;
+  const int64_t o0 = sload(a.r.offsets + seq), o1 = sload(a.r.offsets + seq + 1), T = a.r.T1;
   if (o0 < 0 || o1 < o0 || o1 > T || (o1 > o0 + 1 && (o0 < seq || o1 - 1 - seq > a.D))) {
-    if (writes && lane == 0) {
-      a.accepted[seq] = -1;
-      a.stops[seq].row = -1;
-    }
-    return;
+    if (writes && lane == 0) a.accepted[seq] = -1;
+    return VerifyStop{-1, 0};
   }
   const int64_t n = o1 - o0;
   int64_t stop = n;            // where the sequence ends
@@ -118,43 +133,43 @@ __global__ __launch_bounds__(kVerifyBlock) void cis_verify_kernel(const VerifyAr
     const int64_t i = i0 + lane, row = o0 + i;
     enum { kTake, kDraw, kEnd } what = kEnd;
     int d = 0;
-    float lp = 0.f, lk = 0.f;
-    if (i < n) {
-      const RowKept k = a.kept[row];
-      if (k.id < 0) {
-      } else if (i == n - 1) {   // after the last draft
-        what = kTake;
-        d = k.id;
-        lp = k.logp;
-        lk = k.logp_kept;
-      } else {
-        const int64_t id = a.draft_ids[row - seq];
-        bool ok = id >= 0 && id < a.r.V;
-        double share = (double)k.N;
-        if (ok && a.r.draft) {
-          const RowKept q = a.kept[T + row - seq];
-          ok = q.id >= 0;
-          if (ok) {
-            const uint32_t w = kept_weight(q, lane_elem<E>(a.r.draft, a.r.draft_bytes, row - seq, (int)id),
-                                           (int)id);
-            share = (double)w * ((double)k.N / (double)q.N);
-          }
-        }
-        if (ok) {
-          d = (int)id;
-          const float f = lane_elem<E>(a.r.logits, a.r.row_bytes, row, d);
-          const uint32_t w = kept_weight(k, f, d);
-          what = (double)a.u[row] * share < (double)w ? kTake : kDraw;
-          if (what == kTake) {
-            lp = kept_logp(k, f);
-            lk = kept_share(k, w);
-          }
-        }
+    uint32_t w = 0;
+    float f = 0.f;
+    RowKept k;
+    k.id = -1;
+    const bool drafted = i < n - 1;
+    int64_t id = -1;
+    float u = 0.f;
+    if (i < n) k = a.kept[row];
+    if (drafted) {
+      id = a.draft_ids[row - seq];
+      u = a.u[row];
+    }
+    if (k.id >= 0 && !drafted) {   // after the last draft
+      what = kTake;
+      d = k.id;
+    } else if (k.id >= 0 && id >= 0 && id < a.r.V) {
+      d = (int)id;
+      f = lane_elem<E>(a.r.logits, a.r.row_bytes, row, d);
+      w = kept_weight(k, f, d);
+      double share = (double)k.N;
+      bool ok = true;
+      if (a.r.draft) {
+        const RowKept q = a.kept[T + row - seq];
+        const float g = lane_elem<E>(a.r.draft, a.r.draft_bytes, row - seq, d);
+        ok = q.id >= 0;
+        share = (double)kept_weight(q, g, d) * ((double)k.N / (double)q.N);
       }
+      if (ok) what = (double)u * share < (double)w ? kTake : kDraw;
     }
     const u64 ends = __ballot(what != kTake);
     const int first = ends ? __ffsll(ends) - 1 : 64;
-    if (writes && lane < first) put_token(a, row, d, lp, lk);
+    if (writes && lane < first) {
+      if (drafted)
+        put_token(a, row, d, kept_logp(k, f), kept_share(k, w));
+      else
+        put_token(a, row, d, k.logp, k.logp_kept);
+    }
     if (ends) {
       stop = i0 + first;
       turned_down = __shfl((int)what, first, 64) == kDraw;
@@ -162,22 +177,44 @@ __global__ __launch_bounds__(kVerifyBlock) void cis_verify_kernel(const VerifyAr
       break;
     }
   }
-  if (turned_down) {   // its draw needs a number
-    const float ud = sload(a.u + o1 - 1);
-    turned_down = ud >= 0.f && ud < 1.f;
+  if (turned_down) {
+    const RowKept k = a.kept[o0 + stop];
+    const float u = sload(a.u + o1 - 1);
+    turned_down = u >= 0.f && u < 1.f;   // (its draw needs a number)
+    if (turned_down && k.N == kDrawOne) {
+      // a distribution of one token: the largest logit's weight, and nothing besides
+      if (writes && lane == 0) put_token(a, o0 + stop, k.id, k.logp, k.logp_kept);
+      turned_down = false;
+    }
   }
   // (a sequence that goes through ends with the token after its last draft)
-  if (writes && lane == 0) {
-    a.accepted[seq] = (int32_t)(stop < n ? stop : n > 0 ? n - 1 : 0);
-    a.stops[seq] = VerifyStop{turned_down ? o0 + stop : -1, draft};
+  if (writes && lane == 0) a.accepted[seq] = (int32_t)(stop < n ? stop : n > 0 ? n - 1 : 0);
+  return VerifyStop{turned_down ? o0 + stop : -1, draft};
+}
+
+template <class E>
+__global__ __launch_bounds__(kVerifyBlock) void cis_verify_kernel(const VerifyArgs a) {
+  constexpr int NW = kVerifyBlock / 64;
+  __shared__ VerifyStop shared;
+  const int lane = threadIdx.x & 63, wid = __builtin_amdgcn_readfirstlane(threadIdx.x) >> 6;
+  const uint32_t at = blockIdx.x / (uint32_t)a.parts;
+  const int part = (int)(blockIdx.x - at * (uint32_t)a.parts);
+  const int64_t seq = a.seq0 + at;
+  if (wid == 0) {
+    const VerifyStop j = judge<E>(a, seq, part == 0);
+    if (lane == 0) {
+      shared = j;
+      if (part == 0) a.stops[seq] = j;
+    }
   }
-  if (!turned_down) return;
-  const VerifyStop s{o0 + stop, draft};
+  __syncthreads();
+  const VerifyStop s = shared;
+  if (s.row < 0) return;
   const Leftover<E> left(a, s, seq);
   const float* cmax = a.cmax + s.row * a.nch;
-  for (int ch = part * NW + wid; ch < a.nch; ch += a.parts * NW) {
-    const u64 sum = left.reaches(cmax[ch]) ? left.chunk(ch, false, lane) : 0;
-    if (lane == 0) a.left[seq * a.nch + ch] = sum;
+  for (int sub = part * NW + wid; sub < a.nsub; sub += a.parts * NW) {
+    const u64 sum = left.reaches(cmax[sub / (kScanVecs / kLeftVecs)]) ? left.piece(sub, false, lane) : 0;
+    if (lane == 0) a.left[seq * a.nsub + sub] = sum;
   }
 }
 
@@ -186,8 +223,8 @@ __global__ __launch_bounds__(kVerifyBlock) void cis_verify_kernel(const VerifyAr
 // ------------------------------------------------------------------------------------------
 template <class E>
 __global__ __launch_bounds__(kVerifyBlock) void cis_verify_draw_kernel(const VerifyArgs a) {
-  constexpr int BLOCK = kVerifyBlock, NW = BLOCK / 64, EPV = E::kPerVec, PV = kScanVecs / BLOCK;
-  static_assert(kScanVecs % BLOCK == 0, "a thread has the same number of vectors");
+  constexpr int BLOCK = kVerifyBlock, NW = BLOCK / 64, EPV = E::kPerVec;
+  static_assert(kLeftVecs <= BLOCK, "a thread has one vector of a piece");
   __shared__ u64 sh[NW];
   __shared__ u64 place[3];
   const int tid = threadIdx.x, lane = tid & 63, wid = tid >> 6;
@@ -195,15 +232,15 @@ __global__ __launch_bounds__(kVerifyBlock) void cis_verify_draw_kernel(const Ver
   const VerifyStop s{a.stops[seq].row, a.stops[seq].draft};
   if (s.row < 0) return;
   const Leftover<E> left(a, s, seq);
-  u64* mass = a.left + seq * a.nch;
+  u64* mass = a.left + seq * a.nsub;
   u64 total = 0;
-  for (int i = tid; i < a.nch; i += BLOCK) total += mass[i];
+  for (int i = tid; i < a.nsub; i += BLOCK) total += mass[i];
   total = block_sum<NW>(total, sh);
   const bool whole = total == 0;
   if (whole) {   // nothing is left: the draw is from the row's own distribution
-    for (int ch = wid; ch < a.nch; ch += NW) {
-      const u64 m = left.chunk(ch, true, lane);
-      if (lane == 0) mass[ch] = m;
+    for (int sub = wid; sub < a.nsub; sub += NW) {
+      const u64 m = left.piece(sub, true, lane);
+      if (lane == 0) mass[sub] = m;
     }
     total = left.p.N;
     __syncthreads();
@@ -212,8 +249,8 @@ __global__ __launch_bounds__(kVerifyBlock) void cis_verify_draw_kernel(const Ver
   if (to >= total) to = total - 1;
   if (tid < 64) {
     u64 before = 0;
-    for (int i0 = 0; i0 < a.nch; i0 += 64) {
-      const u64 m = i0 + lane < a.nch ? mass[i0 + lane] : 0, upto = before + wave_scan(m, lane);
+    for (int i0 = 0; i0 < a.nsub; i0 += 64) {
+      const u64 m = i0 + lane < a.nsub ? mass[i0 + lane] : 0, upto = before + wave_scan(m, lane);
       const u64 hit = __ballot(upto > to);
       if (hit) {
         const int who = __ffsll(hit) - 1;
@@ -228,15 +265,15 @@ __global__ __launch_bounds__(kVerifyBlock) void cis_verify_draw_kernel(const Ver
     }
   }
   __syncthreads();
-  const int v0 = (int)place[0] * kScanVecs + tid * PV;
-  uint32_t w[PV][EPV];
-  float f[PV][EPV];
+  uint32_t w[EPV];
+  float f[EPV];
   u64 sum = 0;
-  static_for<PV>([&](auto J) {
-    left.weights(v0 + J, whole, w[J], f[J]);
+  const int v = (int)place[0] * kLeftVecs + tid;
+  if (tid < kLeftVecs) {
+    left.template weights<true>(v, whole, w, f);
 #pragma unroll
-    for (int e = 0; e < EPV; ++e) sum += w[J][e];
-  });
+    for (int e = 0; e < EPV; ++e) sum += w[e];
+  }
   const u64 upto = wave_scan(sum, lane);
   if (lane == 63) sh[wid] = upto;
   __syncthreads();
@@ -244,18 +281,16 @@ __global__ __launch_bounds__(kVerifyBlock) void cis_verify_draw_kernel(const Ver
   for (int k = 0; k < wid; ++k) before += sh[k];
   if (before <= to && to < before + sum) {
     bool found = false;
-    static_for<PV>([&](auto J) {
 #pragma unroll
-      for (int e = 0; e < EPV; ++e) {
-        if (!found && before + w[J][e] > to) {
-          found = true;
-          const int id = (v0 + J) * EPV + e;
-          put_token(a, s.row, id, kept_logp(left.p, f[J][e]),
-                    kept_share(left.p, kept_weight(left.p, f[J][e], id)));
-        }
-        before += w[J][e];
+    for (int e = 0; e < EPV; ++e) {
+      if (!found && before + w[e] > to) {
+        found = true;
+        const int id = v * EPV + e;
+        put_token(a, s.row, id, kept_logp(left.p, f[e]),
+                  kept_share(left.p, kept_weight(left.p, f[e], id)));
       }
-    });
+      before += w[e];
+    }
   }
 }
 
