@@ -371,6 +371,12 @@ struct RowDraw {
     rest = (float)block_sum<NW>(s, sh.d);
   }
 
+  // Verification: a draft's row is not drawn from; it is done once its distribution is known.
+  __device__ __forceinline__ bool draft() const { return KEEP && row >= a.r.T1; }
+  __device__ __forceinline__ void put_draft(u64 N) const {
+    a.kept[row] = RowKept{last_kept, N, sel.M, p.c, p.least_w, 0.f, 0, 0.f, 0.f};
+  }
+
   // Takes the first of the row's largest logits.
   __device__ __forceinline__ void from_largest() {
     int id = largest;
@@ -438,6 +444,10 @@ struct RowDraw {
     });
     __syncthreads();
     const u64 N = block_sum<NW>(s, sh.u);
+    if (draft()) {
+      if (tid == 0) put_draft(N);
+      return;
+    }
     u64 at = (u64)((double)p.u * (double)N);
     if (at >= N) at = N - 1;
     // in order of the ids: (id, weight) pairs
@@ -523,6 +533,10 @@ struct RowDraw {
       Place at{0, 0, 0, 0, 0};
       u64 tb = 0, nt;
       for (int i0 = 0; i0 < sel.nch; i0 += 64) at.N += wave_sum(chunk_mass(i0, tb, nt));
+      if (draft()) {
+        if (lane == 0) put_draft(at.N);
+        return;
+      }
       at.to = (u64)((double)p.u * (double)at.N);
       if (at.to >= at.N) at.to = at.N - 1;
       tb = 0;
@@ -540,6 +554,7 @@ struct RowDraw {
       }
       if (lane == 0) put_place(at);
     }
+    if (draft()) return;
     auto above = [&](float f, int) {
       const uint32_t q = weight(f);
       return order_key(f) > cut.key && q >= least ? q : 0u;
@@ -943,6 +958,10 @@ struct RowDraw {
       Place at{0, 0, 0, 0, 0};
       for (int i = lane; i < sel.nch; i += 64) at.N += ws.mass[i];
       at.N = wave_sum(at.N);
+      if (draft()) {
+        if (lane == 0) put_draft(at.N);
+        return true;
+      }
       at.to = (u64)((double)p.u * (double)at.N);
       if (at.to >= at.N) at.to = at.N - 1;
       for (int i0 = 0; i0 < sel.nch; i0 += 64) {
@@ -958,6 +977,7 @@ struct RowDraw {
       }
       if (lane == 0) put_place(at);
     }
+    if (draft()) return true;
     auto kept = [&](float f, int id) {
       const float t = draw_exponent(f, sel.M, p.c);
       const int st = draw_step(t);
@@ -971,7 +991,7 @@ struct RowDraw {
 
   __device__ __forceinline__ void run(WideShared* ws) {
     const int tid = threadIdx.x;
-    sum_rest();
+    if (!draft() || p.top_k == 1) sum_rest();
     const int64_t V = sel.V;
     const int k = (int)p.top_k;
     if (p.counted && k == 1) {
