@@ -44,17 +44,24 @@ constexpr int kNormColumns = 256;             // threads of 8 columns each in a 
 constexpr int kNormReduce = 1024, kNormReduceCols = 16;
 constexpr int32_t kNormGradResident = 16384;  // elements of a row up to which the gradients take one pass
 
-// The kernel for rows of H elements, with `lanes` lanes to a row, or in passes over it (0: one workgroup of
-// kNormBlock threads per row).
+// The kernel for rows of H elements, with `lanes` lanes to a row (up to 64 in workgroups of 256, else a
+// workgroup), or in passes over it (0: one workgroup of kNormBlock threads per row).
 struct NormVariant {
   int lanes;
   const void* fn;
 };
-inline int norm_block(int lanes) { return lanes == 0 ? kNormBlock : lanes > 256 ? lanes : 256; }
+inline int norm_block(int lanes) { return lanes == 0 ? kNormBlock : lanes > 64 ? lanes : 256; }
 inline int norm_block_rows(int lanes) { return lanes == 0 ? 1 : norm_block(lanes) / lanes; }
 // x and stream in float32 or bf16; res: a residual is added
 NormVariant norm_kernel(int32_t H, bool x_f32, bool stream_f32, bool res);
 NormVariant norm_grad_kernel(int32_t H, bool dy_f32, bool x_f32);
+// Lanes to a row in the backward pass (0: in passes): whole waves of one group of 8 elements to a lane, or two.
+inline int norm_grad_lanes(int32_t H) {
+  const int n8 = (H + 7) / 8;
+  if (n8 <= 64) return n8 <= 16 ? 16 : n8 <= 32 ? 32 : 64;
+  if (n8 <= 1024) return (n8 + 63) / 64 * 64;
+  return H <= kNormGradResident ? (n8 + 127) / 128 * 64 : 0;
+}
 const void* norm_rstd_kernel(bool x_f32);
 const void* norm_part_kernel(bool dy_f32, bool x_f32);
 const void* norm_reduce_kernel();

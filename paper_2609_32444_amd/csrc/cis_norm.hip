@@ -175,17 +175,17 @@ __device__ __forceinline__ void store_e4m3(const R& row, int g, int H, const flo
 __device__ __forceinline__ int vecs_of(int dtype, int H) {
   return dtype == CIS_E4M3 ? (H + 15) / 16 : dtype == CIS_F32 ? (H + 3) / 4 : (H + 7) / 8;
 }
-__device__ __forceinline__ float rstd_of(double ss, int H, float eps) {
-  return (float)(1.0 / sqrt(ss / (double)H + (double)eps));
+__device__ __forceinline__ float rstd_of(double ss, double inv_h, float eps) {
+  return (float)rsqrt(ss * inv_h + (double)eps);
 }
 
 // The weight's groups as they are stored, asked for without waiting: ones where there is no weight, zeros
 // past its end, beyond which it is not read.
 // (Values are chosen, not stores: else the arrays end up in scratch memory.)
-template <int LANES, int NV>
+template <int NV>
 struct WeightRow {
   u32x4 lo[NV], hi[NV];
-  __device__ __forceinline__ void load(const void* w, bool f32, int l, int H) {
+  __device__ __forceinline__ void load(const void* w, bool f32, int l, int lanes, int H) {
     const int nvec = f32 ? H / 4 : H / 8;   // whole ones
     const uint32_t one = w ? 0u : f32 ? 0x3F800000u : 0x3F803F80u;
     const u32x4 none{one, one, one, one};
@@ -196,7 +196,7 @@ struct WeightRow {
       return i < nvec ? x : none;
     };
     static_for<NV>([&](auto I) __attribute__((always_inline)) {
-      const int g = l + I * LANES;
+      const int g = l + I * lanes;
       lo[I] = at(f32 ? 2 * g : g);
       hi[I] = none;
       if (f32) hi[I] = at(2 * g + 1);
@@ -214,7 +214,7 @@ struct WeightRow {
         }
       const u32x4 last{x[0], x[1], x[2], x[3]};
       static_for<NV>([&](auto I) __attribute__((always_inline)) {
-        const int g = l + I * LANES;
+        const int g = l + I * lanes;
         lo[I] = (f32 ? 2 * g : g) == nvec ? last : lo[I];
         hi[I] = f32 && 2 * g + 1 == nvec ? last : hi[I];
       });
@@ -296,8 +296,8 @@ __global__ __launch_bounds__(kRowBlock<LANES>) void cis_norm_row_kernel(const No
     rx[I] = load_raw<X>(x, l + I * LANES);
     if constexpr (RES) rr[I] = load_raw<S>(r, l + I * LANES);
   });
-  WeightRow<LANES, NV> w;
-  w.load(a.w, a.w_f32, l, H);
+  WeightRow<NV> w;
+  w.load(a.w, a.w_f32, l, LANES, H);
   float f[NV][8];
   double ss = 0.0;
   static_for<NV>([&](auto I) __attribute__((always_inline)) {
@@ -313,7 +313,7 @@ __global__ __launch_bounds__(kRowBlock<LANES>) void cis_norm_row_kernel(const No
 #pragma unroll
     for (int e = 0; e < 8; ++e) ss = fma((double)f[I][e], (double)f[I][e], ss);
   });
-  const float rstd = rstd_of(lanes_sum<LANES>(ss, sh), H, a.eps);
+  const float rstd = rstd_of(lanes_sum<LANES>(ss, sh), 1.0 / (double)H, a.eps);
   if (RES && a.s.p && on) {   // (all of the row has been read)
     const auto s = row_of<WAVE>(a.s, row, a.N, sv);
     static_for<NV>([&](auto I) __attribute__((always_inline)) {
@@ -363,20 +363,34 @@ __global__ __launch_bounds__(kRowBlock<LANES>) void cis_norm_row_kernel(const No
 
 // The gradients, with rows that a workgroup's lanes take in turn and dweight's sums in registers; a
 // workgroup's are a part.
+//
+// Registers decide how many rows a compute unit has on their way: of 8 elements a thread 5 waves fit a SIMD,
+// so that a row of up to 8192 elements takes as many waves as it fills, not a power of two of them.
 template <class D, class X, int LANES, int NV>
-__global__ __launch_bounds__(kRowBlock<LANES>) void cis_norm_grad_row_kernel(const NormGradArgs a) {
-  constexpr int NW = LANES > 64 ? LANES / 64 : 1, BLOCK = kRowBlock<LANES>, R = BLOCK / LANES;
-  __shared__ double sh[2][2][NW];
-  __shared__ float sum[R > 1 ? BLOCK : 1][9];
+__global__ __launch_bounds__(LANES ? 256 : 1024) __attribute__((amdgpu_waves_per_eu(NV == 1 ? 5 : 4)))
+void cis_norm_grad_row_kernel(const NormGradArgs a) {
+  constexpr bool WAVES = LANES == 0;   // a workgroup of any number of waves to a row
+  constexpr int R = WAVES ? 1 : 256 / LANES;
+  const int lanes = WAVES ? (int)blockDim.x : LANES;
+  __shared__ double sh[2][2][16];
+  __shared__ float sum[R > 1 ? 256 : 1][9];
   const int H = a.H, n8 = (H + 7) / 8;
   const int dv = (H + D::kPerVec - 1) / D::kPerVec, xv = (H + X::kPerVec - 1) / X::kPerVec;
   const int rv = a.dx_f32 ? (H + 3) / 4 : n8;
-  constexpr bool WAVE = LANES >= 64;
-  const int l0 = threadIdx.x % LANES;
-  uint32_t at = threadIdx.x / LANES;
-  if (LANES >= 64) at = __builtin_amdgcn_readfirstlane(at);
-  WeightRow<LANES, NV> w;
-  w.load(a.w, a.w_f32, l0, H);
+  constexpr bool WAVE = WAVES || LANES == 64;
+  const int l0 = WAVES ? threadIdx.x : threadIdx.x % (LANES + WAVES);
+  uint32_t at = WAVES ? 0 : threadIdx.x / (LANES + WAVES);
+  if (WAVE) at = __builtin_amdgcn_readfirstlane(at);
+  WeightRow<NV> w;
+  w.load(a.w, a.w_f32, l0, lanes, H);
+  // (waited for here: else every row would wait for all that the row before it stored)
+  opaque(w.lo);
+  opaque(w.hi);
+  if (WAVES) {
+    if (threadIdx.x < 64) (&sh[0][0][0])[threadIdx.x] = 0.0;
+    __syncthreads();
+  }
+  const double inv_h = 1.0 / (double)H;
   float acc[NV][8] = {};
   int turn = 0;
   for (uint64_t row0 = (uint64_t)blockIdx.x * R; row0 < a.rows; row0 += (uint64_t)gridDim.x * R) {
@@ -390,22 +404,22 @@ __global__ __launch_bounds__(kRowBlock<LANES>) void cis_norm_grad_row_kernel(con
     Raw<X> rx[NV];
     Raw<D> rd[NV];
     static_for<NV>([&](auto I) __attribute__((always_inline)) {
-      rx[I] = load_raw<X>(x, l + I * LANES);
-      rd[I] = load_raw<D>(dy, l + I * LANES);
+      rx[I] = load_raw<X>(x, l + I * lanes);
+      rd[I] = load_raw<D>(dy, l + I * lanes);
     });
     u32x4 lo[NV], hi[NV];   // dr
     static_for<NV>([&](auto I) __attribute__((always_inline)) { lo[I] = hi[I] = u32x4{0, 0, 0, 0}; });
     if (a.dr.p) {
       const auto dr = row_of<WAVE>(a.dr, row, a.N, rv);
       static_for<NV>([&](auto I) __attribute__((always_inline)) {
-        const int g = l + I * LANES;
+        const int g = l + I * lanes;
         lo[I] = dr.load(a.dx_f32 ? 2 * g : g);
         if (a.dx_f32) hi[I] = dr.load(2 * g + 1);
       });
     }
     double ss = 0.0, dot = 0.0;
     static_for<NV>([&](auto I) __attribute__((always_inline)) {
-      const int g = l + I * LANES;
+      const int g = l + I * lanes;
       float f[8], d[8], t[8];
       unpack8<X>(rx[I], g, H, f);
       unpack8<D>(rd[I], g, H, d);
@@ -419,14 +433,27 @@ __global__ __launch_bounds__(kRowBlock<LANES>) void cis_norm_grad_row_kernel(con
     });
     hold(rx);
     hold(rd);
-    ss = lanes_sum<LANES>(ss, sh[turn][0]);
-    dot = lanes_sum<LANES>(dot, sh[turn][1]);
-    turn ^= 1;   // (a wave may be a row ahead of another's reading)
-    const float rstd = rstd_of(ss, H, a.eps), mean = (float)(dot * (double)rstd / (double)H);
+    if constexpr (WAVES) {
+      ss = wave_sum(ss);
+      dot = wave_sum(dot);
+      if ((threadIdx.x & 63) == 0) {
+        sh[turn][0][threadIdx.x >> 6] = ss;
+        sh[turn][1][threadIdx.x >> 6] = dot;
+      }
+      __syncthreads();
+      // (zeros behind the last wave's)
+      ss = lanes_sum<16>(sh[turn][0][threadIdx.x & 15], nullptr);
+      dot = lanes_sum<16>(sh[turn][1][threadIdx.x & 15], nullptr);
+      turn ^= 1;   // (a wave may be a row ahead of another's reading)
+    } else {
+      ss = lanes_sum<LANES + WAVES>(ss, nullptr);
+      dot = lanes_sum<LANES + WAVES>(dot, nullptr);
+    }
+    const float rstd = rstd_of(ss, inv_h, a.eps), mean = (float)(dot * (double)rstd * inv_h);
     if (!on) continue;
     const auto dx = row_of<WAVE>(a.dx, row, a.N, rv);
     static_for<NV>([&](auto I) __attribute__((always_inline)) {
-      const int g = l + I * LANES;
+      const int g = l + I * lanes;
       if (g < n8) {
         float f[8], d[8], t[8];
         unpack8<X>(rx[I], g, H, f);
@@ -457,18 +484,19 @@ __global__ __launch_bounds__(kRowBlock<LANES>) void cis_norm_grad_row_kernel(con
   if (!a.dw) return;
   float* out = a.part + (int64_t)blockIdx.x * H;
   static_for<NV>([&](auto I) __attribute__((always_inline)) {
-    const int g = l0 + I * LANES;
+    const int g = l0 + I * lanes;
     if constexpr (R > 1) {   // the rows' lanes, in order
       __syncthreads();
 #pragma unroll
       for (int e = 0; e < 8; ++e) sum[threadIdx.x][e] = acc[I][e];
       __syncthreads();
-      if (threadIdx.x < LANES)
+      if ((int)threadIdx.x < lanes)
+#pragma unroll 1
         for (int k = 1; k < R; ++k)
 #pragma unroll
-          for (int e = 0; e < 8; ++e) acc[I][e] += sum[k * LANES + l0][e];
+          for (int e = 0; e < 8; ++e) acc[I][e] += sum[k * lanes + l0][e];
     }
-    if (threadIdx.x < LANES) {
+    if ((int)threadIdx.x < lanes) {
 #pragma unroll
       for (int e = 0; e < 8; ++e)
         if (g * 8 + e < H) out[g * 8 + e] = acc[I][e];
@@ -510,7 +538,7 @@ __global__ __launch_bounds__(kNormBlock) void cis_norm_kernel(const NormArgs a) 
 #pragma unroll
     for (int e = 0; e < 8; ++e) ss = fma((double)f[e], (double)f[e], ss);
   }
-  const float rstd = rstd_of(block_sum<NW>(ss, sh), H, a.eps);
+  const float rstd = rstd_of(block_sum<NW>(ss, sh), 1.0 / (double)H, a.eps);
   // y's group; of lanes past the row zeros. (The sum is read again as it was stored, by the thread that
   // stored it: it may have replaced what it was made from.)
   auto out8 = [&](int g, float (&f)[8]) {
@@ -592,7 +620,8 @@ __global__ __launch_bounds__(kNormBlock) void cis_norm_grad_kernel(const NormGra
   }
   ss = block_sum<NW>(ss, sh[0]);
   dot = block_sum<NW>(dot, sh[1]);
-  const float rstd = rstd_of(ss, H, a.eps), mean = (float)(dot * (double)rstd / (double)H);
+  const float rstd = rstd_of(ss, 1.0 / (double)H, a.eps),
+              mean = (float)(dot * (double)rstd / (double)H);
   for (int g = threadIdx.x; g < n8; g += kNormBlock) {
     float f[8], d[8];
     load(g, f, d);
@@ -629,7 +658,7 @@ __global__ __launch_bounds__(kNormBlock) void cis_norm_rstd_kernel(const NormGra
     for (int e = 0; e < 8; ++e) ss = fma((double)f[e], (double)f[e], ss);
   }
   ss = block_sum<NW>(ss, sh);
-  if (threadIdx.x == 0) a.rstd[row] = rstd_of(ss, H, a.eps);
+  if (threadIdx.x == 0) a.rstd[row] = rstd_of(ss, 1.0 / (double)H, a.eps);
 }
 
 // dweight's sums over the rows p, p + parts, ... of part p, 8 columns to a thread.
@@ -717,21 +746,19 @@ NormVariant norm_kernel(int32_t H, bool x_f32, bool stream_f32, bool res) {
   return {0, stream_f32 ? (const void*)&cis_norm_kernel<Bf16, F32, true>
                         : (const void*)&cis_norm_kernel<Bf16, Bf16, true>};
 }
-// More lanes of fewer groups, since each group takes another 70 registers: 16384 rows of 2048, dy in
-// float32, 64 lanes of 4 groups 77.7 us, 256 of 1 61.4.
 NormVariant norm_grad_kernel(int32_t H, bool dy_f32, bool x_f32) {
-  const int n8 = (H + 7) / 8;
-#define CIS_NORM(L, V) return grad_variant<L, V>(dy_f32, x_f32)
-  if (n8 <= 16) CIS_NORM(16, 1);
-  if (n8 <= 32) CIS_NORM(32, 1);
-  if (n8 <= 64) CIS_NORM(64, 1);
-  if (n8 <= 128) CIS_NORM(64, 2);
-  if (n8 <= 256) CIS_NORM(256, 1);
-  if (n8 <= 512) CIS_NORM(512, 1);
-  if (n8 <= 1024) CIS_NORM(512, 2);
-  if (n8 <= 2048) CIS_NORM(1024, 2);
-  static_assert(kNormGradResident == 2048 * 8, "the rows' sums need no room up to here");
-#undef CIS_NORM
+  const int lanes = norm_grad_lanes(H);
+  NormVariant v{};
+  if (lanes == 16)
+    v = grad_variant<16, 1>(dy_f32, x_f32);
+  else if (lanes == 32)
+    v = grad_variant<32, 1>(dy_f32, x_f32);
+  else if (lanes == 64)
+    v = grad_variant<64, 1>(dy_f32, x_f32);
+  else if (lanes)
+    v = H <= 8 * lanes ? grad_variant<0, 1>(dy_f32, x_f32) : grad_variant<0, 2>(dy_f32, x_f32);
+  v.lanes = lanes;
+  if (lanes) return v;
   if (dy_f32)
     return {0, x_f32 ? (const void*)&cis_norm_grad_kernel<F32, F32>
                      : (const void*)&cis_norm_grad_kernel<F32, Bf16>};

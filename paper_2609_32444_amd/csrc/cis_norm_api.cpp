@@ -12,8 +12,8 @@ using namespace cis::host;
 
 // Workgroups per launch (HIP refuses 2^32 work items).
 constexpr int64_t kMaxBlocks = int64_t(1) << 21;
-// Parts of dweight's sums: workgroups that take rows in turn.
-constexpr int64_t kGradParts = 1024;
+// Waves that take rows in turn in the backward pass: 20 to a compute unit, as many as registers allow.
+constexpr int64_t kGradCus = 256, kGradWaves = 20;
 
 int bytes_of(int dtype) { return dtype == CIS_E4M3 ? 1 : elem_bytes(dtype); }
 
@@ -78,16 +78,24 @@ int check_weight(const void* w, int dtype) {
   return w && !known(dtype) ? CIS_ERR_DTYPE : CIS_OK;
 }
 
-uint32_t grad_parts(int64_t rows) { return (uint32_t)(rows < kGradParts ? rows : kGradParts); }
+// Parts of dweight's sums: the workgroups of the pass, or of its sums where it is in passes.
+uint32_t grad_parts(int64_t rows, int32_t H) {
+  const int lanes = cis::norm_grad_lanes(H), per = lanes ? cis::norm_block_rows(lanes) : 1,
+            waves = (lanes ? cis::norm_block(lanes) : cis::kNormColumns) / 64;
+  const int64_t need = (rows + per - 1) / per, most = kGradCus * (kGradWaves / waves);
+  return (uint32_t)(need < most ? need : most);
+}
 struct GradLayout {
   size_t rstd, part, total;
+  uint32_t parts;
 };
 GradLayout grad_layout(const Shape& s) {
   GradLayout L{};
   const int64_t rows = s.T * s.N;
+  L.parts = grad_parts(rows, (int32_t)s.H);
   L.rstd = 0;
-  L.part = s.H > cis::kNormGradResident ? cis::align_up((size_t)rows * 4, 256) : 0;
-  L.total = L.part + cis::align_up((size_t)grad_parts(rows) * s.H * 4, 256);
+  L.part = cis::norm_grad_lanes((int32_t)s.H) ? 0 : cis::align_up((size_t)rows * 4, 256);
+  L.total = L.part + cis::align_up((size_t)L.parts * s.H * 4, 256);
   return L;
 }
 
@@ -239,10 +247,9 @@ int cis_rms_norm_bwd(int64_t T, int64_t N, int64_t H, const cis_rows_t* dy, cons
     return launch(cis::norm_reduce_kernel(), grid, cis::kNormReduce, &a, stream);
   };
   if (a.rows == 0) return dweight ? sum_parts() : CIS_OK;
+  a.parts = L.parts;
   const cis::NormVariant v = cis::norm_grad_kernel((int32_t)H, df, xf);
   if (v.lanes) {
-    const int64_t per = cis::norm_block_rows(v.lanes), need = (a.rows + per - 1) / per;
-    a.parts = grad_parts(need);
     if (int rc = launch(v.fn, a.parts, cis::norm_block(v.lanes), &a, stream)) return rc;
     return dweight ? sum_parts() : CIS_OK;
   }
@@ -255,7 +262,6 @@ int cis_rms_norm_bwd(int64_t T, int64_t N, int64_t H, const cis_rows_t* dy, cons
     return (int)CIS_OK;
   };
   if (dweight) {   // ahead of dx, which may replace what it is made from
-    a.parts = grad_parts(a.rows);
     if (int rc = by_rows(cis::norm_rstd_kernel(xf))) return rc;
     const int64_t cols = (H + 8 * cis::kNormColumns - 1) / (8 * cis::kNormColumns);
     if (int rc = launch(cis::norm_part_kernel(df, xf), cols * a.parts, cis::kNormColumns, &a, stream))
