@@ -42,7 +42,7 @@ struct NormGradArgs {
 constexpr int kNormBlock = 1024;              // threads to a row that goes in passes
 constexpr int kNormColumns = 256;             // threads of 8 columns each in a part of dweight's sums
 constexpr int kNormReduce = 1024, kNormReduceCols = 16;
-constexpr int32_t kNormGradResident = 16384;  // elements of a row up to which the gradients take one pass
+constexpr int32_t kNormGradResident = 8192;   // elements of a row up to which dweight's sums stay in registers
 
 // The kernel for rows of H elements, with `lanes` lanes to a row (up to 64 in workgroups of 256, else a
 // workgroup), or in passes over it (0: one workgroup of kNormBlock threads per row).
@@ -55,12 +55,13 @@ inline int norm_block_rows(int lanes) { return lanes == 0 ? 1 : norm_block(lanes
 // x and stream in float32 or bf16; res: a residual is added
 NormVariant norm_kernel(int32_t H, bool x_f32, bool stream_f32, bool res);
 NormVariant norm_grad_kernel(int32_t H, bool dy_f32, bool x_f32);
-// Lanes to a row in the backward pass (0: in passes): whole waves of one group of 8 elements to a lane, or two.
+// Lanes to a row in the backward pass, a group of 8 elements each: a part of a wave, or whole waves. (0: in
+// passes. Of two groups to a lane, 3355 rows of 10000, the registers leave so few waves that they are no
+// faster than passes: 76 us of 115.)
 inline int norm_grad_lanes(int32_t H) {
   const int n8 = (H + 7) / 8;
-  if (n8 <= 64) return n8 <= 16 ? 16 : n8 <= 32 ? 32 : 64;
-  if (n8 <= 1024) return (n8 + 63) / 64 * 64;
-  return H <= kNormGradResident ? (n8 + 127) / 128 * 64 : 0;
+  if (H > kNormGradResident) return 0;
+  return n8 <= 16 ? 16 : n8 <= 32 ? 32 : (n8 + 63) / 64 * 64;
 }
 const void* norm_rstd_kernel(bool x_f32);
 const void* norm_part_kernel(bool dy_f32, bool x_f32);

@@ -91,20 +91,44 @@ __device__ __forceinline__ void round_to(float (&f)[8]) {
     E::unpack(b, f);
   }
 }
+// The first n elements of 1 << LOG bytes of four words (fewer than fill them), in as few stores as there
+// are bits in n.
+template <int LOG>
+__device__ __forceinline__ void store_tail(char* p, u32x4 w, int n) {
+  uint32_t x = w[0], y = w[1];
+  const int bytes = n << LOG;
+  if (bytes & 8) {
+    *(u32x2*)p = u32x2{x, y};
+    x = w[2];
+    y = w[3];
+    p += 8;
+  }
+  if (bytes & 4) {
+    *(uint32_t*)p = x;
+    x = y;
+    p += 4;
+  }
+  if (LOG <= 1 && (bytes & 2)) {
+    *(uint16_t*)p = (uint16_t)x;
+    x >>= 16;
+    p += 2;
+  }
+  if (LOG == 0 && (bytes & 1)) *p = (char)x;
+}
 template <class E, class R>
 __device__ __forceinline__ void store8(const R& row, int g, int H, const float (&f)[8]) {
-  if ((g + 1) * 8 <= H) {
 #pragma unroll
-    for (int k = 0; k < kVecs<E>; ++k) {
-      float t[E::kPerVec];
+  for (int k = 0; k < kVecs<E>; ++k) {
+    float t[E::kPerVec];
 #pragma unroll
-      for (int e = 0; e < E::kPerVec; ++e) t[e] = f[k * E::kPerVec + e];
-      row.store(g * kVecs<E> + k, E::pack(t));
+    for (int e = 0; e < E::kPerVec; ++e) t[e] = f[k * E::kPerVec + e];
+    const int v = g * kVecs<E> + k, n = H - v * E::kPerVec;
+    const u32x4 x = E::pack(t);
+    if (n >= E::kPerVec) {
+      row.store(v, x);
+    } else if (n > 0) {
+      store_tail<E::kPerVec == 8 ? 1 : 2>(row.p + 16 * (int64_t)v, x, n);
     }
-  } else {
-#pragma unroll
-    for (int e = 0; e < 8; ++e)
-      if (g * 8 + e < H) E::store_elem(row.p, g * 8 + e, E::bits_of(f[e]));
   }
 }
 // The weight's group, which is not read past its end.
@@ -167,9 +191,7 @@ __device__ __forceinline__ void store_e4m3(const R& row, int g, int H, const flo
   if ((g + 1) * 8 <= H) {
     row.store2(g, u32x2{b[0], b[1]});
   } else {
-#pragma unroll
-    for (int e = 0; e < 8; ++e)
-      if (g * 8 + e < H) row.p[g * 8 + e] = (char)(b[e / 4] >> (8 * (e % 4)));
+    store_tail<0>(row.p + 8 * (int64_t)g, u32x4{b[0], b[1], 0, 0}, H - g * 8);
   }
 }
 __device__ __forceinline__ int vecs_of(int dtype, int H) {
@@ -366,10 +388,11 @@ __global__ __launch_bounds__(kRowBlock<LANES>) void cis_norm_row_kernel(const No
 //
 // Registers decide how many rows a compute unit has on their way: of 8 elements a thread 5 waves fit a SIMD,
 // so that a row of up to 8192 elements takes as many waves as it fills, not a power of two of them.
-template <class D, class X, int LANES, int NV>
-__global__ __launch_bounds__(LANES ? 256 : 1024) __attribute__((amdgpu_waves_per_eu(NV == 1 ? 5 : 4)))
+template <class D, class X, int LANES>
+__global__ __launch_bounds__(LANES ? 256 : 1024) __attribute__((amdgpu_waves_per_eu(5)))
 void cis_norm_grad_row_kernel(const NormGradArgs a) {
   constexpr bool WAVES = LANES == 0;   // a workgroup of any number of waves to a row
+  constexpr int NV = 1;                // groups to a lane
   constexpr int R = WAVES ? 1 : 256 / LANES;
   const int lanes = WAVES ? (int)blockDim.x : LANES;
   __shared__ double sh[2][2][16];
@@ -622,6 +645,7 @@ __global__ __launch_bounds__(kNormBlock) void cis_norm_grad_kernel(const NormGra
   dot = block_sum<NW>(dot, sh[1]);
   const float rstd = rstd_of(ss, 1.0 / (double)H, a.eps),
               mean = (float)(dot * (double)rstd / (double)H);
+  if (a.rstd && threadIdx.x == 0) a.rstd[row] = rstd;
   for (int g = threadIdx.x; g < n8; g += kNormBlock) {
     float f[8], d[8];
     load(g, f, d);
@@ -670,6 +694,7 @@ __global__ __launch_bounds__(kNormColumns) void cis_norm_part_kernel(const NormG
   const int g = (int)(blockIdx.x / a.parts) * kNormColumns + threadIdx.x;
   if (g >= n8) return;
   float acc[8] = {};
+#pragma unroll 4
   for (uint64_t row = part; row < a.rows; row += a.parts) {
     float f[8], d[8];
     unpack8<X>(load_raw<X>(row_of<false>(a.x, (uint32_t)row, a.N, xv), g), g, H, f);
@@ -714,9 +739,9 @@ NormVariant row_variant(bool x_f32, bool stream_f32, bool res) {
   return stream_f32 ? NormVariant CIS_NORM(Bf16, F32, true) : NormVariant CIS_NORM(Bf16, Bf16, true);
 #undef CIS_NORM
 }
-template <int LANES, int NV>
+template <int LANES>
 NormVariant grad_variant(bool dy_f32, bool x_f32) {
-#define CIS_NORM(D, X) NormVariant{LANES, (const void*)&cis_norm_grad_row_kernel<D, X, LANES, NV>}
+#define CIS_NORM(D, X) NormVariant{LANES, (const void*)&cis_norm_grad_row_kernel<D, X, LANES>}
   if (dy_f32) return x_f32 ? CIS_NORM(F32, F32) : CIS_NORM(F32, Bf16);
   return x_f32 ? CIS_NORM(Bf16, F32) : CIS_NORM(Bf16, Bf16);
 #undef CIS_NORM
@@ -750,13 +775,13 @@ NormVariant norm_grad_kernel(int32_t H, bool dy_f32, bool x_f32) {
   const int lanes = norm_grad_lanes(H);
   NormVariant v{};
   if (lanes == 16)
-    v = grad_variant<16, 1>(dy_f32, x_f32);
+    v = grad_variant<16>(dy_f32, x_f32);
   else if (lanes == 32)
-    v = grad_variant<32, 1>(dy_f32, x_f32);
+    v = grad_variant<32>(dy_f32, x_f32);
   else if (lanes == 64)
-    v = grad_variant<64, 1>(dy_f32, x_f32);
+    v = grad_variant<64>(dy_f32, x_f32);
   else if (lanes)
-    v = H <= 8 * lanes ? grad_variant<0, 1>(dy_f32, x_f32) : grad_variant<0, 2>(dy_f32, x_f32);
+    v = grad_variant<0>(dy_f32, x_f32);
   v.lanes = lanes;
   if (lanes) return v;
   if (dy_f32)

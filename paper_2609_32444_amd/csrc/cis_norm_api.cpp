@@ -78,11 +78,19 @@ int check_weight(const void* w, int dtype) {
   return w && !known(dtype) ? CIS_ERR_DTYPE : CIS_OK;
 }
 
-// Parts of dweight's sums: the workgroups of the pass, or of its sums where it is in passes.
+// Workgroups of cis_norm_part_kernel over the columns.
+int64_t part_columns(int64_t H) { return (H + 8 * cis::kNormColumns - 1) / (8 * cis::kNormColumns); }
+// Parts of dweight's sums: the workgroups of the pass, or where its registers do not hold them, shares of the
+// rows that fill the chip together with the shares of the columns.
 uint32_t grad_parts(int64_t rows, int32_t H) {
-  const int lanes = cis::norm_grad_lanes(H), per = lanes ? cis::norm_block_rows(lanes) : 1,
-            waves = (lanes ? cis::norm_block(lanes) : cis::kNormColumns) / 64;
-  const int64_t need = (rows + per - 1) / per, most = kGradCus * (kGradWaves / waves);
+  const int lanes = cis::norm_grad_lanes(H);
+  int64_t need = rows, most = kGradCus * (kGradWaves / (cis::kNormColumns / 64)) / part_columns(H);
+  if (H <= cis::kNormGradResident) {
+    const int64_t per = cis::norm_block_rows(lanes);
+    need = (rows + per - 1) / per;
+    most = kGradCus * (kGradWaves / (cis::norm_block(lanes) / 64));
+  }
+  if (most < 16) most = 16;
   return (uint32_t)(need < most ? need : most);
 }
 struct GradLayout {
@@ -94,7 +102,7 @@ GradLayout grad_layout(const Shape& s) {
   const int64_t rows = s.T * s.N;
   L.parts = grad_parts(rows, (int32_t)s.H);
   L.rstd = 0;
-  L.part = cis::norm_grad_lanes((int32_t)s.H) ? 0 : cis::align_up((size_t)rows * 4, 256);
+  L.part = s.H <= cis::kNormGradResident ? 0 : cis::align_up((size_t)rows * 4, 256);
   L.total = L.part + cis::align_up((size_t)L.parts * s.H * 4, 256);
   return L;
 }
@@ -249,7 +257,7 @@ int cis_rms_norm_bwd(int64_t T, int64_t N, int64_t H, const cis_rows_t* dy, cons
   if (a.rows == 0) return dweight ? sum_parts() : CIS_OK;
   a.parts = L.parts;
   const cis::NormVariant v = cis::norm_grad_kernel((int32_t)H, df, xf);
-  if (v.lanes) {
+  if (H <= cis::kNormGradResident) {
     if (int rc = launch(v.fn, a.parts, cis::norm_block(v.lanes), &a, stream)) return rc;
     return dweight ? sum_parts() : CIS_OK;
   }
@@ -261,14 +269,16 @@ int cis_rms_norm_bwd(int64_t T, int64_t N, int64_t H, const cis_rows_t* dy, cons
     }
     return (int)CIS_OK;
   };
-  if (dweight) {   // ahead of dx, which may replace what it is made from
-    if (int rc = by_rows(cis::norm_rstd_kernel(xf))) return rc;
-    const int64_t cols = (H + 8 * cis::kNormColumns - 1) / (8 * cis::kNormColumns);
-    if (int rc = launch(cis::norm_part_kernel(df, xf), cols * a.parts, cis::kNormColumns, &a, stream))
-      return rc;
-    if (int rc = sum_parts()) return rc;
-  }
-  return by_rows(v.fn);
+  if (!dweight) return by_rows(v.fn);
+  // dx, then the sums with the rstd that it leaves; ahead of a dx that replaces what they are made from,
+  // with a pass for rstd
+  const bool replaces = overlap(vg, vd) || overlap(vg, vx);
+  if (int rc = by_rows(replaces ? cis::norm_rstd_kernel(xf) : v.fn)) return rc;
+  if (int rc = launch(cis::norm_part_kernel(df, xf), part_columns(H) * a.parts, cis::kNormColumns, &a,
+                      stream))
+    return rc;
+  if (int rc = sum_parts()) return rc;
+  return replaces ? by_rows(v.fn) : CIS_OK;
 }
 
 }  // extern "C"
