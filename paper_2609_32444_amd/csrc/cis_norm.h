@@ -53,7 +53,7 @@ struct NormVariant {
 inline int norm_block(int lanes) { return lanes == 0 ? kNormBlock : lanes > 64 ? lanes : 256; }
 inline int norm_block_rows(int lanes) { return lanes == 0 ? 1 : norm_block(lanes) / lanes; }
 // x and stream in float32 or bf16; res: a residual is added
-NormVariant norm_kernel(int32_t H, bool x_f32, bool stream_f32, bool res);
+NormVariant norm_kernel(int32_t H, int64_t rows, bool x_f32, bool stream_f32, bool res);
 NormVariant norm_grad_kernel(int32_t H, bool dy_f32, bool x_f32);
 // Lanes to a row in the backward pass, a group of 8 elements each: a part of a wave, or whole waves. (0: in
 // passes. Of two groups to a lane, 3355 rows of 10000, the registers leave so few waves that they are no

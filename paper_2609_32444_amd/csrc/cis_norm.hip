@@ -275,55 +275,68 @@ __device__ __forceinline__ double lanes_sum(double x, double* sh) {
     return LANES == 16 ? x : x + __shfl_xor(x, 16, 64);
   }
 }
+// The same over a workgroup of any number of waves.
+__device__ __forceinline__ double waves_sum(double x, double* sh, int waves) {
+  x = wave_sum(x);
+  if ((threadIdx.x & 63) == 0) sh[threadIdx.x >> 6] = x;
+  __syncthreads();
+  const int w = threadIdx.x & 15;
+  return lanes_sum<16>(w < waves ? sh[w] : 0.0, nullptr);
+}
+// LANES = 0: over a workgroup.
 template <int LANES>
 __device__ __forceinline__ uint32_t row_max(uint32_t m, uint32_t* sh) {
   m = lanes_max(m, 16);
 #pragma unroll
-  for (int l = 16; l < 64 && l < LANES; l += l) {
+  for (int l = 16; l < 64 && (LANES == 0 || l < LANES); l += l) {
     const uint32_t o = __shfl_xor(m, l, 64);
     m = o > m ? o : m;
   }
-  if constexpr (LANES > 64) {
+  if constexpr (LANES == 0 || LANES > 64) {
     if ((threadIdx.x & 63) == 0) sh[threadIdx.x >> 6] = m;
     __syncthreads();
-    for (int w = 0; w < LANES / 64; ++w) m = sh[w] > m ? sh[w] : m;
+    const int w = threadIdx.x & 15;
+    m = lanes_max(w < (int)(blockDim.x >> 6) ? sh[w] : 0, 16);
   }
   return m;
 }
 
 // ------------------------------------------------------------------------------------------
-// LANES lanes to a row, which holds at most 8 * NV * LANES elements.
+// LANES lanes to a row, which holds at most 8 * NV * LANES elements; LANES = 0: a workgroup, of as many waves
+// as the row fills. Bound by the memory: 16384 rows of 2048 in 48 us (5.6 TB/s; a copy reaches 6.2), 8192 of
+// 8192 to e4m3 in 130 (5.7). Few rows are bound by the steps' latency, 3.6 us for one.
 // ------------------------------------------------------------------------------------------
 template <int LANES>
-constexpr int kRowBlock = LANES > 256 ? LANES : 256;   // threads of a workgroup
+constexpr int kRowBlock = LANES == 0 ? 1024 : LANES > 256 ? LANES : 256;   // threads of a workgroup (at most)
 template <class X, class S, bool RES, int LANES, int NV>
 __global__ __launch_bounds__(kRowBlock<LANES>) void cis_norm_row_kernel(const NormArgs a) {
-  constexpr int NW = LANES > 64 ? LANES / 64 : 1, R = kRowBlock<LANES> / LANES;
-  __shared__ double sh[NW];
-  __shared__ uint32_t shm[NW];
-  const int H = a.H, n8 = (H + 7) / 8;
+  constexpr bool WAVES = LANES == 0;
+  constexpr int R = WAVES ? 1 : kRowBlock<LANES> / (LANES + WAVES);
+  __shared__ double sh[16];
+  __shared__ uint32_t shm[16];
+  const int H = a.H, n8 = (H + 7) / 8, lanes = WAVES ? (int)blockDim.x : LANES;
   const int xv = (H + X::kPerVec - 1) / X::kPerVec, sv = (H + S::kPerVec - 1) / S::kPerVec;
-  const int l = threadIdx.x % LANES;
-  uint32_t at = threadIdx.x / LANES;
+  const int l = WAVES ? threadIdx.x : threadIdx.x % (LANES + WAVES);
+  uint32_t at = WAVES ? 0 : threadIdx.x / (LANES + WAVES);
   if (LANES >= 64) at = __builtin_amdgcn_readfirstlane(at);
   uint32_t row = a.row0 + blockIdx.x * R + at;
   const bool on = row < a.rows;
   if (!on) row = a.rows - 1;
-  constexpr bool WAVE = LANES >= 64;
+  constexpr bool WAVE = WAVES || LANES >= 64;
   const auto x = row_of<WAVE>(a.x, row, a.N, xv), r = row_of<WAVE>(RES ? a.r : a.x, row, a.N, sv);
   const auto y = row_of<WAVE>(a.y, row, a.N, vecs_of(a.ydt, H));
   Raw<X> rx[NV];
   Raw<S> rr[RES ? NV : 1];
   static_for<NV>([&](auto I) __attribute__((always_inline)) {
-    rx[I] = load_raw<X>(x, l + I * LANES);
-    if constexpr (RES) rr[I] = load_raw<S>(r, l + I * LANES);
+    rx[I] = load_raw<X>(x, l + I * lanes);
+    if constexpr (RES) rr[I] = load_raw<S>(r, l + I * lanes);
   });
   WeightRow<NV> w;
-  w.load(a.w, a.w_f32, l, LANES, H);
+  w.load(a.w, a.w_f32, l, lanes, H);
   float f[NV][8];
   double ss = 0.0;
   static_for<NV>([&](auto I) __attribute__((always_inline)) {
-    const int g = l + I * LANES;
+    const int g = l + I * lanes;
     unpack8<X>(rx[I], g, H, f[I]);
     if constexpr (RES) {
       float t[8];
@@ -335,11 +348,15 @@ __global__ __launch_bounds__(kRowBlock<LANES>) void cis_norm_row_kernel(const No
 #pragma unroll
     for (int e = 0; e < 8; ++e) ss = fma((double)f[I][e], (double)f[I][e], ss);
   });
-  const float rstd = rstd_of(lanes_sum<LANES>(ss, sh), 1.0 / (double)H, a.eps);
+  if constexpr (WAVES)
+    ss = waves_sum(ss, sh, lanes / 64);
+  else
+    ss = lanes_sum<LANES + WAVES>(ss, sh);
+  const float rstd = rstd_of(ss, 1.0 / (double)H, a.eps);
   if (RES && a.s.p && on) {   // (all of the row has been read)
     const auto s = row_of<WAVE>(a.s, row, a.N, sv);
     static_for<NV>([&](auto I) __attribute__((always_inline)) {
-      if (l + I * LANES < n8) store8<S>(s, l + I * LANES, H, f[I]);
+      if (l + I * lanes < n8) store8<S>(s, l + I * lanes, H, f[I]);
     });
   }
   static_for<NV>([&](auto I) __attribute__((always_inline)) {
@@ -353,26 +370,26 @@ __global__ __launch_bounds__(kRowBlock<LANES>) void cis_norm_row_kernel(const No
     if (a.group == 0) {
       uint32_t m = 0;
       static_for<NV>([&](auto I) __attribute__((always_inline)) {
-        const uint32_t b = l + I * LANES < n8 ? size_of8(f[I]) : 0;
+        const uint32_t b = l + I * lanes < n8 ? size_of8(f[I]) : 0;
         m = b > m ? b : m;
       });
       const float scale = e4m3_scale(row_max<LANES>(m, shm));
       if (l == 0 && on) a.scale[row] = scale;
       inv = 1.f / scale;
     }
-    const int lanes = a.group / 8;
+    const int per = a.group / 8;   // lanes of a block
     static_for<NV>([&](auto I) __attribute__((always_inline)) {
-      const int g = l + I * LANES;
+      const int g = l + I * lanes;
       if (a.group) {
-        const float scale = e4m3_scale(lanes_max(g < n8 ? size_of8(f[I]) : 0, lanes));
-        if (g < n8 && (g & (lanes - 1)) == 0 && on) a.scale[(int64_t)row * a.blocks + g / lanes] = scale;
+        const float scale = e4m3_scale(lanes_max(g < n8 ? size_of8(f[I]) : 0, per));
+        if (g < n8 && (g & (per - 1)) == 0 && on) a.scale[(int64_t)row * a.blocks + g / per] = scale;
         inv = 1.f / scale;
       }
       if (g < n8 && on) store_e4m3(y, g, H, f[I], inv);
     });
   } else if (on) {
     static_for<NV>([&](auto I) __attribute__((always_inline)) {
-      const int g = l + I * LANES;
+      const int g = l + I * lanes;
       if (g < n8) {
         if (a.ydt == CIS_F32)
           store8<F32>(y, g, H, f[I]);
@@ -384,10 +401,11 @@ __global__ __launch_bounds__(kRowBlock<LANES>) void cis_norm_row_kernel(const No
 }
 
 // The gradients, with rows that a workgroup's lanes take in turn and dweight's sums in registers; a
-// workgroup's are a part.
-//
-// Registers decide how many rows a compute unit has on their way: of 8 elements a thread 5 waves fit a SIMD,
-// so that a row of up to 8192 elements takes as many waves as it fills, not a power of two of them.
+// workgroup's are a part. 16384 rows of 2048 with a float32 dy in 57 us (4.7 TB/s; 3001 of 4100 in 30, 3.3):
+// bound by a row's chain of loads, sums and a barrier, and by how few rows the registers leave a compute
+// unit: 5 waves of a group of 8 elements to a lane fit a SIMD (two groups take twice the registers: 32 us
+// became 39), so that a row takes as many waves as it fills, not a power of two of them (49). The next row asked
+// for ahead costs a wave a SIMD and gains nothing (61, 39).
 template <class D, class X, int LANES>
 __global__ __launch_bounds__(LANES ? 256 : 1024) __attribute__((amdgpu_waves_per_eu(5)))
 void cis_norm_grad_row_kernel(const NormGradArgs a) {
@@ -409,10 +427,6 @@ void cis_norm_grad_row_kernel(const NormGradArgs a) {
   // (waited for here: else every row would wait for all that the row before it stored)
   opaque(w.lo);
   opaque(w.hi);
-  if (WAVES) {
-    if (threadIdx.x < 64) (&sh[0][0][0])[threadIdx.x] = 0.0;
-    __syncthreads();
-  }
   const double inv_h = 1.0 / (double)H;
   float acc[NV][8] = {};
   int turn = 0;
@@ -464,9 +478,9 @@ void cis_norm_grad_row_kernel(const NormGradArgs a) {
         sh[turn][1][threadIdx.x >> 6] = dot;
       }
       __syncthreads();
-      // (zeros behind the last wave's)
-      ss = lanes_sum<16>(sh[turn][0][threadIdx.x & 15], nullptr);
-      dot = lanes_sum<16>(sh[turn][1][threadIdx.x & 15], nullptr);
+      const int v = threadIdx.x & 15;
+      ss = lanes_sum<16>(v < lanes / 64 ? sh[turn][0][v] : 0.0, nullptr);
+      dot = lanes_sum<16>(v < lanes / 64 ? sh[turn][1][v] : 0.0, nullptr);
       turn ^= 1;   // (a wave may be a row ahead of another's reading)
     } else {
       ss = lanes_sum<LANES + WAVES>(ss, nullptr);
@@ -528,7 +542,8 @@ void cis_norm_grad_row_kernel(const NormGradArgs a) {
 }
 
 // ------------------------------------------------------------------------------------------
-// One workgroup per row, in passes over it.
+// One workgroup per row, in passes over it, which the caches serve: 1024 rows of 32768 elements and more. With
+// dweight a pass over the columns follows, which has 1677 rows of 20000 (float32 dy) in 36 us beside 77.
 // ------------------------------------------------------------------------------------------
 template <class X, class S, bool RES>
 __global__ __launch_bounds__(kNormBlock) void cis_norm_kernel(const NormArgs a) {
@@ -710,7 +725,7 @@ __global__ __launch_bounds__(kNormColumns) void cis_norm_part_kernel(const NormG
 }
 
 // dweight from the parts, in double: kNormReduceCols columns to a workgroup, the parts in turn over its
-// threads.
+// threads. 1280 parts of 2048 columns in 6 us, by latency (8.5 with 8 columns to a workgroup).
 __global__ __launch_bounds__(kNormReduce) void cis_norm_reduce_kernel(const NormGradArgs a) {
   constexpr int C = kNormReduceCols, P = kNormReduce / C;
   __shared__ double sh[P][C + 1];
@@ -748,12 +763,23 @@ NormVariant grad_variant(bool dy_f32, bool x_f32) {
 }
 }  // namespace
 
-// Rows of few elements share a wave; one wave to a row up to 2048 elements, then a workgroup. us for 16384
-// rows of 2048, 64 lanes of 4 groups 47.9, 256 of 1 48.6; for 8192 rows of 8192 with a float32 stream, to
-// e4m3, 256 lanes of 4 groups 129, 512 of 2 130, 1024 of 1 132. In passes they take 125 and 175.
-NormVariant norm_kernel(int32_t H, bool x_f32, bool stream_f32, bool res) {
+// Rows of up to 512 elements share a wave or have one; of more, few rows take as many waves as a row fills,
+// for the shortest chain, and many a wave or a workgroup of several groups to a lane, for more loads on their
+// way. us (bf16, with a residual) in waves and in groups:
+//   H = 640   256 rows 2.7, 3.0; 1024 3.2, 3.2; 4096 6.0, 5.7
+//   H = 2048  1 row 2.3, 3.5; 256 2.8, 4.0; 1024 4.4, 4.8; 4096 12.5, 11.4
+//   H = 4096  1 row 2.4, 2.6; 256 3.3, 3.4; 512 4.4, 4.4; 2048 12.9, 11.7
+//   H = 8192  1 row 3.1, 3.5; 512 7.1, 7.5; 1024 13.2, 12.1
+// Groups to a lane, 16384 rows of 2048: 64 lanes of 4 47.9, 256 of 1 48.6; 8192 rows of 8192 with a float32
+// stream, to e4m3: 256 lanes of 4 129, 512 of 2 130, 1024 of 1 132. In passes they take 125 and 175.
+NormVariant norm_kernel(int32_t H, int64_t rows, bool x_f32, bool stream_f32, bool res) {
   const int n8 = (H + 7) / 8;
 #define CIS_NORM(L, V) return row_variant<L, V>(x_f32, stream_f32, res)
+  if (n8 > 64 && n8 <= 1024 && rows <= 512) {
+    NormVariant v = row_variant<0, 1>(x_f32, stream_f32, res);
+    v.lanes = (n8 + 63) / 64 * 64;
+    return v;
+  }
   if (n8 <= 16) CIS_NORM(16, 1);
   if (n8 <= 32) CIS_NORM(32, 1);
   if (n8 <= 64) CIS_NORM(64, 1);

@@ -171,7 +171,7 @@ int cis_rms_norm_fwd(int64_t T, int64_t N, int64_t H, const cis_rows_t* x,
   a.group = (int32_t)group;
   a.blocks = (int32_t)blocks;
   a.scale = e4m3 ? scale_out : nullptr;
-  const cis::NormVariant v = cis::norm_kernel((int32_t)H, x->dtype == CIS_F32,
+  const cis::NormVariant v = cis::norm_kernel((int32_t)H, rows, x->dtype == CIS_F32,
                                               residual && residual->dtype == CIS_F32,
                                               residual != nullptr);
   const int64_t per = cis::norm_block_rows(v.lanes), most = kMaxBlocks * per;
