@@ -128,6 +128,24 @@ def test_e4m3_sizes(H, group):
     _check_fwd(x, w, r, out, 1e-5, group)
 
 
+@pytest.mark.parametrize("T", [512, 513, 1100])
+@pytest.mark.parametrize("H", [513, 1000, 1024, 1025, 2040, 2048, 2049, 4095, 4096, 4097, 5120, 8191,
+                               8192, 8193])
+def test_sizes_of_many_rows(H, T):
+    """Either side of the count of rows from which a lane takes several groups, every type."""
+    w = _rand((H,), F32, 3).contiguous()
+    for i, (xt, rt) in enumerate(TYPES):
+        x = _rand((T, H), xt, H + i)
+        r = None if rt is None else _rand((T, H), rt, H + 50 + i, 3.0)
+        out_dtype, group = [(BF, 0), (F8, 0), (F32, 0), (F8, 128), (F8, 32)][i]
+        out = cis.rms_norm(x, w, r, eps=1e-6, out_dtype=out_dtype, group=group)
+        rows = torch.cat([torch.arange(8), torch.arange(T - 8, T), torch.randint(0, T, (40,))])
+        some = {k: v[rows] for k, v in out.items()}
+        _check_fwd(x[rows], w, None if r is None else r[rows], some, 1e-6, group)
+        if r is not None:
+            assert torch.equal(out["residual"], (x.float() + r.float()).to(rt))
+
+
 @pytest.mark.parametrize("T", [1, 2, 3, 63, 64, 65, 1000, 5000, 20011])
 @pytest.mark.parametrize("H", [64, 640, 2048])
 def test_row_counts(T, H):
