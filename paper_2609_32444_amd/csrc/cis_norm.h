@@ -61,7 +61,7 @@ NormVariant norm_grad_kernel(int32_t H, bool dy_f32, bool x_f32);
 inline int norm_grad_lanes(int32_t H) {
   const int n8 = (H + 7) / 8;
   if (H > kNormGradResident) return 0;
-  return n8 <= 16 ? 16 : n8 <= 32 ? 32 : (n8 + 63) / 64 * 64;
+  return n8 <= 4 ? 4 : n8 <= 8 ? 8 : n8 <= 16 ? 16 : n8 <= 32 ? 32 : (n8 + 63) / 64 * 64;
 }
 const void* norm_rstd_kernel(bool x_f32);
 const void* norm_part_kernel(bool dy_f32, bool x_f32);

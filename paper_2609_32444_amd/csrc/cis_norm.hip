@@ -271,8 +271,12 @@ __device__ __forceinline__ double lanes_sum(double x, double* sh) {
       return __builtin_bit_cast(double, ((u64)dpp_word<C>((uint32_t)(b >> 32)) << 32) |
                                             dpp_word<C>((uint32_t)b));
     };
-    x = wave_reduce(x, step);
-    return LANES == 16 ? x : x + __shfl_xor(x, 16, 64);
+    x += step(x, std::integral_constant<int, kDppXor1>{});
+    x += step(x, std::integral_constant<int, kDppXor2>{});
+    if constexpr (LANES >= 8) x += step(x, std::integral_constant<int, kDppHalfMirror>{});
+    if constexpr (LANES >= 16) x += step(x, std::integral_constant<int, kDppRowMirror>{});
+    if constexpr (LANES >= 32) x += __shfl_xor(x, 16, 64);
+    return x;
   }
 }
 // The same over a workgroup of any number of waves.
@@ -286,7 +290,7 @@ __device__ __forceinline__ double waves_sum(double x, double* sh, int waves) {
 // LANES = 0: over a workgroup.
 template <int LANES>
 __device__ __forceinline__ uint32_t row_max(uint32_t m, uint32_t* sh) {
-  m = lanes_max(m, 16);
+  m = lanes_max(m, LANES == 0 || LANES > 16 ? 16 : LANES);
 #pragma unroll
   for (int l = 16; l < 64 && (LANES == 0 || l < LANES); l += l) {
     const uint32_t o = __shfl_xor(m, l, 64);
@@ -377,12 +381,13 @@ __global__ __launch_bounds__(kRowBlock<LANES>) void cis_norm_row_kernel(const No
       if (l == 0 && on) a.scale[row] = scale;
       inv = 1.f / scale;
     }
-    const int per = a.group / 8;   // lanes of a block
+    // lanes of a block (or of a row that is shorter)
+    const int per = lanes < a.group / 8 ? lanes : a.group / 8;
     static_for<NV>([&](auto I) __attribute__((always_inline)) {
       const int g = l + I * lanes;
       if (a.group) {
         const float scale = e4m3_scale(lanes_max(g < n8 ? size_of8(f[I]) : 0, per));
-        if (g < n8 && (g & (per - 1)) == 0 && on) a.scale[(int64_t)row * a.blocks + g / per] = scale;
+        if (g < n8 && (g & (per - 1)) == 0 && on) a.scale[(int64_t)row * a.blocks + g / (a.group / 8)] = scale;
         inv = 1.f / scale;
       }
       if (g < n8 && on) store_e4m3(y, g, H, f[I], inv);
@@ -401,13 +406,13 @@ __global__ __launch_bounds__(kRowBlock<LANES>) void cis_norm_row_kernel(const No
 }
 
 // The gradients, with rows that a workgroup's lanes take in turn and dweight's sums in registers; a
-// workgroup's are a part. 16384 rows of 2048 with a float32 dy in 57 us (4.7 TB/s; 3001 of 4100 in 30, 3.3):
+// workgroup's are a part. 16384 rows of 2048 with a float32 dy in 57 us (4.7 TB/s; 3001 of 4100 in 30, 3.3 TB/s):
 // bound by a row's chain of loads, sums and a barrier, and by how few rows the registers leave a compute
-// unit: 5 waves of a group of 8 elements to a lane fit a SIMD (two groups take twice the registers: 32 us
-// became 39), so that a row takes as many waves as it fills, not a power of two of them (49). The next row asked
-// for ahead costs a wave a SIMD and gains nothing (61, 39).
+// unit: 6 waves of a group of 8 elements to a lane fit a SIMD (with 84 registers 5, which leaves a compute unit one
+// row of 9 waves for two: 38 us for 30; two groups to a lane 39), so that a row takes as many waves as it fills,
+// not a power of two of them (49). The next row asked for ahead costs a wave a SIMD and gains nothing (61, 39).
 template <class D, class X, int LANES>
-__global__ __launch_bounds__(LANES ? 256 : 1024) __attribute__((amdgpu_waves_per_eu(5)))
+__global__ __launch_bounds__(LANES ? 256 : 1024) __attribute__((amdgpu_waves_per_eu(6)))
 void cis_norm_grad_row_kernel(const NormGradArgs a) {
   constexpr bool WAVES = LANES == 0;   // a workgroup of any number of waves to a row
   constexpr int NV = 1;                // groups to a lane
@@ -763,7 +768,8 @@ NormVariant grad_variant(bool dy_f32, bool x_f32) {
 }
 }  // namespace
 
-// Rows of up to 512 elements share a wave or have one; of more, few rows take as many waves as a row fills,
+// Rows of up to 512 elements share a wave, of 4 lanes and more, or have one (524288 rows of 64 in 40 us with 8
+// lanes, 50 with 16); of more, few rows take as many waves as a row fills,
 // for the shortest chain, and many a wave or a workgroup of several groups to a lane, for more loads on their
 // way. us (bf16, with a residual) in waves and in groups:
 //   H = 640   256 rows 2.7, 3.0; 1024 3.2, 3.2; 4096 6.0, 5.7
@@ -780,6 +786,8 @@ NormVariant norm_kernel(int32_t H, int64_t rows, bool x_f32, bool stream_f32, bo
     v.lanes = (n8 + 63) / 64 * 64;
     return v;
   }
+  if (n8 <= 4) CIS_NORM(4, 1);
+  if (n8 <= 8) CIS_NORM(8, 1);
   if (n8 <= 16) CIS_NORM(16, 1);
   if (n8 <= 32) CIS_NORM(32, 1);
   if (n8 <= 64) CIS_NORM(64, 1);
@@ -800,7 +808,11 @@ NormVariant norm_kernel(int32_t H, int64_t rows, bool x_f32, bool stream_f32, bo
 NormVariant norm_grad_kernel(int32_t H, bool dy_f32, bool x_f32) {
   const int lanes = norm_grad_lanes(H);
   NormVariant v{};
-  if (lanes == 16)
+  if (lanes == 4)
+    v = grad_variant<4>(dy_f32, x_f32);
+  else if (lanes == 8)
+    v = grad_variant<8>(dy_f32, x_f32);
+  else if (lanes == 16)
     v = grad_variant<16>(dy_f32, x_f32);
   else if (lanes == 32)
     v = grad_variant<32>(dy_f32, x_f32);

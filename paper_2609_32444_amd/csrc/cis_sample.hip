@@ -2,8 +2,8 @@
 //
 // A row is drawn from the scan (TokScan) in one of five ways, by what its cuts keep at most:
 //   * greedy rows, and top_k = 1: the first of the largest logits.
-//   * top_k up to kDrawK: the candidates that RowSelect collects, put in order; the
-//     cuts and the draw run on that list.
+//   * top_k up to kDrawK: the candidates that RowSelect collects, put in order; the cuts and the draw
+//     run on that list.
 //   * nothing but min_p cuts: the weights' sums by chunks (cis_weigh_kernel), the chunk that the
 //     random number falls into, and the token within it.
 //   * top_p without a count: a histogram of the weights over the whole row (cis_hist_kernel) gives the
@@ -40,8 +40,8 @@ __device__ __forceinline__ RowParams row_params(const SampleArgs& a, int64_t row
   const int k = a.top_k ? sload(a.top_k + at) : a.prm.top_k;
   p.top_p = a.top_p ? sload(a.top_p + at) : a.prm.top_p;
   p.min_p = a.min_p ? sload(a.min_p + at) : a.prm.min_p;
-  p.ok = (KEEP ? tok_seq_on(a.r, row) : tok_on(a.r, row)) && p.u >= 0.f && p.u < 1.f && p.temp >= 0.f && p.temp < INFINITY &&
-         k >= 0 && p.top_p > 0.f && p.top_p <= 1.f && p.min_p >= 0.f && p.min_p <= 1.f;
+  p.ok = (KEEP ? tok_seq_on(a.r, row) : tok_on(a.r, row)) && p.u >= 0.f && p.u < 1.f &&
+         p.temp >= 0.f && p.temp < INFINITY && k >= 0 && p.top_p > 0.f && p.top_p <= 1.f && p.min_p >= 0.f && p.min_p <= 1.f;
   p.c = kLog2e / p.temp;
   const bool greedy = !(p.c < INFINITY);
   p.top_k = greedy ? 1 : k == 0 || k >= a.r.V ? a.r.V : k;
@@ -225,21 +225,21 @@ __global__ __launch_bounds__(kWeighBlock) void cis_weigh_kernel(const SampleArgs
       uint32_t in[2] = {0, 0};
       // (without a min_p two instructions a logit less; with STEP that does not pay)
       auto add_up = [&](auto min_p) __attribute__((always_inline)) {
-      static_for<kScanSlots>([&](auto I) {
-        float f[EPV];
-        E::unpack(x[I], f);
-        uint32_t vs = 0;   // (8 weights stay below 2^32)
+        static_for<kScanSlots>([&](auto I) {
+          float f[EPV];
+          E::unpack(x[I], f);
+          uint32_t vs = 0;   // (8 weights stay below 2^32)
 #pragma unroll
-        for (int e = 0; e < EPV; ++e) {
-          const float t = draw_exponent(f[e], M, p.c);
-          const uint32_t q = exponent_weight(t);
-          if (STEP) in[I / 4] = in[I / 4] * 2 + (t > within && t <= above ? 1 : 0);
-          vs += (!STEP || t > above) && (!min_p || q >= p.least_w) ? q : 0u;
-        }
-        s += vs;
-        if (STEP) asm volatile("" : "+v"(in[I / 4]));   // (else all vectors are unpacked first)
-        slot_fence();
-      });
+          for (int e = 0; e < EPV; ++e) {
+            const float t = draw_exponent(f[e], M, p.c);
+            const uint32_t q = exponent_weight(t);
+            if (STEP) in[I / 4] = in[I / 4] * 2 + (t > within && t <= above ? 1 : 0);
+            vs += (!STEP || t > above) && (!min_p || q >= p.least_w) ? q : 0u;
+          }
+          s += vs;
+          if (STEP) asm volatile("" : "+v"(in[I / 4]));   // (else all vectors are unpacked first)
+          slot_fence();
+        });
       };
       if (STEP || p.least_w > 0)
         add_up(std::true_type{});

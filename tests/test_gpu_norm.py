@@ -95,7 +95,7 @@ def _check_fwd(x, w, r, out, eps, group=0):
 
 
 # lengths at and beside those where a kernel's shape changes, odd ones and the smallest
-SIZES = [1, 2, 7, 8, 9, 15, 64, 79, 127, 128, 129, 250, 256, 257, 391, 511, 512, 513, 1000, 1023,
+SIZES = [1, 2, 7, 8, 9, 15, 31, 32, 33, 40, 63, 64, 65, 79, 127, 128, 129, 250, 256, 257, 391, 511, 512, 513, 1000, 1023,
          1024, 1025, 2040, 2048, 2049, 4095, 4096, 4097, 5120, 8191, 8192, 8193, 16383, 16384, 16385,
          32768, 32769, 50001]
 TYPES = [(BF, None), (F32, None), (BF, BF), (BF, F32), (F32, F32)]
