@@ -35,7 +35,7 @@ struct View {
   bool given() const { return m.p != nullptr; }
 };
 int check_strides(const cis_rows_t& r, const Shape& s) {
-  const int64_t most = INT64_MAX / 8;   // an address's offset fits 64 bits
+  const int64_t most = INT64_MAX / 16;   // an address's offset fits 64 bits
   if ((s.T > 1 && (r.stride_t < 0 || r.stride_t > most / s.T)) ||
       (s.N > 1 && (r.stride_n < 0 || r.stride_n > most / s.N)))
     return CIS_ERR_SHAPE;

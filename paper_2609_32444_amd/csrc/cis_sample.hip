@@ -40,7 +40,12 @@ __device__ __forceinline__ RowParams row_params(const SampleArgs& a, int64_t row
   const int k = a.top_k ? sload(a.top_k + at) : a.prm.top_k;
   p.top_p = a.top_p ? sload(a.top_p + at) : a.prm.top_p;
   p.min_p = a.min_p ? sload(a.min_p + at) : a.prm.min_p;
-  p.ok = (KEEP ? tok_seq_on(a.r, row) : tok_on(a.r, row)) && p.u >= 0.f && p.u < 1.f &&
+  bool on;
+  if constexpr (KEEP)
+    on = tok_seq_on(a.r, row) && (!a.need || sload_byte(a.need, row) != 0);
+  else
+    on = tok_on(a.r, row);
+  p.ok = on && p.u >= 0.f && p.u < 1.f &&
          p.temp >= 0.f && p.temp < INFINITY && k >= 0 && p.top_p > 0.f && p.top_p <= 1.f && p.min_p >= 0.f && p.min_p <= 1.f;
   p.c = kLog2e / p.temp;
   const bool greedy = !(p.c < INFINITY);

@@ -114,6 +114,7 @@ struct SampleArgs {
   float* logp;                // nullable
   float* logp_kept;           // nullable
   RowKept* kept;              // verification: [T]; else null
+  const uint8_t* need;        // verification: [T] rows that are looked at; null: all
 };
 
 // Where a sequence's token is drawn in place of a draft.
@@ -126,7 +127,10 @@ struct VerifyArgs {
   const float* cmax;          // [T, nch] of the scan
   int32_t nch;
   int32_t nsub, parts;        // pieces of kLeftVecs vectors in a row; workgroups of a sequence
+  const double* csum;         // of the scan
   const RowKept* kept;        // [T]
+  uint8_t* verdict;           // [T1] what the scan's sums decide (Verdict); null: not looked at
+  uint8_t* need;              // [T] as in SampleArgs
   const int64_t* draft_ids;
   int64_t D;
   const float* u;
@@ -199,6 +203,8 @@ struct DrawKernels {
 DrawKernels draw_kernels(int dtype, bool wide, bool step, bool keep);
 constexpr int kVerifyBlock = 256;
 constexpr int kLeftVecs = 128;   // vectors of a piece (a wave's)
+enum Verdict : uint8_t { kOpen = 0, kAccepted = 1, kTurnedDown = 2 };
+const void* verdict_kernel(int dtype);
 const void* verify_kernel(int dtype);
 const void* verify_draw_kernel(int dtype);
 const void* top_kernel(int dtype, int64_t K);

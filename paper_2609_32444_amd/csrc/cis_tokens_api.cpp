@@ -298,6 +298,7 @@ struct DrawCall {
   int64_t* ids;
   float *logp, *logp_kept;
   cis::RowKept* kept;
+  cis::VerifyArgs* judged;   // verification: what the scan's sums decide is looked at ahead; else null
 };
 size_t draw_bytes(int64_t T, int64_t V, int dtype) {
   // (the shape of the scan goes by the call's parameters: the larger of its two)
@@ -313,8 +314,8 @@ bool sample_params_ok(const cis_sample_params_t& p, const float* temperature, co
   if (!top_p && !(p.top_p > 0.f && p.top_p <= 1.f)) return false;
   return min_p || (p.min_p >= 0.f && p.min_p <= 1.f);
 }
-// cmax: where to leave the chunks' largest logits.
-int run_draws(const DrawCall& c, char* base, hipStream_t stream, const float** cmax = nullptr) {
+// scan: where to leave the scan's place.
+int run_draws(const DrawCall& c, char* base, hipStream_t stream, cis::TokScan* scan = nullptr) {
   const cis_sample_params_t& p = c.p;
   const cis::TokRows& r = c.r;
   const int64_t T = r.T, V = r.V;
@@ -335,8 +336,20 @@ int run_draws(const DrawCall& c, char* base, hipStream_t stream, const float** c
                                        lists ? cis::scan_group(r.nvec, counted ? k : kManyLogits)
                                              : 0);
   const cis::TokScan s = scan_at(base, L.scan);
-  if (cmax) *cmax = s.cmax;
+  if (scan) *scan = s;
   if (int rc = launch_scan(r, s, dtype, cis::scan_c(1.f), stream)) return rc;
+  if (c.judged) {
+    cis::VerifyArgs& v = *c.judged;
+    v.cmax = s.cmax;
+    v.csum = s.csum;
+    v.nch = s.nch;
+    for (v.seq0 = 0; v.seq0 < r.n_seq; v.seq0 += kMaxBlocks)
+      if (int rc = launch(cis::verdict_kernel(dtype),
+                          r.n_seq - v.seq0 < kMaxBlocks ? r.n_seq - v.seq0 : kMaxBlocks,
+                          cis::kVerifyBlock, &v, stream))
+        return rc;
+    v.seq0 = 0;
+  }
   cis::SampleArgs a{};
   a.r = r;
   a.s = s;
@@ -357,6 +370,7 @@ int run_draws(const DrawCall& c, char* base, hipStream_t stream, const float** c
   a.logp = c.logp;
   a.logp_kept = c.logp_kept;
   a.kept = c.kept;
+  a.need = c.judged ? c.judged->need : nullptr;
   const cis::DrawKernels fn = cis::draw_kernels(dtype, wide, stepped, c.kept != nullptr);
   const int block = wide ? cis::kTokBlock : cis::kTopBlock;
   const int64_t most = stepped ? kStepRows : kMaxRows;
@@ -385,8 +399,13 @@ int run_draws(const DrawCall& c, char* base, hipStream_t stream, const float** c
 constexpr int64_t kMaxVerify = int64_t(1) << 31;
 // Workgroups of cis_verify_kernel beyond which a wave takes several pieces.
 constexpr int64_t kVerifyBlocks = 8192;
+// Logits, in bytes, from which it pays to look at what the scan's sums decide: a launch more for fewer rows that
+// have to be weighed. us with and without, sequences of 4 drafts, bf16:
+//   V = 32768   32 sequences (18 MiB) 39, 35; 128 (72 MiB) 57, 56
+//   V = 151936  1 (2.6 MiB) 31, 27; 16 (42 MiB) 47, 46; 32 (84 MiB) 59, 65; 64 (167 MiB) 89, 97; 128 150, 165
+constexpr int64_t kJudgeBytes = int64_t(80) << 20;
 struct VerifyLayout {
-  size_t kept, stops, left, total;
+  size_t kept, stops, left, verdict, need, total;
 };
 VerifyLayout verify_layout(int64_t T, int64_t D, int64_t n_seq, int64_t V, int dtype) {
   VerifyLayout L{};
@@ -394,7 +413,9 @@ VerifyLayout verify_layout(int64_t T, int64_t D, int64_t n_seq, int64_t V, int d
   L.kept = cis::align_up(draw_bytes(T + D, V, dtype), 256);
   L.stops = L.kept + cis::align_up((size_t)(T + D) * sizeof(cis::RowKept), 256);
   L.left = L.stops + cis::align_up((size_t)n_seq * sizeof(cis::VerifyStop), 256);
-  L.total = L.left + cis::align_up((size_t)n_seq * nsub * 8, 256);
+  L.verdict = L.left + cis::align_up((size_t)n_seq * nsub * 8, 256);
+  L.need = L.verdict + cis::align_up((size_t)T, 256);
+  L.total = L.need + cis::align_up((size_t)(T + D), 256);
   if (L.total < 256) L.total = 256;
   return L;
 }
@@ -558,10 +579,7 @@ int cis_verify(const void* logits, int dtype, int64_t T, int64_t V, int64_t ld,
   c.logp_kept = logp_kept_out;
   c.kept = reinterpret_cast<cis::RowKept*>(base + L.kept);
   cis::VerifyArgs a{};
-  if (c.r.T > 0)
-    if (int rc = run_draws(c, base, stream, &a.cmax)) return rc;
   a.r = c.r;
-  a.nch = (c.r.nvec + cis::kScanVecs - 1) / cis::kScanVecs;
   a.kept = c.kept;
   a.draft_ids = draft_ids;
   a.D = D;
@@ -572,6 +590,20 @@ int cis_verify(const void* logits, int dtype, int64_t T, int64_t V, int64_t ld,
   a.accepted = accepted_out;
   a.logp = logp_out;
   a.logp_kept = logp_kept_out;
+  // the scan's sums say something of uncut rows at temperature 1
+  const bool uncut = !temperature && params->temperature == 1.f && !top_k &&
+                     (params->top_k == 0 || params->top_k >= V) && !top_p && params->top_p == 1.f &&
+                     !min_p && params->min_p == 0.f;
+  if (uncut && D > 0 && c.r.T * c.r.row_bytes >= kJudgeBytes) {
+    a.verdict = reinterpret_cast<uint8_t*>(base + L.verdict);
+    a.need = reinterpret_cast<uint8_t*>(base + L.need);
+    c.judged = &a;
+  }
+  cis::TokScan scan{};
+  if (c.r.T > 0)
+    if (int rc = run_draws(c, base, stream, &scan)) return rc;
+  a.cmax = scan.cmax;
+  a.nch = (c.r.nvec + cis::kScanVecs - 1) / cis::kScanVecs;
   a.nsub = (c.r.nvec + cis::kLeftVecs - 1) / cis::kLeftVecs;
   const int64_t per = cis::kVerifyBlock / 64, most = (a.nsub + per - 1) / per,
                 fill = (kVerifyBlocks + n_seq - 1) / n_seq;

@@ -114,6 +114,73 @@ struct Leftover {
 };
 
 // ------------------------------------------------------------------------------------------
+// What the scan's sums decide of uncut rows at temperature 1, by one workgroup per sequence: drafts that are
+// surely accepted or surely turned down, and so which rows have to be looked at: those of the target up
+// to the first that is surely turned down, and the drafts' up to there that are not surely accepted.
+//
+// The scan's S = sum of exp(z - M) is within 2^-16 of what its float32 exponents (28 * 2^-24 and less where
+// a weight is not 0), exp2 and sums of 8 add up to, and a token's weight is below 2^28 exp(z - M) by less than
+// 1, so that N lies in [2^28 S (1 - 2^-16) - V, 2^28 S (1 + 2^-16)]. What holds for both ends of N and N', with
+// 2^-40 for the comparison's own roundings, holds for what they are; all else stays open. A row with a NaN or
+// an infinity, or without a token, has a NaN sum, and nothing that is compared with it holds.
+// ------------------------------------------------------------------------------------------
+struct SumRange {
+  float M;
+  double lo, hi;
+};
+__device__ __forceinline__ SumRange sum_range(const VerifyArgs& a, int64_t row, int lane) {
+  const float* cmax = a.cmax + row * a.nch;
+  const double* csum = a.csum + row * a.nch;
+  float M = -INFINITY;
+  for (int i = lane; i < a.nch; i += 64) M = fmaxf(M, cmax[i]);
+  M = wave_max(M);
+  double S = 0.0;
+  for (int i = lane; i < a.nch; i += 64)
+    S += csum[i] * (double)fast_exp2((cmax[i] - M) * kLog2e);
+  S = wave_sum(S) * (double)kDrawOne;
+  return SumRange{M, S * (1 - 0x1p-16) - (double)a.r.V, S * (1 + 0x1p-16)};
+}
+template <class E>
+__global__ __launch_bounds__(kVerifyBlock) void cis_verdict_kernel(const VerifyArgs a) {
+  constexpr int NW = kVerifyBlock / 64;
+  __shared__ int64_t first[NW];
+  const int lane = threadIdx.x & 63, wid = __builtin_amdgcn_readfirstlane(threadIdx.x) >> 6;
+  const int64_t seq = a.seq0 + blockIdx.x, T = a.r.T1;
+  const int64_t o0 = sload(a.r.offsets + seq), o1 = sload(a.r.offsets + seq + 1);
+  if (o0 < 0 || o1 <= o0 || o1 > T || (o1 > o0 + 1 && (o0 < seq || o1 - 1 - seq > a.D))) return;
+  int64_t stop = o1;   // the first row whose draft is surely turned down
+  for (int64_t row = o0 + wid; row < o1 - 1; row += NW) {
+    const int64_t id = sload(a.draft_ids + row - seq);
+    const float u = sload(a.u + row);
+    uint8_t v = kOpen;
+    if (id >= 0 && id < a.r.V && u >= 0.f && u < 1.f) {
+      const SumRange p = sum_range(a, row, lane);
+      const double w = (double)draw_weight(lane_elem<E>(a.r.logits, a.r.row_bytes, row, (int)id), p.M, kLog2e);
+      double most = p.hi, least = p.lo;   // of what u is multiplied by
+      if (a.r.draft) {
+        const SumRange q = sum_range(a, T + row - seq, lane);
+        const double wq = (double)draw_weight(
+            lane_elem<E>(a.r.draft, a.r.draft_bytes, row - seq, (int)id), q.M, kLog2e);
+        most = q.lo > 0.0 ? wq * (p.hi / q.lo) : INFINITY;
+        least = wq * (p.lo / q.hi);
+      }
+      if ((double)u * most * (1 + 0x1p-40) < w) v = kAccepted;
+      if (least > 0.0 && (double)u * least * (1 - 0x1p-40) >= w) v = kTurnedDown;
+    }
+    if (lane == 0) a.verdict[row] = v;
+    if (v == kTurnedDown && row < stop) stop = row;
+  }
+  if (lane == 0) first[wid] = stop;
+  __syncthreads();
+#pragma unroll
+  for (int k = 0; k < NW; ++k) stop = first[k] < stop ? first[k] : stop;
+  for (int64_t row = o0 + threadIdx.x; row < o1; row += kVerifyBlock) {
+    a.need[row] = row <= stop;
+    if (row < o1 - 1 && a.r.draft) a.need[T + row - seq] = row <= stop && a.verdict[row] != kAccepted;
+  }
+}
+
+// ------------------------------------------------------------------------------------------
 // A sequence's drafts, a lane to a row, up to the first that is turned down, by the first wave of each of
 // its workgroups (of which one writes); then the weights that are left of its row, a piece to a wave: some 30
 // instructions a token, two exp2 and a product in double among them. Bound by the latency of both steps: 13 us
@@ -148,9 +215,15 @@ __device__ __forceinline__ VerifyStop judge(const VerifyArgs& a, int64_t seq, bo
       id = a.draft_ids[row - seq];
       u = a.u[row];
     }
+    const uint8_t verdict = drafted && a.verdict ? a.verdict[row] : kOpen;
     if (k.id >= 0 && !drafted) {   // after the last draft
       what = kTake;
       d = k.id;
+    } else if (verdict != kOpen) {
+      d = (int)id;
+      f = lane_elem<E>(a.r.logits, a.r.row_bytes, row, d);
+      w = kept_weight(k, f, d);
+      what = verdict == kAccepted ? kTake : kDraw;
     } else if (k.id >= 0 && id >= 0 && id < a.r.V) {
       d = (int)id;
       f = lane_elem<E>(a.r.logits, a.r.row_bytes, row, d);
@@ -297,6 +370,10 @@ __global__ __launch_bounds__(kVerifyBlock) void cis_verify_draw_kernel(const Ver
   }
 }
 
+const void* verdict_kernel(int dtype) {
+  return dtype == CIS_BF16 ? (const void*)&cis_verdict_kernel<Bf16>
+                           : (const void*)&cis_verdict_kernel<F32>;
+}
 const void* verify_kernel(int dtype) {
   return dtype == CIS_BF16 ? (const void*)&cis_verify_kernel<Bf16>
                            : (const void*)&cis_verify_kernel<F32>;

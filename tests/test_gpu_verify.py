@@ -226,6 +226,68 @@ def test_many_sequences_and_settings_of_their_own():
     _check(*batch, out, s, only=[b for b in range(B) if b not in bad])
 
 
+def _same_as_settings_of_their_own(batch):
+    """A temperature of 1 per sequence takes the kernels that weigh every row; one for all, over as many
+    logits as here, those that look at what the scan's sums decide first. Every output is the same."""
+    ones = torch.ones(len(batch[3]) - 1, device=DEV)
+    a, b = _run(*batch, {}), _run(*batch, dict(temperature=ones))
+    for k in ("ids", "accepted", "logp", "logp_kept"):
+        assert torch.equal(a[k], b[k]), k
+    return a
+
+
+@pytest.mark.parametrize("kind", ["normal", "peaked", "banned"])
+@pytest.mark.parametrize("near", [0.0, 0.02, 0.7, 4.0])
+def test_drafts_that_the_sums_decide(near, kind):
+    """At temperature 1 with nothing cut, over more than 80 MiB of logits: drafts from the target itself, from close
+    to it (where many a random number is near its border) and from far away."""
+    batch = _batch([5, 7, 1, 4, 2, 9, 3, 70, 6], 300001, int(10 * near), F32, kind, near=near)
+    out = _same_as_settings_of_their_own(batch)
+    if near == 0.0:
+        assert out["accepted"].tolist() == [4, 6, 0, 3, 1, 8, 2, 69, 5]
+    _check(*batch, out, {}, only=[0, 3, 4])
+    # random numbers at the very border of the first draft's acceptance, and one step beside it
+    logits, ids, u, offsets, q = batch
+    P, Q = _row_weights(logits[0], {}), _row_weights(q[0], {})
+    share = float(Q[ids[0]]) * (float(int(P.sum())) / float(int(Q.sum())))
+    edge = np.float32(min(float(P[ids[0]]) / share, 1 - 2.0 ** -24))
+    for x in (edge, np.nextafter(edge, np.float32(0)), np.nextafter(edge, np.float32(1))):
+        u[0] = float(min(x, np.float32(1 - 2.0 ** -24)))
+        _check(*batch, _same_as_settings_of_their_own(batch), {}, only=[0])
+
+
+@pytest.mark.parametrize("dtype,V,n", [(BF, 151936, 64), (F32, 32768, 200), (BF, 50257, 300)])
+def test_decided_batches(dtype, V, n):
+    for certain in (False, True):
+        g = _gen(V + certain)
+        lengths = torch.randint(1, 8 if not certain else 14, (n,), generator=g, device=DEV).tolist()
+        _same_as_settings_of_their_own(_batch(lengths, V, n, dtype, "peaked", certain=certain))
+
+
+def test_unusable_rows_among_decided_ones():
+    V = 300001
+    lengths = [5] * 9
+    logits, ids, u, offsets, q = _batch(lengths, V, 2, F32, near=0.0)
+    logits[offsets[1] + 1, 7] = math.nan
+    logits[offsets[2] + 4, 8] = math.inf
+    q[offsets[3] - 3 + 2, V - 1] = math.nan
+    q[offsets[4] - 4] = -math.inf
+    ids[offsets[5] - 5 + 1], ids[offsets[6] - 6] = V, -1
+    u[offsets[7] + 1], u[offsets[8] + 4] = math.nan, 1.0
+    batch = (logits, ids, u, offsets, q)
+    out = _same_as_settings_of_their_own(batch)
+    assert out["accepted"].tolist() == [4, 1, 4, 2, 0, 1, 0, 1, 4]
+    _check(*batch, out, {}, only=[1, 3, 4, 5, 7, 8])
+    # a draft that is surely turned down ahead of rows that cannot be used, which nobody looks at
+    for b in (1, 3, 5):
+        ids[offsets[b] - b] = int(logits[offsets[b]].argmin())
+        u[offsets[b]] = 0.999
+        q[offsets[b] - b, ids[offsets[b] - b]] = 40.0
+    out = _same_as_settings_of_their_own(batch)
+    assert out["accepted"].tolist() == [4, 0, 4, 0, 0, 0, 0, 1, 4]
+    _check(*batch, out, {}, only=[1, 3, 5])
+
+
 def test_a_sequence_of_one_row_is_a_draw():
     V, T = 5000, 40
     logits = _store(_logits(T, V, 1), BF)
