@@ -38,7 +38,8 @@ extern "C" {
  *
  *   ids        the accepted drafts and the drawn token; -1 for the sequence's other rows, and for rows
  *              that no sequence has
- *   accepted   how many drafts were accepted (-1: the sequence's offsets are out of range)
+ *   accepted   how many drafts were accepted (-1: the sequence's offsets are out of range; where offsets fall,
+ *              the others that share its rows are undefined)
  *   logp       log softmax of the target's row at its token, at temperature 1: what the loss entry
  *              points take as logp_infer
  *   logp_kept  log(P_y / N)
