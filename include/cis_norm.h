@@ -44,8 +44,8 @@ typedef struct cis_rows {
  *
  *   scale = max(max |y| / 448, 2^-126),   values e4m3(y / scale)
  *
- * so that y is about value * scale. The quotient is formed in float32 as y * (1 / scale) and rounded to
- * nearest, ties to even. A block with a NaN has a NaN scale and its NaN; with an infinity an infinite
+ * so that y is about value * scale. The quotient is rounded to float32, and that to the nearest value, ties
+ * to even. A block with a NaN has a NaN scale and its NaN; with an infinity an infinite
  * scale, NaN in its place and zeros elsewhere.
  *
  *   T, N, H       T >= 0, N >= 1, T * N < 2^31, 1 <= H <= CIS_NORM_MAX_H

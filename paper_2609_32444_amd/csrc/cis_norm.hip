@@ -180,13 +180,25 @@ __device__ __forceinline__ float e4m3_scale(uint32_t size) {
   const float s = __uint_as_float(size) / 448.f;
   return s < 0x1p-126f ? 0x1p-126f : s;
 }
+// 1 / scale in double, within 2^-52: the reciprocal in float32 is off by e (2^-22 at most), and e + e^2 of it is
+// added. The product of y with it, rounded to float32, is the quotient y / scale as float32 rounds it: of two
+// numbers of 24 bits the quotient is never a border between two float32 numbers, nor nearer to one than 2^-49 of
+// itself. (Quotients below float32's normal numbers are zeros of e4m3 either way.) In float32, y * (1 / scale)
+// gave 61 of the 1536000 values of 300 rows of 5120 the e4m3 number beside theirs; it took 5.5 us for 5.8, 132 for 133 of
+// 8192 rows of 8192. A division takes 6.2 and 133, and of 16384 rows of 2048 from the caches 24 us where this takes 20.4.
+__device__ __forceinline__ double e4m3_inverse(float scale) {
+  const double s = scale, x = __builtin_amdgcn_rcpf(scale), e = fma(-s, x, 1.0);
+  return scale == INFINITY ? 0.0 : fma(x, fma(e, e, e), x);
+}
 template <class R>
-__device__ __forceinline__ void store_e4m3(const R& row, int g, int H, const float (&f)[8], float inv) {
+__device__ __forceinline__ void store_e4m3(const R& row, int g, int H, const float (&f)[8],
+                                           double inv) {
+  auto over = [&](float y) __attribute__((always_inline)) { return (float)((double)y * inv); };
   uint32_t b[2];
 #pragma unroll
   for (int k = 0; k < 2; ++k) {
-    b[k] = __builtin_amdgcn_cvt_pk_fp8_f32(f[4 * k] * inv, f[4 * k + 1] * inv, 0, false);
-    b[k] = __builtin_amdgcn_cvt_pk_fp8_f32(f[4 * k + 2] * inv, f[4 * k + 3] * inv, b[k], true);
+    b[k] = __builtin_amdgcn_cvt_pk_fp8_f32(over(f[4 * k]), over(f[4 * k + 1]), 0, false);
+    b[k] = __builtin_amdgcn_cvt_pk_fp8_f32(over(f[4 * k + 2]), over(f[4 * k + 3]), b[k], true);
   }
   if ((g + 1) * 8 <= H) {
     row.store2(g, u32x2{b[0], b[1]});
@@ -370,7 +382,7 @@ __global__ __launch_bounds__(kRowBlock<LANES>) void cis_norm_row_kernel(const No
     for (int e = 0; e < 8; ++e) f[I][e] = f[I][e] * rstd * t[e];
   });
   if (a.ydt == CIS_E4M3) {
-    float inv = 0.f;
+    double inv = 0.0;
     if (a.group == 0) {
       uint32_t m = 0;
       static_for<NV>([&](auto I) __attribute__((always_inline)) {
@@ -379,7 +391,7 @@ __global__ __launch_bounds__(kRowBlock<LANES>) void cis_norm_row_kernel(const No
       });
       const float scale = e4m3_scale(row_max<LANES>(m, shm));
       if (l == 0 && on) a.scale[row] = scale;
-      inv = 1.f / scale;
+      inv = e4m3_inverse(scale);
     }
     // lanes of a block (or of a row that is shorter)
     const int per = lanes < a.group / 8 ? lanes : a.group / 8;
@@ -388,7 +400,7 @@ __global__ __launch_bounds__(kRowBlock<LANES>) void cis_norm_row_kernel(const No
       if (a.group) {
         const float scale = e4m3_scale(lanes_max(g < n8 ? size_of8(f[I]) : 0, per));
         if (g < n8 && (g & (per - 1)) == 0 && on) a.scale[(int64_t)row * a.blocks + g / (a.group / 8)] = scale;
-        inv = 1.f / scale;
+        inv = e4m3_inverse(scale);
       }
       if (g < n8 && on) store_e4m3(y, g, H, f[I], inv);
     });
@@ -597,7 +609,7 @@ __global__ __launch_bounds__(kNormBlock) void cis_norm_kernel(const NormArgs a) 
 #pragma unroll
     for (int e = 0; e < 8; ++e) f[e] = f[e] * rstd * w[e];
   };
-  float inv = 0.f;
+  double inv = 0.0;
   if (a.ydt == CIS_E4M3 && a.group == 0) {
     uint32_t m = 0;
     for (int g = tid; g < n8; g += kNormBlock) {
@@ -608,7 +620,7 @@ __global__ __launch_bounds__(kNormBlock) void cis_norm_kernel(const NormArgs a) 
     }
     const float scale = e4m3_scale(row_max<kNormBlock>(m, shm));
     if (tid == 0) a.scale[row] = scale;
-    inv = 1.f / scale;
+    inv = e4m3_inverse(scale);
   }
   for (int g0 = 0; g0 < n8; g0 += kNormBlock) {   // (whole waves together)
     const int g = g0 + tid;
@@ -619,7 +631,7 @@ __global__ __launch_bounds__(kNormBlock) void cis_norm_kernel(const NormArgs a) 
         const int lanes = a.group / 8;
         const float scale = e4m3_scale(lanes_max(size_of8(f), lanes));
         if (g < n8 && g % lanes == 0) a.scale[(int64_t)row * a.blocks + g / lanes] = scale;
-        inv = 1.f / scale;
+        inv = e4m3_inverse(scale);
       }
       if (g < n8) store_e4m3(y, g, H, f, inv);
     } else if (g < n8) {

@@ -5,7 +5,7 @@ there: one rounding, the same as torch's) and to the residual's type, and compar
   * rstd is formed in double and rounded once (u); y = (s rstd) w adds u twice, and the sums in double
     less than u in all: 4u, relative, and half a step of the output's type.
   * e4m3: scale is the largest |y| (4u) over 448 (u): 6u. The values stand for y: y / scale is off by
-    4u for y, 6u for the scale, 2u for the reciprocal and the product; then half a step of e4m3,
+    4u for y, 6u for the scale, u for the quotient (12u in all are allowed); then half a step of e4m3,
     2^-4 of the value or 2^-10 where it is below the least normal 2^-6.
   * dx = rstd (g - xh m) + dr, m = mean(g xh). g rounds once (u |g|). m = (sum of s g in double)
     rstd / H: u |m| for rstd and u |m| for its own rounding, and u mean(|g xh|) for the g that are
@@ -126,6 +126,43 @@ def test_e4m3_sizes(H, group):
     out = cis.rms_norm(x, w.contiguous(), r, eps=1e-5, out_dtype=F8, group=group)
     assert out["scale"].shape == ((T, (H + group - 1) // group) if group else (T,))
     _check_fwd(x, w, r, out, 1e-5, group)
+
+
+def _check_quotients(x, w, r, group, eps=1e-6):
+    """Scales and values from the same call's float32 y by the definition, bit for bit: y, the scale and the
+    quotient are one float32 rounding each, and that is rounded to e4m3."""
+    y = cis.rms_norm(x, w, r, eps=eps, out_dtype=F32)["y"]
+    out = cis.rms_norm(x, w, r, eps=eps, out_dtype=F8, group=group)
+    H = y.shape[-1]
+    n = group or H
+    blocks = torch.nn.functional.pad(y, (0, -H % n)).view(y.shape[0], -1, n)
+    top = blocks.abs().amax(2)
+    # (a quotient by a tensor: one by a number is a product with its reciprocal on the device)
+    scale = (top / torch.full_like(top, 448.0)).clamp(min=2.0 ** -126)
+    assert torch.equal(out["scale"].view(scale.shape), scale)
+    want = (blocks / scale[:, :, None]).view(y.shape[0], -1)[:, :H].to(F8)
+    off = out["y"].view(torch.uint8) != want.view(torch.uint8)
+    assert not off.any(), f"{int(off.sum())} of {off.numel()} values"
+
+
+@pytest.mark.parametrize("T,H", [(300, 5120), (600, 5120), (700, 2048), (20000, 72), (9000, 200), (3000, 516),
+                                 (200, 16384), (70, 32768), (60, 40001), (1, 2048)])
+@pytest.mark.parametrize("group", [0, 32, 64, 128])
+def test_e4m3_values_are_the_quotients_rounded(T, H, group):
+    """bf16 rows and weights have products of 16 bits, whose quotients often are halfway between two values."""
+    w = _rand((H,), BF, 3).contiguous()
+    _check_quotients(_rand((T, H), BF, 1), w, _rand((T, H), BF, 2, 3.0), group)
+    _check_quotients(_rand((T, H), F32, 4), None, None, group)
+
+
+@pytest.mark.parametrize("H", [64, 3000, 40000])
+def test_e4m3_quotients_of_extreme_scales(H):
+    """Scales at the least one and just above it (the values subnormal numbers of float32), and near the end of float32."""
+    x = torch.randn(9, H, generator=_gen(H), device=DEV)
+    for size in (2.0 ** -149, 2.0 ** -140, 2.0 ** -126, 2.0 ** -120, 2.0 ** -117, 2.0 ** -60, 2.0 ** 60, 2.0 ** 124):
+        w = torch.full((H,), size, device=DEV)
+        for group in (0, 32):
+            _check_quotients(_store(x, F32), w, None, group, eps=0.0)
 
 
 @pytest.mark.parametrize("T", [512, 513, 1100])
