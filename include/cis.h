@@ -75,8 +75,8 @@ enum {
                           /* workspace not 256-byte aligned                                   */
   CIS_ERR_LAUNCH = -6,    /* the HIP runtime rejected a kernel launch                         */
   CIS_ERR_WORKSPACE = -7, /* workspace smaller than cis_workspace_bytes(T)                    */
-  CIS_ERR_ALIAS = -8,     /* dlogits == logits with ld_g != ld, a partial overlap, or an
-                             LM-head gradient overlapping an operand or the workspace        */
+  CIS_ERR_ALIAS = -8,     /* an output overlaps another argument in a way that its entry point
+                             does not take: dlogits == logits with ld_g != ld, say            */
   CIS_ERR_DEVICE = -9,    /* the current device is not a gfx950 GPU, or no device            */
   CIS_ERR_SCRATCH = -10   /* T > CIS_NOALLOC_MAX_T (cis_loss_bwd_noalloc)                     */
 };

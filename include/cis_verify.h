@@ -68,8 +68,10 @@ size_t cis_verify_workspace_bytes(int64_t T, int64_t D, int64_t n_seq, int64_t V
  *   logp_out, logp_kept_out [T] float   NULL = not written
  *   workspace               >= cis_verify_workspace_bytes(T, draft_logits ? D : 0, n_seq, V, dtype)
  *                           bytes, 256-byte aligned
+ * No output overlaps another argument, nor does the workspace (as many bytes of it as are needed):
+ * CIS_ERR_ALIAS.
  * Errors: CIS_ERR_NULL, CIS_ERR_SHAPE (n_seq < 1 with T > 0 included), CIS_ERR_DTYPE, CIS_ERR_PARAM (as
- * for cis_sample), CIS_ERR_ALIGN, CIS_ERR_WORKSPACE, CIS_ERR_LAUNCH, CIS_ERR_DEVICE.
+ * for cis_sample), CIS_ERR_ALIGN, CIS_ERR_WORKSPACE, CIS_ERR_LAUNCH, CIS_ERR_DEVICE, CIS_ERR_ALIAS.
  */
 int cis_verify(const void* logits, int dtype, int64_t T, int64_t V, int64_t ld,
                const void* draft_logits, int64_t D, int64_t ld_d, const int64_t* draft_ids,

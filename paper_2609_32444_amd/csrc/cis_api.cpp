@@ -763,7 +763,8 @@ const char* cis_status_string(int status) {
              "workspace 256-byte aligned)";
     case CIS_ERR_LAUNCH: return "kernel launch failed";
     case CIS_ERR_WORKSPACE: return "workspace too small (see cis_workspace_bytes)";
-    case CIS_ERR_ALIAS: return "dlogits overlaps logits other than exactly in place (ld_g == ld)";
+    case CIS_ERR_ALIAS:
+      return "an output overlaps another argument (gradients other than exactly in place, ld_g == ld)";
     case CIS_ERR_DEVICE: return "current device is not a gfx950 GPU";
     case CIS_ERR_SCRATCH:
       return "T exceeds the fixed scratch of cis_loss_bwd_noalloc (CIS_NOALLOC_MAX_T = 262144 "

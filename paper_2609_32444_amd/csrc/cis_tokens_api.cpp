@@ -420,6 +420,17 @@ VerifyLayout verify_layout(int64_t T, int64_t D, int64_t n_seq, int64_t V, int d
   return L;
 }
 
+// The bytes of an argument (none where it is not given), and whether two have some in common.
+struct Bytes {
+  uintptr_t lo, hi;
+};
+Bytes bytes_of(const void* p, int64_t n, int64_t size) {
+  return Bytes{(uintptr_t)p, (uintptr_t)p + (p ? (uintptr_t)(n * size) : 0)};
+}
+bool overlap(Bytes a, Bytes b) {
+  return a.lo < a.hi && b.lo < b.hi && a.lo < b.hi && b.lo < a.hi;
+}
+
 }  // namespace
 
 extern "C" {
@@ -550,13 +561,28 @@ int cis_verify(const void* logits, int dtype, int64_t T, int64_t V, int64_t ld,
   if (n_seq > 0 && (!seq_offsets || !accepted_out)) return CIS_ERR_NULL;
   if (D > 0 && !draft_ids) return CIS_ERR_NULL;
   const int64_t Dl = draft_logits ? D : 0;   // rows of them
-  if (int rc = check_workspace(workspace, workspace_bytes,
-                               cis_verify_workspace_bytes(T, Dl, n_seq, V, dtype)))
-    return rc;
+  const size_t need = cis_verify_workspace_bytes(T, Dl, n_seq, V, dtype);
+  if (int rc = check_workspace(workspace, workspace_bytes, need)) return rc;
   if (T > 0 && !aligned_rows(logits, dtype, ld)) return CIS_ERR_ALIGN;
   if (Dl > 0 && !aligned_rows(draft_logits, dtype, ld_d)) return CIS_ERR_ALIGN;
   if (const int cus = device_cus(); cus < 0) return cus;
   if (n_seq == 0) return CIS_OK;
+  // ids are cleared while drafts are still to be read, and the workspace is written from the first kernel on
+  const int es = elem_bytes(dtype);
+  const Bytes out[] = {bytes_of(workspace, 1, (int64_t)need), bytes_of(ids_out, T, 8),
+                       bytes_of(accepted_out, n_seq, 4), bytes_of(logp_out, T, 4),
+                       bytes_of(logp_kept_out, T, 4)};
+  const Bytes in[] = {bytes_of(logits, T > 0 ? (T - 1) * ld + V : 0, es),
+                      bytes_of(draft_logits, Dl > 0 ? (Dl - 1) * ld_d + V : 0, es),
+                      bytes_of(draft_ids, D, 8), bytes_of(u, T, 4),
+                      bytes_of(seq_offsets, n_seq + 1, 8), bytes_of(temperature, n_seq, 4),
+                      bytes_of(top_k, n_seq, 4), bytes_of(top_p, n_seq, 4), bytes_of(min_p, n_seq, 4)};
+  for (const Bytes& o : out) {
+    for (const Bytes& i : in)
+      if (overlap(o, i)) return CIS_ERR_ALIAS;
+    for (const Bytes& p : out)
+      if (&p != &o && overlap(o, p)) return CIS_ERR_ALIAS;
+  }
 
   char* base = static_cast<char*>(workspace);
   const VerifyLayout L = verify_layout(T, Dl, n_seq, V, dtype);

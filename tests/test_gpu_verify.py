@@ -9,6 +9,7 @@ rounded once; logp is the difference of two logits and the log of a sum, whose e
 below 128 in base 2: 2^-24 (128 + 2 * 32) ln 2 and less than 2e-6 for exp2 and the sums, under 1e-5.
 """
 
+import ctypes
 import math
 
 import numpy as np
@@ -17,6 +18,7 @@ import torch
 
 import paper_2609_32444_amd as cis
 from oracle import tokens, verify as orc
+from paper_2609_32444_amd import _tokens, _verify
 
 pytestmark = pytest.mark.gpu
 DEV = "cuda"
@@ -432,6 +434,67 @@ def test_streams_graphs_and_repeats():
         torch.cuda.synchronize()
         assert same(call.out, want_a if rep % 2 else want_b)
         torch.randn(1000, 1000, device=DEV).sum().item()
+
+
+def _placed(n=2, T=6, D=4, V=64):
+    """The arguments of cis_verify in one buffer, apart from each other: (buffer, {name: (offset, bytes)})."""
+    need = cis.verify_workspace_bytes(T, D, n, V, F32)
+    sizes = dict(logits=T * V * 4, q=D * V * 4, ids=D * 8, u=T * 4, offs=(n + 1) * 8, temps=n * 4, ks=n * 4,
+                 ps=n * 4, ms=n * 4, out=T * 8, acc=n * 4, lp=T * 4, lk=T * 4, ws=need)
+    at, end = {}, 256
+    for name, size in sizes.items():
+        at[name] = (end, size)
+        end = (end + size + 255) // 256 * 256
+    buf = torch.zeros(end + 256, dtype=torch.uint8, device=DEV)
+    put = lambda name, t: buf[at[name][0]:][:at[name][1]].copy_(t.view(torch.uint8).view(-1))  # noqa: E731
+    logits, ids, u, offsets, q = _batch([3, 3], V, 1, F32)
+    for name, t in (("logits", logits), ("q", q), ("ids", ids), ("u", u),
+                    ("offs", torch.tensor(offsets, device=DEV)), ("temps", torch.ones(n, device=DEV)),
+                    ("ks", torch.zeros(n, dtype=torch.int32, device=DEV)), ("ps", torch.ones(n, device=DEV)),
+                    ("ms", torch.zeros(n, device=DEV))):
+        put(name, t.contiguous())
+    want = cis.verify(logits, ids, u, torch.tensor(offsets, device=DEV), q)
+    return buf, at, want
+
+
+def _call_placed(base, at, n=2, T=6, D=4, V=64, **moved):
+    p = {k: base + v[0] for k, v in at.items()}
+    p.update(moved)
+    prm = _tokens._SampleParams(1.0, 0, 1.0, 0.0)
+    return _verify._lib().cis_verify(
+        p["logits"], 1, T, V, V, p["q"], D, V, p["ids"], p["u"], p["offs"], n, ctypes.byref(prm), p["temps"],
+        p["ks"], p["ps"], p["ms"], p["out"], p["acc"], p["lp"], p["lk"], p["ws"], at["ws"][1],
+        torch.cuda.current_stream().cuda_stream)
+
+
+def test_overlapping_arguments_are_refused():
+    """Each output, and the workspace, on each other argument: at its first bytes and at its last ones."""
+    buf, at, want = _placed()
+    base = buf.data_ptr()
+    assert base % 256 == 0
+    keep = buf.clone()
+    outs = ("out", "acc", "lp", "lk", "ws")
+    for o in outs:
+        for a in at:
+            if a == o:
+                continue
+            first, last = base + at[a][0], base + at[a][0] + at[a][1]
+            step = 256 if o == "ws" else 8 if o == "out" else 4
+            for place in (first, (last - 1) // step * step):
+                assert _call_placed(base, at, **{o: place}) == -8, (o, a)
+            # and up to the first byte of it
+            place = first - at[o][1] + step
+            assert place % step or _call_placed(base, at, **{o: place}) == -8, (o, a)
+    torch.cuda.synchronize()
+    assert torch.equal(buf, keep)      # nothing was launched
+    assert _call_placed(base, at) == 0
+    got = lambda name, dt: buf[at[name][0]:][:at[name][1]].view(dt)  # noqa: E731
+    assert torch.equal(got("out", torch.int64), want["ids"])
+    assert torch.equal(got("acc", torch.int32), want["accepted"])
+    assert torch.equal(got("lp", F32), want["logp"]) and torch.equal(got("lk", F32), want["logp_kept"])
+    # side by side is no overlap
+    assert _call_placed(base, at, lp=base + at["out"][0] + at["out"][1]) == 0
+    torch.cuda.synchronize()
 
 
 def test_binding_refuses():
