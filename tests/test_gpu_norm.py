@@ -220,6 +220,76 @@ def test_backward_sizes(H):
         assert torch.equal(alone["dx"], out["dx"]) and "dweight" not in alone
 
 
+def _share(H):
+    """(parts of dweight's sums, rows that a part takes side by side) where there are rows enough for all parts."""
+    rows = 1 << 20
+    nbytes = cis.rms_norm_workspace_bytes(rows, 1, H) - (rows * 4 if H > 8192 else 0)
+    groups = (H + 7) // 8
+    side = 1 if groups > 64 else 256 // max(4, 1 << (groups - 1).bit_length())
+    return nbytes // (4 * H), side
+
+
+def _whole(T, H):
+    g = _gen(T + H)
+    return (torch.randint(-8, 9, (T, H), generator=g, device=DEV),
+            torch.randint(0, 2, (T, H), generator=g, device=DEV) * 2 - 1)
+
+
+def _check_turns(T, H, dt, xt, place=None, dr=True):
+    """Rows that a part's lanes take one after the other. A lane adds as many products as it takes turns, then those of
+    the rows beside it: dweight's tolerance is that count (turns + side, and 3 roundings a product), not the rows'. And with
+    rows of +-1, eps = 0 and whole numbers for dy every product and sum is exact, so that a row left out or
+    taken twice shows whatever its size."""
+    parts, side = _share(H)
+    turns = -(-T // (parts * side))
+    w = _rand((H,), F32, 2).contiguous()
+    d = _rand((T, H), xt, 60, 1e-3) if dr else None
+    buffers = lambda dy, s: (dy, s, {"dx": dy} if place == 0 else {"dx": s} if place == 1 else {})  # noqa: E731
+    dy, s = _rand((T, H), dt, T, 1e-3), _rand((T, H), xt, T + 1, 3.0)
+    dy_np, s_np = _np(dy), _np(s)
+    gy, gs, kw = buffers(dy, s)
+    out = cis.rms_norm_bwd(gy, gs, w, d, eps=1e-5, **kw)
+    dx, dw, size_w, size = orc.backward(dy_np, s_np, _np(w), float(np.float32(1e-5)), None if d is None else _np(d))
+    _near(out["dx"], dx, 9 * U * size + (U + HALF[out["dx"].dtype]) * np.abs(dx))
+    _near(out["dweight"], dw, (turns + side + 4) * U * size_w + U * np.abs(dw))
+    whole, sign = _whole(T, H)
+    gy, gs, kw = buffers(_store(whole, dt), _store(sign, xt))
+    out = cis.rms_norm_bwd(gy, gs, w, d, eps=0.0, **kw)
+    assert torch.equal(out["dweight"].long(), (whole * sign).sum(0))
+
+
+@pytest.mark.parametrize("H", [20, 64, 100, 128, 256, 391, 512, 1000, 2048, 3000, 4100, 5632, 8192])
+def test_backward_takes_rows_in_turn(H):
+    """One row more than all parts take at once, and several turns of which the last is of some parts."""
+    parts, side = _share(H)
+    all_at_once = parts * side
+    _check_turns(all_at_once + 1, H, BF, BF)
+    _check_turns(2 * all_at_once + side + 3, H, F32, BF, dr=False)
+    if H <= 512:
+        _check_turns(all_at_once + side // 2 + 1, H, F32, F32, place=1)
+        _check_turns(3 * all_at_once - 1, H, BF, F32, dr=False)
+    else:
+        _check_turns(4 * parts + 77, H, F32, F32, place=0)
+
+
+def test_backward_of_many_rows_to_the_last_one():
+    T = (1 << 21) + 77
+    for H, dt, xt in ((9, BF, BF), (40, F32, F32)):
+        whole, sign = _whole(T, H)
+        out = cis.rms_norm_bwd(_store(whole, dt), _store(sign, xt), eps=0.0)
+        assert torch.equal(out["dweight"].long(), (whole * sign).sum(0))
+
+
+@pytest.mark.parametrize("place", [None, 0, 1])
+@pytest.mark.parametrize("T,H", [(257, 8200), (700, 8200), (1300, 8200), (143, 16400), (76, 33001), (400, 33001)])
+def test_backward_of_long_rows_takes_them_in_turn(T, H, place):
+    """More rows than parts, a part's turns not a multiple of the loop's unrolling; in place, where the sums go first."""
+    parts, side = _share(H)
+    assert T > parts and side == 1
+    _check_turns(T, H, BF, BF, place)
+    _check_turns(T, H, F32, F32, place, dr=place is None)
+
+
 @pytest.mark.parametrize("D", [64, 128, 80, 200])
 def test_heads_of_a_packed_projection(D):
     """Queries and keys between others' columns, tokens or heads outermost, in place."""
