@@ -423,8 +423,12 @@ __global__ __launch_bounds__(kRowBlock<LANES>) void cis_norm_row_kernel(const No
 // unit: 6 waves of a group of 8 elements to a lane fit a SIMD (with 84 registers 5, which leaves a compute unit one
 // row of 9 waves for two: 38 us for 30; two groups to a lane 39), so that a row takes as many waves as it fills,
 // not a power of two of them (49). The next row asked for ahead costs a wave a SIMD and gains nothing (61, 39).
+// Of short rows in float32 throughout 5 waves fit: in the registers of 6 they would keep 3 to 5 words a lane in scratch
+// memory (us, 131072 rows of 256 83.5 for 86.0, 1048576 of 32 85.4 for 87.9; 262144 of 128 83 and 524288 of 64 83 both ways).
 template <class D, class X, int LANES>
-__global__ __launch_bounds__(LANES ? 256 : 1024) __attribute__((amdgpu_waves_per_eu(6)))
+constexpr int kGradEu = D::kPerVec == 4 && X::kPerVec == 4 && LANES > 0 && LANES < 64 ? 5 : 6;
+template <class D, class X, int LANES>
+__global__ __launch_bounds__(LANES ? 256 : 1024) __attribute__((amdgpu_waves_per_eu(kGradEu<D, X, LANES>)))
 void cis_norm_grad_row_kernel(const NormGradArgs a) {
   constexpr bool WAVES = LANES == 0;   // a workgroup of any number of waves to a row
   constexpr int NV = 1;                // groups to a lane
