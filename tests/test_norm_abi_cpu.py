@@ -5,7 +5,6 @@ import ctypes
 import os
 import re
 import shutil
-import struct
 import subprocess
 
 import pytest
@@ -13,6 +12,7 @@ import torch
 
 import paper_2609_32444_amd as cis
 from paper_2609_32444_amd import _norm
+from tests.code_objects import kernels
 
 ROOT = os.path.dirname(os.path.dirname(os.path.abspath(__file__)))
 AT = 0x10000000   # 256-byte aligned, never dereferenced on these paths
@@ -45,25 +45,11 @@ def test_workspace_sizes():
         assert cis.rms_norm_workspace_bytes(*bad) == 0
 
 
-def _kernels(path):
-    """The metadata of a built library's kernels: the message-pack notes of its device code objects."""
-    msgpack = pytest.importorskip("msgpack")
-    data, found = open(path, "rb").read(), []
-    name = b"AMDGPU\0\0"
-    at = data.find(name)
-    while at >= 0:
-        name_size, size, kind = struct.unpack("<III", data[at - 12:at])
-        if name_size == 7 and kind == 32:
-            found += msgpack.unpackb(data[at + 8:at + 8 + size])["amdhsa.kernels"]
-        at = data.find(name, at + 1)
-    return found
-
-
 def test_rows_stay_in_registers():
     """No kernel of the norm keeps a part of its rows in scratch memory."""
-    kernels = [k for k in _kernels(cis.library_path()) if "cis_norm" in k[".name"]]
-    assert len(kernels) >= 50
-    for k in kernels:
+    norm = [k for k in kernels(cis.library_path()) if "cis_norm" in k[".name"]]
+    assert len(norm) >= 50
+    for k in norm:
         assert k[".private_segment_fixed_size"] == 0 and k[".vgpr_spill_count"] == 0, k[".name"]
 
 

@@ -10,6 +10,7 @@ import torch
 
 import paper_2609_32444_amd as cis
 from paper_2609_32444_amd import _tokens
+from tests.code_objects import kernels
 
 ROOT = os.path.dirname(os.path.dirname(os.path.abspath(__file__)))
 FAKE = 0x10000   # a 256-byte aligned non-null address; never dereferenced on these paths
@@ -194,3 +195,11 @@ def test_top_k_beyond_int32_stays_beyond_every_row():
         assert field(k) == 2 ** 31 - 1   # V is 2^28 at most
     for k in (-1, -3, -2 ** 31 - 1, -2 ** 32):
         assert field(k) < 0
+
+
+def test_weights_of_uncut_rows_leave_eight_waves():
+    """The sampler's sum of uncut rows unpacks a vector at a time: at most 64 registers, 8 waves to a SIMD."""
+    weigh = [k for k in kernels(cis.library_path()) if "cis_weigh_kernel" in k[".name"] and "ELb0ELb0E" in k[".name"]]
+    assert len(weigh) == 2    # bf16 and float32
+    for k in weigh:
+        assert k[".vgpr_count"] <= 64, k[".name"]
