@@ -52,7 +52,8 @@ typedef struct cis_rows {
  *   x             bf16 or float32
  *   residual      NULL, or rows of x's type or float32
  *   weight        [H] bf16 or float32 (weight_dtype), 16-byte aligned; NULL = ones
- *   eps           >= 0, finite (0: a row of zeros gives NaN)
+ *   eps           >= 0, finite (0: a row of zeros gives NaN, and rstd, a float32, is infinite where the root is
+ *                 below 2^-128, which takes subnormal elements throughout)
  *   residual_out  s, in the residual's type; NULL = not written. Needs a residual.
  *   y             bf16, float32 or e4m3
  *   scale_out     [T * N, ceil(H / group)] float, with y in e4m3 (else NULL); [T * N] for group = 0

@@ -320,7 +320,7 @@ __device__ __forceinline__ uint32_t row_max(uint32_t m, uint32_t* sh) {
 // ------------------------------------------------------------------------------------------
 // LANES lanes to a row, which holds at most 8 * NV * LANES elements; LANES = 0: a workgroup, of as many waves
 // as the row fills. Bound by the memory: 16384 rows of 2048 in 48 us (5.6 TB/s; a copy reaches 6.2), 8192 of
-// 8192 to e4m3 in 130 (5.7). Few rows are bound by the steps' latency, 3.6 us for one.
+// 8192 to e4m3 in 133 (5.6). Few rows are bound by the steps' latency, 2.3 us for one.
 // ------------------------------------------------------------------------------------------
 template <int LANES>
 constexpr int kRowBlock = LANES == 0 ? 1024 : LANES > 256 ? LANES : 256;   // threads of a workgroup (at most)

@@ -198,8 +198,8 @@ __global__ __launch_bounds__(kHistBlock) void cis_step_kernel(const SampleArgs a
 // A wave's chunks one after the other, of one row in a workgroup: the sum of their weights, of a row
 // that top_p cuts those above the step of the cut, whose tokens are listed. A chunk whose largest logit
 // does not reach that far is not read. Without STEP, no row is cut by top_p. Bound by some 10
-// instructions a logit (24 us) and the second read of the row: 512 rows of V = 151936 in 32 us; with
-// STEP 256 rows of V = 262144, half of them peaked, in 21.
+// instructions a logit (24 us; 8 without a min_p) and the second read of the row: 512 rows of V = 151936 in
+// 30 us, 33 with a min_p; with STEP 256 rows of V = 262144, half of them peaked, in 21.
 // ------------------------------------------------------------------------------------------
 template <class E, bool STEP, bool KEEP>
 __global__ __launch_bounds__(kWeighBlock) void cis_weigh_kernel(const SampleArgs a) {
