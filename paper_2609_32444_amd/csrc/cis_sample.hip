@@ -130,7 +130,7 @@ __global__ __launch_bounds__(kHistBlock) void cis_hist_kernel(const SampleArgs a
   for (int i = tid; i < kFineSteps; i += kHistBlock) mass[i] = 0;
   const float* cmax = a.s.cmax + row * nch;
   const float M = row_max(cmax, nch, lane);
-  const __amdgpu_buffer_rsrc_t rs = tok_rsrc(a.r, row);
+  const __amdgpu_buffer_rsrc_t rs = tok_rsrc<KEEP>(a.r, row);
   float least = 0.f;
   for (int i = lane; i < nch; i += 64) least += fast_exp2(draw_exponent(cmax[i], M, p.c));
   least = 0.99f * wave_sum(least);
@@ -222,7 +222,7 @@ __global__ __launch_bounds__(kWeighBlock) void cis_weigh_kernel(const SampleArgs
     u64 s = 0;
     if (top >= -28.f && draw_step(top) <= step) {
       u32x4 x[kScanSlots];
-      load_chunk<E, 0>(tok_rsrc(a.r, row), a.r, ch, lane, x);
+      load_chunk<E, 0>(tok_rsrc<KEEP>(a.r, row), a.r, ch, lane, x);
       // which of the lane's tokens are in the step: a bit each, of 4 vectors to a word, the first
       // token's highest
       constexpr int kBits = 4 * EPV;
@@ -292,7 +292,7 @@ struct RowDraw {
   static constexpr int NW = BLOCK / 64, EPV = E::kPerVec;
   const SampleArgs& a;
   const RowParams& p;
-  RowSelect<E, BLOCK, LIST>& sel;
+  RowSelect<E, BLOCK, LIST, KEEP>& sel;
   SelectShared<LIST>& sh;
   int64_t row;
   float rest;   // sum of exp(z - M) over the row but one of its largest logits
@@ -1064,7 +1064,7 @@ __global__ __launch_bounds__(BLOCK) __attribute__((amdgpu_waves_per_eu(4))) void
   const int lane = threadIdx.x & 63;
   u64 mass0 = 0;
   if (row_weighed(p, a) && lane < a.s.nch) mass0 = a.draw[row * a.s.nch + lane];
-  RowSelect<E, BLOCK, LIST> sel(sh, a.r, a.s, row, p.ok, p.counted && p.top_k > 1);
+  RowSelect<E, BLOCK, LIST, KEEP> sel(sh, a.r, a.s, row, p.ok, p.counted && p.top_k > 1);
   if (!p.ok || !sel.tokens()) {
     if (threadIdx.x == 0) {
       if constexpr (KEEP) a.kept[row].id = -1;

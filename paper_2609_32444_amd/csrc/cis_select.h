@@ -112,7 +112,7 @@ __device__ __forceinline__ void sort_list(u64* list, int count) {
   __syncthreads();
 }
 
-template <class E, int BLOCK, int LIST>
+template <class E, int BLOCK, int LIST, bool DRAFTS = false>
 struct RowSelect {
   static constexpr int NW = BLOCK / 64, EPV = E::kPerVec;
   SelectShared<LIST>& sh;
@@ -133,7 +133,7 @@ struct RowSelect {
 
   __device__ __forceinline__ RowSelect(SelectShared<LIST>& s, const TokRows& r, const TokScan& t,
                                        int64_t row, bool on, bool groups)
-      : sh(s), rs(tok_rsrc(r, row)), V(r.V), nvec(r.nvec), ngrp(t.ngrp), gv(t.gv), nch(t.nch),
+      : sh(s), rs(tok_rsrc<DRAFTS>(r, row)), V(r.V), nvec(r.nvec), ngrp(t.ngrp), gv(t.gv), nch(t.nch),
         gm((const elem_t<E>*)t.gmax + row * t.ngrp), cmax(t.cmax + row * t.nch),
         csum(t.csum + row * t.nch) {
     const int tid = threadIdx.x, lane = tid & 63, wid = tid >> 6;

@@ -193,8 +193,8 @@ constexpr int kTopBlock = 256;
 constexpr int kWeighBlock = 256;
 constexpr int kDrawK = 1024;      // top_k up to which a row is drawn from a list
 constexpr int kDrawListK = 128;   // top_k that the kernel for short lists takes
-// keep: the logits stay in the caches for a later kernel's read
-const void* scan_kernel(int dtype, int32_t gv, bool keep);
+// keep: the logits stay in the caches for a later kernel's read; drafts: the rows are those of verification
+const void* scan_kernel(int dtype, int32_t gv, bool keep, bool drafts);
 // wide: any parameters; else top_k in [1, 128] for every row or nothing to cut but min_p. step: a row may be
 // cut by top_p alone. keep: for verification.
 struct DrawKernels {

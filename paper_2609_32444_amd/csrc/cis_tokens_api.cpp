@@ -108,7 +108,7 @@ int launch_scan(const cis::TokRows& r, const cis::TokScan& s, int dtype, float c
   const int64_t per = cis::kScanBlock / 64, need = (r.T * s.nch + per - 1) / per;
   // What fits the memory-side cache (256 MiB) is read from it later on.
   const bool keep = r.T * r.row_bytes <= int64_t(192) << 20;
-  return launch(cis::scan_kernel(dtype, s.gv, keep), need < kMaxBlocks ? need : kMaxBlocks,
+  return launch(cis::scan_kernel(dtype, s.gv, keep, r.offsets != nullptr), need < kMaxBlocks ? need : kMaxBlocks,
                 cis::kScanBlock, &a, stream);
 }
 

@@ -12,7 +12,7 @@ namespace cis {
 // logits than the memory-side cache holds are marked as not used again (6000 rows, K = 256: 54 us
 // less); those of fewer are not (512 uncut rows, which are read again: 70 to 65 us).
 // ------------------------------------------------------------------------------------------
-template <class E, int GV, int AUX>
+template <class E, int GV, int AUX, bool DRAFTS>
 __global__ __launch_bounds__(kScanBlock) void cis_scan_kernel(const ScanArgs a) {
   constexpr int EPV = E::kPerVec, K = kScanSlots, NW = kScanBlock / 64;
   const int lane = threadIdx.x & 63, wid = __builtin_amdgcn_readfirstlane(threadIdx.x) >> 6;
@@ -21,8 +21,8 @@ __global__ __launch_bounds__(kScanBlock) void cis_scan_kernel(const ScanArgs a) 
   for (int64_t w = (int64_t)blockIdx.x * NW + wid; w < total; w += (int64_t)gridDim.x * NW) {
     const int64_t row = w / nch;
     const int ch = (int)(w - row * nch);
-    if (a.r.offsets ? !tok_seq_on(a.r, row) : !tok_on(a.r, row)) continue;
-    const __amdgpu_buffer_rsrc_t rs = tok_rsrc(a.r, row);
+    if (DRAFTS ? !tok_seq_on(a.r, row) : !tok_on(a.r, row)) continue;
+    const __amdgpu_buffer_rsrc_t rs = tok_rsrc<DRAFTS>(a.r, row);
     const int v0 = ch * kScanVecs + lane;
     u32x4 x[K];
     load_chunk<E, AUX>(rs, a.r, ch, lane, x);
@@ -74,14 +74,18 @@ __global__ __launch_bounds__(kScanBlock) void cis_scan_kernel(const ScanArgs a) 
   }
 }
 
-const void* scan_kernel(int dtype, int32_t gv, bool keep) {
+template <bool DRAFTS>
+const void* scan_kernel_of(int dtype, int32_t gv, bool keep) {
 #define CIS_SCAN_G(E, G)                                       \
-  (keep ? (const void*)&cis_scan_kernel<E, G, 0>               \
-        : (const void*)&cis_scan_kernel<E, G, kAuxNT>)
+  (keep ? (const void*)&cis_scan_kernel<E, G, 0, DRAFTS>       \
+        : (const void*)&cis_scan_kernel<E, G, kAuxNT, DRAFTS>)
 #define CIS_SCAN(E) (gv == 0 ? CIS_SCAN_G(E, 0) : gv == 1 ? CIS_SCAN_G(E, 1) : CIS_SCAN_G(E, 8))
   return dtype == CIS_BF16 ? CIS_SCAN(Bf16) : CIS_SCAN(F32);
 #undef CIS_SCAN
 #undef CIS_SCAN_G
+}
+const void* scan_kernel(int dtype, int32_t gv, bool keep, bool drafts) {
+  return drafts ? scan_kernel_of<true>(dtype, gv, keep) : scan_kernel_of<false>(dtype, gv, keep);
 }
 
 // ------------------------------------------------------------------------------------------

@@ -57,14 +57,14 @@ struct Leftover {
   int V, draft;
   bool dist;    // the draft has a distribution
   __device__ __forceinline__ Leftover(const VerifyArgs& a, const VerifyStop& s, int64_t seq)
-      : p(a.kept[s.row]), rp(tok_rsrc(a.r, s.row)), V(a.r.V), draft(s.draft), dist(a.r.draft != nullptr) {
+      : p(a.kept[s.row]), rp(tok_rsrc<true>(a.r, s.row)), V(a.r.V), draft(s.draft), dist(a.r.draft != nullptr) {
     rho = 0.0;
     q = p;
     rq = rp;
     if (dist) {
       const int64_t d = a.r.T1 + s.row - seq;
       q = a.kept[d];
-      rq = tok_rsrc(a.r, d);
+      rq = tok_rsrc<true>(a.r, d);
       rho = (double)p.N / (double)q.N;
     }
   }
